@@ -137,6 +137,184 @@ int mopar_plan_slices(const mopar_layer_profile* layers, int32_t n, const mopar_
                       mopar_plan* out);
 
 /* ------------------------------------------------------------------------ */
+/* Decoding with a paged cache                                               */
+/* ------------------------------------------------------------------------ */
+
+/* The operators that a decoder-style language model needs beside its linear
+ * layers and norms, for callers that keep a key/value cache: rotary positions,
+ * storing keys and values in the cache's pages, causal attention over packed
+ * prompts, attention of newly drafted tokens over the cache, and keeping the
+ * accepted ones.  (Inside a model, MOPAR_OP_ROTARY and
+ * MOPAR_OP_CAUSAL_ATTENTION run the first and the third over whole sequences.)
+ * The conventions of this header hold: nothing is allocated, nothing
+ * synchronises, every call is one to three kernel launches on `stream`, fit
+ * for capture into a graph, and bitwise reproducible.
+ *
+ * Types.     MOPAR_F32 and MOPAR_BF16.  Dot products, softmax statistics,
+ *            weighted sums and rotations are float32, rounded once when
+ *            stored; with bf16 the softmax weights are rounded to bf16 before
+ *            they meet the values (they are at most 2^8, and their sum is
+ *            taken in float32 before the rounding).
+ * Rows.      A tensor of packed tokens is a mopar_rows: element (token t,
+ *            head h, dim i) at data + t * token_stride + h * head_stride + i,
+ *            strides in elements, so heads may sit inside wider fused rows or
+ *            tokens inside heads.  data is 16-byte aligned, both strides are
+ *            multiples of 16 bytes and not negative, 64 token strides span
+ *            less than 2 GiB, and the rows of an output must not overlap.
+ * Device     Offsets, positions, lengths, page numbers and paths are int32 on
+ * integers.  the device, read when the kernels run.  The host cannot check
+ *            them, so the kernels bound every access: a sequence is cut to
+ *            the tokens, cache and limits passed from the host, and a page
+ *            number outside the pool stands for an absent page -- its tokens
+ *            are not visible, and nothing is stored there. */
+
+typedef struct {
+    void* data;
+    int64_t token_stride;       /* elements */
+    int64_t head_stride;        /* elements */
+} mopar_rows;
+
+/* Rotary positions: the first rot_dim dims of a head form rot_dim / 2 pairs, and
+ * pair j of a token at position p turns by the angle p * w_j:
+ *   (x, y) -> m * (x cos - y sin, y cos + x sin).
+ * HALF pairs dims (j, j + rot_dim / 2), INTERLEAVED (2j, 2j + 1); the other dims
+ * pass unchanged.  With r = rot_dim, b = base, f = factor:
+ *   NONE    w_j = b^(-2j/r)
+ *   LINEAR  w_j = b^(-2j/r) / f                  (positions interpolated)
+ *   NTK     w_j = (b f^(r/(r-2)))^(-2j/r)        (base stretched; r > 2)
+ *   YARN    w_j = b^(-2j/r) (g + (1 - g) / f),   g = 0 .. 1 as the pair makes
+ *           beta_slow .. beta_fast turns (0, 0: 1 .. 32) within `context`
+ *           positions: g = clamp((context w / 2 pi - slow) / (fast - slow))
+ * m is mscale; 0 stands for 1, with YARN for 0.1 ln(f) + 1 (arXiv 2309.00071).
+ * Angles are taken modulo a full turn in 64-bit fixed point, so a far position
+ * costs no accuracy (error below 2^-32 turns for any int32 position). */
+typedef enum { MOPAR_ROTARY_HALF = 0, MOPAR_ROTARY_INTERLEAVED = 1 } mopar_rotary_layout;
+typedef enum {
+    MOPAR_ROTARY_NONE = 0,
+    MOPAR_ROTARY_LINEAR = 1,
+    MOPAR_ROTARY_NTK = 2,
+    MOPAR_ROTARY_YARN = 3
+} mopar_rotary_scaling;
+
+typedef struct {
+    int32_t layout;             /* mopar_rotary_layout                                            */
+    int32_t scaling;            /* mopar_rotary_scaling                                           */
+    int32_t head_dim;           /* multiple of 16 bytes of the rows it is used on, at most 256    */
+    int32_t rot_dim;            /* even, 2 .. head_dim                                            */
+    double base;                /* >= 1                                                           */
+    double factor;              /* >= 1; not read with NONE                                       */
+    double context;             /* YARN: the trained context, > 0                                 */
+    double beta_slow, beta_fast;/* YARN: 0 <= slow < fast; 0, 0 for 1, 32                         */
+    double mscale;              /* >= 0; 0 for the default                                        */
+} mopar_rotary_desc;
+
+typedef struct mopar_rotary_s* mopar_rotary_t;
+
+/* The angles of a descriptor as the kernels take them.  Host code only.
+ * Errors: MOPAR_E_ARG (null pointers, a field out of its range). */
+int mopar_rotary_create(const mopar_rotary_desc* desc, mopar_rotary_t* out);
+void mopar_rotary_destroy(mopar_rotary_t rotary);
+
+/* y = x turned, for `heads` heads (the rotary's head_dim) of `tokens` rows, row t
+ * at position pos_dev[t].  y may be x itself (same data and strides); any other
+ * overlap is undefined.  tokens or heads 0: nothing to do.
+ * Errors: MOPAR_E_ARG, MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (head_dim off the
+ * 16-byte granule, tokens * heads >= 2^31), MOPAR_E_HIP. */
+int mopar_rotary_apply(mopar_rotary_t rotary, int32_t dtype, int64_t tokens, int32_t heads, const int32_t* pos_dev,
+                       const mopar_rows* x, const mopar_rows* y, void* stream);
+
+/* A paged key/value cache of one layer.  Slot i of sequence s is row
+ * i mod page_tokens of page table_dev[s * table_stride + i / page_tokens]; page p
+ * of head h is page_tokens rows of head_dim at
+ * ((p * kv_heads + h) * page_tokens) * head_dim of k and of v (device, 16-byte
+ * aligned, any size: offsets are 64-bit).  A sequence has slots for
+ * max_pages * page_tokens tokens; further ones do not exist. */
+typedef struct {
+    int32_t dtype;
+    int32_t kv_heads;
+    int32_t head_dim;           /* a multiple of 16 bytes, at most 256 */
+    int32_t page_tokens;        /* a power of two, 1 .. 4096           */
+    int64_t pages;              /* pages in k and in v, 1 .. 2^31 - 1  */
+    void* k;
+    void* v;
+    const int32_t* table_dev;
+    int64_t table_stride;       /* entries between the rows of two sequences, >= max_pages */
+    int32_t max_pages;          /* entries of a sequence's row, >= 1                       */
+    int32_t n_seq;              /* rows of the table, >= 0                                 */
+} mopar_cache;
+
+/* Store key and value rows in the cache: row t goes to slot slot_dev[t] of sequence
+ * seq_dev[t].  With a rotary, keys turn by position pos_dev[t] on the way, and the
+ * `heads` query heads of q go to q_out turned the same (q_out may be q).  Without
+ * one (NULL), pos_dev, q and q_out are not read and keys are stored as they are.
+ * A row with seq or slot out of range, or on an absent page, is not stored (padding
+ * rows carry seq -1; their queries turn all the same).  Two rows for one slot: one
+ * of them is stored, which is not defined.
+ * heads 0: no queries (q and q_out may be NULL).
+ * Errors: as mopar_rotary_apply. */
+int mopar_cache_append(const mopar_cache* cache, mopar_rotary_t rotary, int64_t tokens, int32_t heads,
+                       const int32_t* pos_dev, const int32_t* seq_dev, const int32_t* slot_dev, const mopar_rows* q,
+                       const mopar_rows* q_out, const mopar_rows* k, const mopar_rows* v, void* stream);
+
+/* Heads and scale of an attention: query head h reads key/value head
+ * h / (heads / kv_heads). */
+typedef struct {
+    int32_t dtype;
+    int32_t heads, kv_heads;    /* heads a multiple of kv_heads      */
+    int32_t head_dim;           /* 32, 64, 96 or 128                 */
+    float scale;                /* > 0, finite; usually 1/sqrt(head_dim) */
+    int32_t reserved;
+} mopar_attention;
+
+/* Causal attention over packed prompts: sequence s is the rows
+ * offsets_dev[s] .. offsets_dev[s + 1] - 1 of q, k, v and out (n_seq + 1
+ * non-decreasing offsets, the first 0 or more, the last at most `tokens`), and row i
+ * of a sequence is the softmax(scale q_i . k_j) weighted sum of v_j over its rows
+ * j <= i.  max_len bounds the length of a sequence (a longer one is cut to its first
+ * max_len rows).  Rows of no sequence are neither read nor written, and what is not
+ * visible to a row -- infinities and NaN included -- does not reach it.  out must
+ * not overlap q, k or v.
+ * Errors: MOPAR_E_ARG, MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (head_dim), MOPAR_E_HIP. */
+int mopar_attention_prompt(const mopar_attention* a, int64_t tokens, int32_t n_seq, const int32_t* offsets_dev,
+                           int32_t max_len, const mopar_rows* q, const mopar_rows* k, const mopar_rows* v,
+                           const mopar_rows* out, void* stream);
+
+/* Attention of newly drafted tokens over the cache.  The drafted tokens of sequence s
+ * are the rows offsets_dev[s] .. offsets_dev[s + 1] - 1 of q and out (as above, of
+ * `tokens` rows; at most max_q a sequence); before them the sequence has len_dev[s]
+ * tokens, in slots 0 .. len_dev[s] - 1, and their own keys and values are already in
+ * the slots that follow, in order (mopar_cache_append).  Drafted token i sees the
+ * sequence's tokens before the draft and those drafted tokens j whose bit j mod 64 is set
+ * in word mask_dev[row * mask_words + j / 64] of its row -- its ancestors in the
+ * drafted tree and, normally, itself; bits past the draft do not count.  mask_dev
+ * NULL: tokens j <= i (one new token, or a chain of them).  A row that sees nothing
+ * gets zeros.  max_len >= 1 bounds len + drafted tokens; slots from max_len on are not
+ * read.  `ws` holds mopar_attention_cache_workspace_bytes; its contents need not
+ * survive between calls, and calls that overlap need one each.
+ * Errors: MOPAR_E_ARG (also a mask of fewer than ceil(max_q / 64) words),
+ * MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (head_dim; heads / kv_heads * max_q of 2^20
+ * and more), MOPAR_E_WORKSPACE, MOPAR_E_HIP. */
+int mopar_attention_cache_workspace_bytes(const mopar_attention* a, const mopar_cache* cache, int64_t tokens,
+                                          int32_t max_q, int32_t max_len, size_t* bytes);
+int mopar_attention_cache(const mopar_attention* a, const mopar_cache* cache, int64_t tokens, const int32_t* offsets_dev,
+                          int32_t max_q, const int32_t* len_dev, int32_t max_len, const uint64_t* mask_dev,
+                          int32_t mask_words, const mopar_rows* q, const mopar_rows* out, void* ws, size_t ws_bytes,
+                          void* stream);
+
+/* Keep the accepted path of a drafted tree: in each of `layers` caches (k and v of
+ * layer l start l * layer_stride elements after those of `cache`), slot
+ * len_dev[s] + path_dev[i] of sequence s moves to slot len_dev[s] + i - lo, for i = lo ..
+ * hi - 1 with lo, hi = path_offsets_dev[s], [s + 1] (non-decreasing, from 0 to at most
+ * `entries`).  Drafted indices of a path ascend (as ancestors do in any order that puts
+ * parents first); an index below its place i - lo, which no such path has, moves
+ * nothing, nor does one from or to an absent page.  max_path bounds a path's length; entries past it are left.
+ * Afterwards the sequence has len_dev[s] + (hi - lo) tokens.
+ * Errors: MOPAR_E_ARG, MOPAR_E_UNSUPPORTED, MOPAR_E_HIP. */
+int mopar_cache_keep(const mopar_cache* cache, int32_t layers, int64_t layer_stride, const int32_t* len_dev,
+                     const int32_t* path_offsets_dev, int64_t entries, const int32_t* path_dev, int32_t max_path,
+                     void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Model description                                                         */
 /* ------------------------------------------------------------------------ */
 

@@ -69,6 +69,28 @@ class Codec(ctypes.Structure):
                 ("b_enc", c_vp), ("w_dec", c_vp), ("b_dec", c_vp)]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("token_stride", c_i64), ("head_stride", c_i64)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("layout", c_i32), ("scaling", c_i32), ("head_dim", c_i32), ("rot_dim", c_i32), ("base", c_f64),
+                ("factor", c_f64), ("context", c_f64), ("beta_slow", c_f64), ("beta_fast", c_f64), ("mscale", c_f64)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("kv_heads", c_i32), ("head_dim", c_i32), ("page_tokens", c_i32), ("pages", c_i64),
+                ("k", c_vp), ("v", c_vp), ("table_dev", c_vp), ("table_stride", c_i64), ("max_pages", c_i32),
+                ("n_seq", c_i32)]
+
+
+class Attention(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("heads", c_i32), ("kv_heads", c_i32), ("head_dim", c_i32), ("scale", c_f32),
+                ("reserved", c_i32)]
+
+
+P_ROWS, P_CACHE, P_ATT = ctypes.POINTER(Rows), ctypes.POINTER(Cache), ctypes.POINTER(Attention)
+
 # every exported symbol of include/mopar.h, with its signature
 SIGNATURES = {
     "mopar_subslice_range": (c_i32, [c_i32, c_i32, c_i32, ctypes.POINTER(c_i32), ctypes.POINTER(c_i32)]),
@@ -100,6 +122,15 @@ SIGNATURES = {
     "mopar_model_cut_tensors": (c_i32, [c_vp, c_i32, ctypes.POINTER(c_i32), c_i32, ctypes.POINTER(c_i32)]),
     "mopar_model_measure": (c_i32, [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp,
                                     ctypes.POINTER(c_f64)]),
+    "mopar_rotary_create": (c_i32, [ctypes.POINTER(RotaryDesc), ctypes.POINTER(c_vp)]),
+    "mopar_rotary_destroy": (None, [c_vp]),
+    "mopar_rotary_apply": (c_i32, [c_vp, c_i32, c_i64, c_i32, c_vp, P_ROWS, P_ROWS, c_vp]),
+    "mopar_cache_append": (c_i32, [P_CACHE, c_vp, c_i64, c_i32, c_vp, c_vp, c_vp, P_ROWS, P_ROWS, P_ROWS, P_ROWS, c_vp]),
+    "mopar_cache_keep": (c_i32, [P_CACHE, c_i32, c_i64, c_vp, c_vp, c_i64, c_vp, c_i32, c_vp]),
+    "mopar_attention_prompt": (c_i32, [P_ATT, c_i64, c_i32, c_vp, c_i32, P_ROWS, P_ROWS, P_ROWS, P_ROWS, c_vp]),
+    "mopar_attention_cache_workspace_bytes": (c_i32, [P_ATT, P_CACHE, c_i64, c_i32, c_i32, ctypes.POINTER(ctypes.c_size_t)]),
+    "mopar_attention_cache": (c_i32, [P_ATT, P_CACHE, c_i64, c_vp, c_i32, c_vp, c_i32, c_vp, c_i32, P_ROWS, P_ROWS, c_vp,
+                                      ctypes.c_size_t, c_vp]),
     "mopar_last_error": (ctypes.c_char_p, []),
     "mopar_version": (ctypes.c_char_p, []),
 }

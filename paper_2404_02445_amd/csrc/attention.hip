@@ -1,0 +1,678 @@
+// Attention of decoder-style models (gfx950): causal attention over packed prompts, and attention of newly
+// drafted tokens over a paged cache.  One pass over the keys with the running maximum and sum of the softmax.
+//
+// Tiles.  A wave owns 32 query rows.  Scores come out transposed, S^T = K Q^T on the 32x32 MFMA (key fragment
+// first): a lane holds one query (lane % 32) and, in register i, key 8 (i / 4) + 4 (lane / 32) + i % 4 of a 32-key
+// tile, so a row's maximum and sum are in-lane but for one exchange with lane ^ 32, the statistics are one
+// register per lane, and the weights are already in the layout of the second product's B operand, O^T = V^T P^T
+// -- the k index of an MFMA may run over the keys in any order that both operands share, so P never leaves the
+// registers.  V^T fragments come from row-major V in LDS by transposing reads (bf16) or element reads (float32).
+//
+// Keys and values stream to LDS with 16-byte direct loads, two stages; a row of LDS is the head's dims, a power
+// of two of 16-byte chunks, chunk c of row r at place c ^ f(r) (swizzle()), which keeps both the fragment reads
+// of K (32 rows, one chunk) and those of V (four rows, 64 bytes) off each other's banks.
+#include <algorithm>
+#include <type_traits>
+
+#include "internal.h"
+
+namespace mopar {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+typedef const __attribute__((address_space(1))) void* gptr_t;
+
+// what absent keys and values are read from
+__device__ __attribute__((aligned(16))) const unsigned int kZeros[4] = {0u, 0u, 0u, 0u};
+
+constexpr float kNoMax = -3.40282347e38f;    // running maximum of a row that has seen no key
+
+struct AttnParams {
+    const unsigned char *q, *k, *v;
+    unsigned char* out;
+    int64_t q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs;   // bytes
+    const int32_t* offsets;          // null: n_seq sequences of max_rows rows
+    int n_seq, max_rows;             // rows (tokens) of a sequence at most
+    int64_t tokens;
+    int heads, kv_heads, group;
+    float c;                         // scale * log2(e): weights are powers of two
+    // cache
+    const int32_t *table, *len;
+    int64_t table_stride, pages;
+    int max_pages, shift, max_len;
+    const uint64_t* mask;
+    int mask_words;
+    // the parts of the key axis
+    int part_keys, parts;
+    float *part, *stat;
+    int row_tiles;                   // blocks of rows per (sequence, head)
+};
+
+constexpr int pow2_up(int v) { int p = 1; while (p < v) p *= 2; return p; }
+
+template <typename T, int D> struct Geo {
+    static constexpr int ES = sizeof(T), EPC = 16 / ES;
+    static constexpr int CH = D / EPC;           // chunks of a row
+    static constexpr int RS = pow2_up(CH);       // chunk places of a row in LDS
+    static constexpr int RB = RS * 16;           // bytes of a row in LDS
+};
+
+// Chunk c of row r sits at place c ^ swizzle(r): linear in the bits of r.
+template <int RS> __host__ __device__ constexpr int swizzle(int r) {
+    if (RS >= 16) return ((r & 3) << 2) | ((r >> 2) & 3);
+    if (RS == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    return (r >> 2) & 3;
+}
+
+template <int OFF> __device__ __forceinline__ u32x4 lds_read16(unsigned addr) {
+    static_assert(OFF >= 0 && OFF < 65536, "ds offset");
+    u32x4 v;
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+    return v;
+}
+template <int OFF> __device__ __forceinline__ u32x2 lds_read_tr(unsigned addr) {
+    static_assert(OFF >= 0 && OFF < 65536, "ds offset");
+    u32x2 v;
+    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+    return v;
+}
+template <int OFF> __device__ __forceinline__ unsigned lds_read4(unsigned addr) {
+    static_assert(OFF >= 0 && OFF < 65536, "ds offset");
+    unsigned v;
+    asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+    return v;
+}
+__device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+template <typename V> __device__ __forceinline__ void pin(V& v) { asm volatile("" : "+v"(v)); }
+
+template <int N, typename F, int I = 0> __device__ __forceinline__ void static_for(F&& f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<N, F, I + 1>(static_cast<F&&>(f));
+    }
+}
+
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+
+// a sequence's rows [start, start + rows) of the packed tensors
+__device__ __forceinline__ void rows_of(const AttnParams& p, int s, int64_t& start, int& rows) {
+    if (!p.offsets) {
+        start = static_cast<int64_t>(s) * p.max_rows;
+        rows = p.max_rows;
+        return;
+    }
+    const int64_t lo = min(max(static_cast<int64_t>(p.offsets[s]), int64_t(0)), p.tokens);
+    const int64_t hi = min(static_cast<int64_t>(p.offsets[s + 1]), p.tokens);
+    start = lo;
+    rows = static_cast<int>(min(max(hi - lo, int64_t(0)), static_cast<int64_t>(p.max_rows)));
+}
+
+// WR waves take 32 RT rows each, WK waves share a row tile and take every WK-th 32-key tile.
+template <typename T, int D, int WR, int WK, int RT, int SUBS, bool PAGED>
+__global__ __launch_bounds__(WR * WK * 64) void attention_kernel(const AttnParams p) {
+    using G = Geo<T, D>;
+    constexpr int ES = G::ES, CH = G::CH, RS = G::RS, RB = G::RB, DT = D / 32;
+    constexpr int NW = WR * WK;
+    constexpr int BM = WR * RT * 32;                 // rows of a block
+    constexpr int KT = 32 * SUBS * WK;               // keys of a stage
+    constexpr int TILE = KT * RB;                    // bytes of K (or V) in a stage
+    constexpr int NBLK = TILE / 1024, LPW = (NBLK + NW - 1) / NW;
+    constexpr int MERGE = WK > 1 ? WK * BM * (D + 4) * 4 + WK * BM * 8 : 0;
+    constexpr int LDS = 4 * TILE > MERGE ? 4 * TILE : MERGE;
+    static_assert(TILE % 1024 == 0, "whole load blocks");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wr = wave % WR, wk = wave / WR;
+    const int lr = lane & 31, lh = lane >> 5;
+
+    // --- what this block does ------------------------------------------------------------------
+    int64_t start;
+    int rows, kvh, head = 0, tile, part = 0, s;
+    if constexpr (PAGED) {
+        int b = blockIdx.x;
+        part = b % p.parts;
+        b /= p.parts;
+        tile = b % p.row_tiles;
+        b /= p.row_tiles;
+        kvh = b % p.kv_heads;
+        s = b / p.kv_heads;
+        rows_of(p, s, start, rows);
+    } else {
+        head = blockIdx.x % p.heads;
+        kvh = head / p.group;
+        int item = blockIdx.x / p.heads;
+        for (s = 0;; ++s) {
+            if (s >= p.n_seq) return;
+            rows_of(p, s, start, rows);
+            const int nt = (rows + BM - 1) / BM;
+            if (item < nt) break;
+            item -= nt;
+        }
+        tile = item;
+    }
+    const int group = PAGED ? p.group : 1;
+    const int nrow = rows * group;                    // query rows: tokens, times the heads of a group over a cache
+    const int row0 = tile * BM;
+    if (row0 >= nrow) return;
+    const int past = PAGED ? min(max(p.len[s], 0), p.max_len) : 0;     // tokens before the first query's
+    const int total = PAGED ? min(min(past + rows, p.max_len), p.max_pages << p.shift) : rows;
+    // keys of this block: [key0, key1)
+    const int key0 = PAGED ? part * p.part_keys : 0;
+    int key1 = PAGED ? min(total, key0 + p.part_keys) : min(total, row0 + BM);
+    if (PAGED && key0 >= total && part > 0) return;   // (part 0 of an empty sequence stores zeros)
+    const bool whole = !PAGED || total <= p.part_keys;   // no other part: results, not partial sums
+
+    // --- rows of this wave ---------------------------------------------------------------------
+    int qtok[RT];                                     // the row's token within the sequence
+    u32x4 qf[RT][CH / 2];
+    const unsigned char* qrow[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int row = min(row0 + (wr * RT + r) * 32 + lr, nrow - 1);
+        qtok[r] = row / group;
+        const int h = PAGED ? kvh * group + (row - qtok[r] * group) : head;
+        qrow[r] = p.q + (start + qtok[r]) * p.q_ts + h * p.q_hs;
+#pragma unroll
+        for (int i = 0; i < CH / 2; ++i) qf[r][i] = *reinterpret_cast<const u32x4*>(qrow[r] + (2 * i + lh) * 16);
+    }
+
+    // --- loads -----------------------------------------------------------------------------------
+    // Block b of a stage is rows b * 64 / RS ..; lane l fills place l % RS of row (b * 64 + l) / RS.
+    const unsigned char* const kbase = p.k + (PAGED ? 0 : start * p.k_ts + kvh * p.k_hs);
+    const unsigned char* const vbase = p.v + (PAGED ? 0 : start * p.v_ts + kvh * p.v_hs);
+    const unsigned char* const zeros = reinterpret_cast<const unsigned char*>(kZeros);
+    auto issue = [&](int k0, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < LPW; ++j) {
+            const int b = wave + NW * j;
+            if (NBLK % NW != 0 && b >= NBLK) continue;
+            const int row = (b * 64 + lane) / RS, ch = (lane % RS) ^ swizzle<RS>(row);
+            const int key = k0 + row;
+            const unsigned char *ks = zeros, *vs = zeros;
+            if (key < key1 && ch < CH) {
+                if constexpr (PAGED) {
+                    const int page = p.table[s * p.table_stride + (key >> p.shift)];
+                    if (page >= 0 && page < p.pages) {
+                        const int64_t off = (((page * static_cast<int64_t>(p.kv_heads) + kvh) << p.shift) + (key & ((1 << p.shift) - 1))) *
+                                                (D * ES) + ch * 16;
+                        ks = kbase + off;
+                        vs = vbase + off;
+                    }
+                } else {
+                    ks = kbase + key * p.k_ts + ch * 16;
+                    vs = vbase + key * p.v_ts + ch * 16;
+                }
+            }
+            __builtin_amdgcn_global_load_lds((gptr_t)ks, (lds_ptr_t)(lds + buf * 2 * TILE + b * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((gptr_t)vs, (lds_ptr_t)(lds + buf * 2 * TILE + TILE + b * 1024), 16, 0, 0);
+        }
+    };
+
+    // --- state -----------------------------------------------------------------------------------
+    f32x16 o[RT][DT];
+    float m[RT], l[RT];                               // maximum (times c) so far; this lane's share of the sum
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        m[r] = kNoMax;
+        l[r] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[r][d][i] = 0.0f;
+    }
+    const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_ptr_t)lds));
+    // K fragment: row lr, chunk 2 st + lh;  V fragment (bf16): row 4 lh + (lane % 16) / 4 of eight, dims 16 ((lane / 16) % 2)
+    // + 4 (lane % 4) of 32; (float32): row 4 lh, dim lr of 32
+    const unsigned ka = lds0 + static_cast<unsigned>(lr * RB + ((lh ^ swizzle<RS>(lr)) << 4));
+    unsigned va;
+    if constexpr (ES == 2) {
+        const int row = 4 * lh + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        va = lds0 + static_cast<unsigned>(TILE + row * RB + ((ch ^ swizzle<RS>(row)) << 4) + (lane & 1) * 8);
+    } else {
+        const int row = 4 * lh, ch = lr >> 2;
+        va = lds0 + static_cast<unsigned>(TILE + row * RB + ((ch ^ swizzle<RS>(row)) << 4) + (lr & 3) * 4);
+    }
+
+    // visible keys of a row among 64 from k0 on, one bit each
+    auto visible = [&](int r, int k0) -> uint64_t {
+        const int own = total - past;                 // drafted tokens within bounds
+        auto ones = [](int n) -> uint64_t { return n <= 0 ? 0 : n >= 64 ? ~uint64_t(0) : (uint64_t(1) << n) - 1; };
+        if (!PAGED || !p.mask) return ones(min(past + qtok[r] + 1, key1) - k0);
+        const uint64_t* mrow = p.mask + (start + qtok[r]) * p.mask_words;
+        const int j0 = k0 - past;
+        uint64_t bits;
+        if (j0 >= 0) {
+            const int w = j0 >> 6, sh = j0 & 63;
+            const uint64_t lo = w < p.mask_words ? mrow[w] : 0, hi = w + 1 < p.mask_words ? mrow[w + 1] : 0;
+            bits = (sh ? (lo >> sh) | (hi << (64 - sh)) : lo) & ones(own - j0);
+        } else {
+            bits = ones(-j0) | (-j0 < 64 ? (mrow[0] & ones(own)) << -j0 : 0);
+        }
+        return bits & ones(key1 - k0);
+    };
+
+    // one 32-key tile: scores, weights and products
+    auto tile32 = [&](int buf, auto sub, int k0) __attribute__((always_inline)) {
+        const int st0 = buf * 2 * TILE + (WK > 1 ? wk * 32 * RB : 0);
+        f32x16 sc[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[r][i] = 0.0f;
+        {
+            u32x4 kf[CH / 2];
+            static_for<CH / 2>([&](auto st) __attribute__((always_inline)) { kf[st] = lds_read16<sub * 32 * RB>((ka + st0) ^ (st << 5)); });
+            lds_wait();
+            static_for<CH / 2>([&](auto st) __attribute__((always_inline)) {
+                pin(kf[st]);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    if constexpr (ES == 2)
+                        sc[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[st]), __builtin_bit_cast(bf16x8, qf[r][st]),
+                                                                        sc[r], 0, 0, 0);
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            sc[r] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[st][e]), __uint_as_float(qf[r][st][e]), sc[r], 0, 0, 0);
+                }
+            });
+        }
+        // keys that some row of this wave does not see
+        const bool cut = k0 + 32 > key1 || k0 + 32 > past + (PAGED ? (p.mask ? 0 : qtok[0]) : 0);
+        bool masked = false;
+        uint64_t vis[RT];
+        if (__any(cut)) {
+            masked = true;
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                vis[r] = visible(r, k0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!((vis[r] >> (8 * (i / 4) + 4 * lh + i % 4)) & 1)) sc[r][i] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float mx = sc[r][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[r][i]);
+            mx = fmaxf(mx, other_half(mx)) * p.c;
+            const float mn = fmaxf(m[r], mx), f = __builtin_amdgcn_exp2f(m[r] - mn);
+            m[r] = mn;
+            l[r] *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[r][d][i] *= f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                sc[r][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r][i], p.c, -mn));
+                l[r] += sc[r][i];
+            }
+        }
+        // O^T += V^T P^T
+        constexpr int STEPS = ES == 2 ? 2 : 4;        // groups of registers whose V fragments are read together
+        static_for<STEPS>([&](auto u) __attribute__((always_inline)) {
+            constexpr int PER = 16 / STEPS;           // score registers of a group
+            bf16x8 pf[RT];
+            if constexpr (ES == 2)
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) pf[r][i] = static_cast<__bf16>(sc[r][8 * u + i]);
+            u32x4 vf[DT];
+            if constexpr (ES == 2) {
+                static_for<DT>([&](auto d) __attribute__((always_inline)) {
+                    const u32x2 lo = lds_read_tr<(sub * 32 + u * 16) * RB>((va + st0) ^ (d << 6));
+                    const u32x2 hi = lds_read_tr<(sub * 32 + u * 16 + 8) * RB>((va + st0) ^ ((d << 6) | (swizzle<RS>(8) << 4)));
+                    vf[d] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                });
+            } else {
+                static_for<DT>([&](auto d) __attribute__((always_inline)) {
+                    static_for<4>([&](auto e) __attribute__((always_inline)) {
+                        constexpr int row = 8 * u + e, el = e;
+                        vf[d][el] = lds_read4<(sub * 32 + row) * RB>((va + st0) ^ ((d << 7) ^ (swizzle<RS>(row) << 4)));
+                    });
+                });
+            }
+            lds_wait();
+#pragma unroll
+            for (int d = 0; d < DT; ++d) pin(vf[d]);
+            // Where a row does not see every key, an infinity or NaN among the values must not meet its zero weight
+            bool special = false;
+            if (masked) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        special |= ES == 2 ? (((vf[d][e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0
+                                           : (vf[d][e] & 0x7f800000u) == 0x7f800000u;
+                special = __any(special);
+            }
+            if (!special) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        if constexpr (ES == 2)
+                            o[r][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d]), pf[r], o[r][d], 0, 0, 0);
+                        else
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                o[r][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(vf[d][e]), sc[r][4 * u + e], o[r][d], 0, 0, 0);
+                    }
+            } else {
+                // one key at a time, added only where it is seen
+                for (int key = 0; key < 2 * PER; ++key) {
+                    const int kh = (key >> 2) & 1, kr = (key & 3) + 4 * (key >> 3);       // half and register of the key
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        const bool seen = (vis[r] >> (u * 2 * PER + key)) & 1;
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            f32x16 one;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) one[i] = 0.0f;
+                            if constexpr (ES == 2) {
+                                u32x4 w = vf[d];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    w[e] &= lh != kh || (kr >> 1) != e ? 0u : (kr & 1) ? 0xffff0000u : 0xffffu;
+                                one = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf[r], one, 0, 0, 0);
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    one = __builtin_amdgcn_mfma_f32_32x32x2f32(lh == kh && kr == e ? __uint_as_float(vf[d][e]) : 0.0f,
+                                                                               sc[r][4 * u + e], one, 0, 0, 0);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[r][d][i] += seen ? one[i] : 0.0f;
+                        }
+                    }
+                }
+            }
+        });
+    };
+
+    // --- the keys ----------------------------------------------------------------------------------
+    // rows of this wave, all of them past the last visible key of the tile: nothing to do (causal)
+    const int wave_end = PAGED ? key1 : min(key1, row0 + (wr + 1) * RT * 32);
+    if (key0 < key1) issue(key0, 0);
+    int buf = 0;
+    for (int k0 = key0; k0 < key1; k0 += KT, buf ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (k0 + KT < key1) issue(k0 + KT, buf ^ 1);
+        static_for<SUBS>([&](auto sub) __attribute__((always_inline)) {
+            const int k = k0 + (WK > 1 ? wk * 32 : 0) + sub * 32;
+            if (k < wave_end) tile32(buf, sub, k);
+        });
+    }
+
+    // --- results -----------------------------------------------------------------------------------
+#pragma unroll
+    for (int r = 0; r < RT; ++r) l[r] += other_half(l[r]);
+    if constexpr (WK == 1) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int row = row0 + (wr * RT + r) * 32 + lr;
+            if (row >= nrow) continue;
+            const int h = PAGED ? kvh * group + (row - qtok[r] * group) : head;
+            if (whole) {
+                const float inv = l[r] != 0.0f ? 1.0f / l[r] : 0.0f;
+                unsigned char* dst = p.out + (start + qtok[r]) * p.o_ts + h * p.o_hs;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x4 v = {o[r][d][4 * i] * inv, o[r][d][4 * i + 1] * inv, o[r][d][4 * i + 2] * inv, o[r][d][4 * i + 3] * inv};
+                        const int dim = d * 32 + 8 * i + 4 * lh;
+                        if constexpr (ES == 2)
+                            *reinterpret_cast<bf16x4*>(dst + dim * 2) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+                        else
+                            *reinterpret_cast<f32x4*>(dst + dim * 4) = v;
+                    }
+            } else {
+                const int64_t at = ((start + qtok[r]) * p.heads + h) * p.parts + part;
+                if (lh == 0) {
+                    p.stat[2 * at] = m[r];
+                    p.stat[2 * at + 1] = l[r];
+                }
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<f32x4*>(p.part + at * D + d * 32 + 8 * i + 4 * lh) =
+                            f32x4{o[r][d][4 * i], o[r][d][4 * i + 1], o[r][d][4 * i + 2], o[r][d][4 * i + 3]};
+            }
+        }
+    } else {
+        // the waves of a row tile meet in LDS
+        static_assert(RT == 1 || WK == 1, "one row tile a wave");
+        constexpr int LD = D + 4;
+        __syncthreads();                              // the last stage has been read
+        float* const os = reinterpret_cast<float*>(lds);
+        float* const ms = os + WK * BM * LD;
+        {
+            const int row = wr * 32 + lr;
+            float* dst = os + (wk * BM + row) * LD + 4 * lh;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<f32x4*>(dst + d * 32 + 8 * i) = f32x4{o[0][d][4 * i], o[0][d][4 * i + 1], o[0][d][4 * i + 2], o[0][d][4 * i + 3]};
+            if (lh == 0) {
+                ms[(wk * BM + row) * 2] = m[0];
+                ms[(wk * BM + row) * 2 + 1] = l[0];
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < BM * (D / 4); i += NW * 64) {
+            const int rr = i / (D / 4), dim = (i - rr * (D / 4)) * 4, row = row0 + rr;
+            if (row >= nrow) continue;
+            float top = kNoMax, sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) top = fmaxf(top, ms[(w * BM + rr) * 2]);
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < WK; ++w) {
+                const float f = __builtin_amdgcn_exp2f(ms[(w * BM + rr) * 2] - top);
+                sum += ms[(w * BM + rr) * 2 + 1] * f;
+                acc += *reinterpret_cast<const f32x4*>(os + (w * BM + rr) * LD + dim) * f;
+            }
+            const int tok = row / group, h = PAGED ? kvh * group + (row - tok * group) : head;
+            if (whole) {
+                const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+                unsigned char* dst = p.out + (start + tok) * p.o_ts + h * p.o_hs;
+                acc *= inv;
+                if constexpr (ES == 2)
+                    *reinterpret_cast<bf16x4*>(dst + dim * 2) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
+                else
+                    *reinterpret_cast<f32x4*>(dst + dim * 4) = acc;
+            } else {
+                const int64_t at = ((start + tok) * p.heads + h) * p.parts + part;
+                if (dim == 0) {
+                    p.stat[2 * at] = top;
+                    p.stat[2 * at + 1] = sum;
+                }
+                *reinterpret_cast<f32x4*>(p.part + at * D + dim) = acc;
+            }
+        }
+    }
+}
+
+// Partial sums of a row's parts, in order: 32 threads a row.  Rows whose sequence has one part are done already.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p) {
+    const int s = blockIdx.y;
+    int64_t start;
+    int rows;
+    rows_of(p, s, start, rows);
+    const int past = min(max(p.len[s], 0), p.max_len);
+    const int total = min(min(past + rows, p.max_len), p.max_pages << p.shift);
+    const int parts = (total + p.part_keys - 1) / p.part_keys;
+    if (parts <= 1) return;
+    for (int row = blockIdx.x * 8 + threadIdx.x / 32; row < rows * p.heads; row += gridDim.x * 8) {
+        const int tok = row / p.heads, h = row - tok * p.heads;
+        const int64_t at = ((start + tok) * p.heads + h) * p.parts;
+        float top = kNoMax, sum = 0.0f;
+        for (int i = 0; i < parts; ++i) top = fmaxf(top, p.stat[2 * (at + i)]);
+        float acc[D / 32] = {};
+        for (int i = 0; i < parts; ++i) {
+            const float f = __builtin_amdgcn_exp2f(p.stat[2 * (at + i)] - top);
+            sum += p.stat[2 * (at + i) + 1] * f;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) acc[d] += p.part[(at + i) * D + d * 32 + (threadIdx.x & 31)] * f;
+        }
+        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+        T* dst = reinterpret_cast<T*>(p.out + (start + tok) * p.o_ts + h * p.o_hs);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) dst[d * 32 + (threadIdx.x & 31)] = static_cast<T>(acc[d] * inv);
+    }
+}
+
+void set_rows(AttnParams& p, int es, const mopar_rows* q, const mopar_rows* out) {
+    p.q = static_cast<const unsigned char*>(q->data);
+    p.q_ts = q->token_stride * es;
+    p.q_hs = q->head_stride * es;
+    p.out = static_cast<unsigned char*>(out->data);
+    p.o_ts = out->token_stride * es;
+    p.o_hs = out->head_stride * es;
+}
+
+template <typename F> hipError_t by_type(int dtype, int d, F&& go) {
+    auto dims = [&](auto t) {
+        switch (d) {
+            case 32: return go(t, std::integral_constant<int, 32>{});
+            case 64: return go(t, std::integral_constant<int, 64>{});
+            case 96: return go(t, std::integral_constant<int, 96>{});
+            default: return go(t, std::integral_constant<int, 128>{});
+        }
+    };
+    return dtype == MOPAR_BF16 ? dims(__bf16{}) : dims(float{});
+}
+
+// Keys of a part: the least multiple of 256 that leaves no more than about two blocks a CU over all
+// sequences at their longest.
+struct CacheSplit {
+    int part_keys, parts;
+};
+CacheSplit cache_split(int n_seq, int kv_heads, int row_tiles, int max_len) {
+    const int64_t blocks = static_cast<int64_t>(n_seq) * kv_heads * row_tiles;
+    const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(blocks, 1));
+    int64_t keys = (max_len + want - 1) / want;
+    keys = std::max<int64_t>(256, (keys + 255) / 256 * 256);
+    return {static_cast<int>(std::min<int64_t>(keys, int64_t(1) << 30)), static_cast<int>((max_len + keys - 1) / keys)};
+}
+
+int cache_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+
+}  // namespace
+
+hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int n_seq, const int32_t* offsets, int max_len,
+                                   const mopar_rows* q, const mopar_rows* k, const mopar_rows* v, const mopar_rows* out,
+                                   hipStream_t s) {
+    if (tokens == 0 || n_seq == 0 || max_len == 0) return hipSuccess;
+    const int es = static_cast<int>(dtype_size(a.dtype));
+    AttnParams p{};
+    set_rows(p, es, q, out);
+    p.k = static_cast<const unsigned char*>(k->data);
+    p.k_ts = k->token_stride * es;
+    p.k_hs = k->head_stride * es;
+    p.v = static_cast<const unsigned char*>(v->data);
+    p.v_ts = v->token_stride * es;
+    p.v_hs = v->head_stride * es;
+    p.offsets = offsets;
+    p.n_seq = n_seq;
+    p.max_rows = max_len;
+    p.tokens = tokens;
+    p.heads = a.heads;
+    p.kv_heads = a.kv_heads;
+    p.group = a.heads / a.kv_heads;
+    p.c = a.scale * 1.44269504088896341f;
+    // tiles of 128 rows: no more than the tokens fill and one more a sequence
+    const int64_t items = std::min<int64_t>(tokens / 128 + n_seq, static_cast<int64_t>(n_seq) * ((max_len + 127) / 128));
+    if (items * a.heads >= (int64_t(1) << 31)) return hipErrorInvalidValue;
+    const dim3 grid(static_cast<unsigned>(items * a.heads));
+    return by_type(a.dtype, a.head_dim, [&](auto t, auto d) {
+        using T = decltype(t);
+        launch_kernel((attention_kernel<T, d, 4, 1, 1, sizeof(T) == 2 ? 2 : 1, false>), grid, dim3(256), 0, s, p);
+        return hipGetLastError();
+    });
+}
+
+size_t attention_cache_ws_bytes(const mopar_attention& a, const mopar_cache& c, int64_t tokens, int max_q, int max_len) {
+    const int64_t rows = static_cast<int64_t>(max_q) * (a.heads / a.kv_heads);
+    const int bm = cache_rows(rows);
+    const CacheSplit sp = cache_split(c.n_seq, a.kv_heads, static_cast<int>((rows + bm - 1) / bm), max_len);
+    if (sp.parts <= 1) return 0;
+    return static_cast<size_t>(tokens) * a.heads * sp.parts * (a.head_dim + 2) * 4;
+}
+
+hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c, int64_t tokens, const int32_t* offsets,
+                                  int max_q, const int32_t* len, int max_len, const uint64_t* mask, int mask_words,
+                                  const mopar_rows* q, const mopar_rows* out, void* ws, hipStream_t s) {
+    if (tokens == 0 || c.n_seq == 0 || max_q == 0) return hipSuccess;
+    const int es = static_cast<int>(dtype_size(a.dtype));
+    AttnParams p{};
+    set_rows(p, es, q, out);
+    p.k = static_cast<const unsigned char*>(c.k);
+    p.v = static_cast<const unsigned char*>(c.v);
+    p.offsets = offsets;
+    p.n_seq = c.n_seq;
+    p.max_rows = max_q;
+    p.tokens = tokens;
+    p.heads = a.heads;
+    p.kv_heads = a.kv_heads;
+    p.group = a.heads / a.kv_heads;
+    p.c = a.scale * 1.44269504088896341f;
+    p.table = c.table_dev;
+    p.len = len;
+    p.table_stride = c.table_stride;
+    p.pages = c.pages;
+    p.max_pages = c.max_pages;
+    p.shift = __builtin_ctz(static_cast<unsigned>(c.page_tokens));
+    p.max_len = max_len;
+    p.mask = mask;
+    p.mask_words = mask_words;
+    const int64_t rows = static_cast<int64_t>(max_q) * p.group;
+    const int bm = cache_rows(rows);
+    p.row_tiles = static_cast<int>((rows + bm - 1) / bm);
+    const CacheSplit sp = cache_split(c.n_seq, a.kv_heads, p.row_tiles, max_len);
+    p.part_keys = sp.part_keys;
+    p.parts = sp.parts;
+    p.part = static_cast<float*>(ws);
+    if (sp.parts > 1) p.stat = p.part + tokens * a.heads * sp.parts * a.head_dim;
+    const int64_t blocks = static_cast<int64_t>(c.n_seq) * a.kv_heads * p.row_tiles * p.parts;
+    if (blocks >= (int64_t(1) << 31) || c.n_seq > 65535) return hipErrorInvalidValue;
+    const dim3 grid(static_cast<unsigned>(blocks));
+    hipError_t e = by_type(a.dtype, a.head_dim, [&](auto t, auto d) {
+        using T = decltype(t);
+        constexpr int F = sizeof(T) == 2 ? 1 : 0;
+        if (bm == 32)
+            launch_kernel((attention_kernel<T, d, 1, F ? 4 : 2, 1, 1, true>), grid, dim3(F ? 256 : 128), 0, s, p);
+        else if (bm == 64)
+            launch_kernel((attention_kernel<T, d, 2, 2, 1, 1, true>), grid, dim3(256), 0, s, p);
+        else
+            launch_kernel((attention_kernel<T, d, 4, 1, 1, F ? 2 : 1, true>), grid, dim3(256), 0, s, p);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess || sp.parts <= 1) return e;
+    const int64_t join_rows = static_cast<int64_t>(max_q) * a.heads;
+    const dim3 jgrid(static_cast<unsigned>(std::min<int64_t>((join_rows + 7) / 8, 4096)), static_cast<unsigned>(c.n_seq));
+    return by_type(a.dtype, a.head_dim, [&](auto t, auto d) {
+        launch_kernel((attention_join_kernel<decltype(t), d>), jgrid, dim3(256), 0, s, p);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace mopar

@@ -198,6 +198,33 @@ hipError_t launch_codec_narrow(const void* x, const void* w, const void* b, void
                                int cout, int dtype, hipStream_t s);
 hipError_t launch_copy(const void* src, void* dst, size_t bytes, hipStream_t s);
 
+// Rotary positions as the kernels take them: pair j's angle per position as a 64-bit fraction of a turn.
+struct RotaryTable {
+    uint64_t w[128];
+    float m;               // factor on sines and cosines
+    int d, rot;            // head dim, dims that turn (0: none)
+    int interleaved;
+};
+// Rows of `heads` heads turned, row t at position pos[t] (pos null: t mod period).
+hipError_t launch_rotary(const RotaryTable& tab, int dtype, int64_t tokens, int heads, const int32_t* pos, int period,
+                         const mopar_rows* x, const mopar_rows* y, hipStream_t s);
+// Keys (turned, with a table) and values into their pages; with a table also q turned into q_out.
+hipError_t launch_cache_append(const mopar_cache& c, const RotaryTable* tab, int64_t tokens, int heads, const int32_t* pos,
+                               const int32_t* seq, const int32_t* slot, const mopar_rows* q, const mopar_rows* q_out,
+                               const mopar_rows* k, const mopar_rows* v, hipStream_t s);
+hipError_t launch_cache_keep(const mopar_cache& c, int layers, int64_t layer_stride, const int32_t* len, const int32_t* offsets,
+                             int64_t entries, const int32_t* path, int max_path, hipStream_t s);
+// Causal attention over packed prompts; offsets null: n_seq sequences of max_len rows each.
+hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int n_seq, const int32_t* offsets, int max_len,
+                                   const mopar_rows* q, const mopar_rows* k, const mopar_rows* v, const mopar_rows* out,
+                                   hipStream_t s);
+// Attention over the paged cache: the parts that its key axis is split into (a function of what the host
+// knows) and the launches; `ws` holds attention_cache_ws_bytes.
+size_t attention_cache_ws_bytes(const mopar_attention& a, const mopar_cache& c, int64_t tokens, int max_q, int max_len);
+hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c, int64_t tokens, const int32_t* offsets,
+                                  int max_q, const int32_t* len, int max_len, const uint64_t* mask, int mask_words,
+                                  const mopar_rows* q, const mopar_rows* out, void* ws, hipStream_t s);
+
 size_t dtype_size(int dtype);
 
 }  // namespace mopar

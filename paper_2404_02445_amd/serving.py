@@ -1,0 +1,210 @@
+"""Decoding with a paged key/value cache: the C entry points of include/mopar.h on torch tensors.
+
+Row tensors are [tokens, heads, head_dim] views whose last dimension is contiguous (slices of fused
+rows included); pools are [pages, kv_heads, page_tokens, head_dim], or with a leading [layers].  Device
+integers are contiguous int32 tensors.  Every call runs on ``stream``, by default the current stream
+of the tensors' device.  Sizes that the library cannot see (one tensor against another) are checked here
+and raise ``ValueError``; the library's own refusals raise ``MoparError``.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+
+import torch
+
+from . import _lib as L
+from ._lib import check, lib
+
+_DTYPE = {torch.float32: L.MOPAR_F32, torch.bfloat16: L.MOPAR_BF16}
+_LAYOUT = {"half": 0, "interleaved": 1}
+_SCALING = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _on(device, stream):
+    """The stream's handle, and a context in which the device is the current one."""
+    _need(device.type == "cuda", "the tensors must be on a GPU")
+    same = device.index is None or device.index == torch.cuda.current_device()
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    else:
+        _need(stream.device.index == (torch.cuda.current_device() if device.index is None else device.index),
+              "the stream is on another device than the tensors")
+    return contextlib.nullcontext() if same else torch.cuda.device(device), stream.cuda_stream
+
+
+def _dtype(t):
+    _need(t.dtype in _DTYPE, "tensors must be float32 or bfloat16")
+    return _DTYPE[t.dtype]
+
+
+def _rows(t, name, like, shape=None):
+    """A mopar_rows of t; `like` is the tensor whose device and dtype it shares."""
+    _need(t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] == 1), f"{name}: [tokens, heads, head_dim] with contiguous dims")
+    _need(t.device == like.device and t.dtype == like.dtype, f"{name}: device or dtype differs")
+    _need(shape is None or tuple(t.shape) == tuple(shape), f"{name}: shape must be {tuple(shape or ())}")
+    return L.Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _ints(t, name, like, n, dtype=torch.int32):
+    _need(t.dtype == dtype and t.device == like.device and t.is_contiguous(), f"{name}: a contiguous {dtype} tensor on the same device")
+    _need(t.numel() == n, f"{name}: {n} entries expected")
+    return t.data_ptr()
+
+
+class Rotary:
+    """Rotary positions (mopar_rotary_create): the angles of a descriptor, made once."""
+
+    def __init__(self, head_dim, rot_dim=None, layout="half", base=10000.0, scaling="none", factor=1.0, context=0.0,
+                 beta_slow=0.0, beta_fast=0.0, mscale=0.0):
+        _need(layout in _LAYOUT and scaling in _SCALING, f"layout of {list(_LAYOUT)} and scaling of {list(_SCALING)}")
+        d = L.RotaryDesc(_LAYOUT[layout], _SCALING[scaling], head_dim, head_dim if rot_dim is None else rot_dim, base, factor,
+                         context, beta_slow, beta_fast, mscale)
+        h = ctypes.c_void_p()
+        check(lib().mopar_rotary_create(ctypes.byref(d), ctypes.byref(h)))
+        self.handle, self.head_dim = h, head_dim
+
+    def __del__(self):
+        h = getattr(self, "handle", None)
+        if h is not None and h.value and L._lib is not None:
+            L._lib.mopar_rotary_destroy(h)
+            self.handle = None
+
+
+class PagedCache:
+    """A paged cache's pools and page table (mopar_cache).  ``table`` [sequences, max_pages] int32 may be
+    changed in place between calls; its entries outside the pool stand for absent pages."""
+
+    def __init__(self, k, v, table):
+        _need(k.dim() in (4, 5) and k.shape == v.shape and k.dtype == v.dtype and k.device == v.device,
+              "k and v: [pages, kv_heads, page_tokens, head_dim], with a leading [layers] or not, of one shape, dtype and device")
+        layer = k[0] if k.dim() == 5 else k
+        _need((layer.is_contiguous() and (v[0] if v.dim() == 5 else v).is_contiguous()) and k.stride() == v.stride(),
+              "k and v: a layer's pages must be contiguous")
+        _need(table.dim() == 2 and table.dtype == torch.int32 and table.device == k.device and
+              (table.stride(1) == 1 or table.shape[1] == 1), "table: int32 [sequences, max_pages] on the pools' device")
+        self.k, self.v, self.table = k, v, table
+        self.layers = k.shape[0] if k.dim() == 5 else 1
+        self.layer_stride = k.stride(0) if k.dim() == 5 else 0
+        pages, heads, page, d = layer.shape
+        self.raw = L.Cache(_dtype(k), heads, d, page, pages, k.data_ptr(), v.data_ptr(), table.data_ptr(),
+                           max(table.stride(0), table.shape[1]), table.shape[1], table.shape[0])
+
+    def layer(self, i):
+        """The cache of layer i."""
+        _need(self.k.dim() == 5, "the cache has no layers")
+        return PagedCache(self.k[i], self.v[i], self.table)
+
+
+def _single(cache):
+    _need(cache.k.dim() == 4, "one layer's cache is needed: cache.layer(i)")
+    return cache
+
+
+def mopar_rotary_apply(rotary, x, y, pos, stream=None):
+    """y = x with every head turned to its row's position."""
+    rx, ry = _rows(x, "x", x), _rows(y, "y", x, x.shape)
+    _need(x.shape[2] == rotary.head_dim, "x: head_dim is not the rotary's")
+    p = _ints(pos, "pos", x, x.shape[0])
+    ctx, st = _on(x.device, stream)
+    with ctx:
+        check(lib().mopar_rotary_apply(rotary.handle, _dtype(x), x.shape[0], x.shape[1], p, ctypes.byref(rx), ctypes.byref(ry), st))
+    return y
+
+
+def mopar_cache_append(cache, k, v, seq, slot, rotary=None, pos=None, q=None, q_out=None, stream=None):
+    """Key and value rows to slot slot[t] of sequence seq[t]; with a rotary, keys turned, and q to q_out."""
+    c = _single(cache).raw
+    t = k.shape[0]
+    shape = (t, c.kv_heads, c.head_dim)
+    rk, rv = _rows(k, "k", cache.k, shape), _rows(v, "v", cache.k, shape)
+    rq = ro = None
+    heads = 0
+    if rotary is not None:
+        _need(pos is not None, "pos: needed with a rotary")
+        _need((q is None) == (q_out is None), "q and q_out come together")
+        if q is not None:
+            heads = q.shape[1]
+            rq, ro = _rows(q, "q", cache.k, (t, heads, c.head_dim)), _rows(q_out, "q_out", cache.k, (t, heads, c.head_dim))
+    else:
+        _need(pos is None and q is None and q_out is None, "pos, q and q_out go with a rotary")
+    ps = None if pos is None else _ints(pos, "pos", cache.k, t)
+    sq, sl = _ints(seq, "seq", cache.k, t), _ints(slot, "slot", cache.k, t)
+    ctx, st = _on(cache.k.device, stream)
+    with ctx:
+        check(lib().mopar_cache_append(ctypes.byref(c), None if rotary is None else rotary.handle, t, heads, ps, sq, sl,
+                                       None if rq is None else ctypes.byref(rq), None if ro is None else ctypes.byref(ro),
+                                       ctypes.byref(rk), ctypes.byref(rv), st))
+
+
+def mopar_cache_keep(cache, lens, path_offsets, path, max_path, stream=None):
+    """The accepted drafted tokens of every sequence moved to where it goes on, in every layer."""
+    c = cache.raw
+    ln, po = _ints(lens, "lens", cache.k, c.n_seq), _ints(path_offsets, "path_offsets", cache.k, c.n_seq + 1)
+    pa = _ints(path, "path", cache.k, path.numel())
+    ctx, st = _on(cache.k.device, stream)
+    with ctx:
+        check(lib().mopar_cache_keep(ctypes.byref(c), cache.layers, cache.layer_stride, ln, po, path.numel(), pa, max_path, st))
+
+
+def _attention(q, kv_heads, scale):
+    d = q.shape[2]
+    return L.Attention(_dtype(q), q.shape[1], kv_heads, d, d ** -0.5 if scale is None else scale, 0)
+
+
+def mopar_attention_prompt(q, k, v, out, offsets, max_len, scale=None, stream=None):
+    """Causal attention over packed prompts; sequence s is rows offsets[s] .. offsets[s + 1] - 1."""
+    _need(q.dim() == 3 and k.dim() == 3, "q, k: [tokens, heads, head_dim]")
+    t, d = q.shape[0], q.shape[2]
+    rq, ro = _rows(q, "q", q), _rows(out, "out", q, q.shape)
+    rk, rv = _rows(k, "k", q, (t, k.shape[1], d)), _rows(v, "v", q, (t, k.shape[1], d))
+    off = _ints(offsets, "offsets", q, offsets.numel())
+    _need(offsets.numel() >= 1, "offsets: one more than sequences")
+    a = _attention(q, k.shape[1], scale)
+    ctx, st = _on(q.device, stream)
+    with ctx:
+        check(lib().mopar_attention_prompt(ctypes.byref(a), t, offsets.numel() - 1, off, max_len, ctypes.byref(rq), ctypes.byref(rk),
+                                           ctypes.byref(rv), ctypes.byref(ro), st))
+    return out
+
+
+def mopar_attention_cache_workspace_bytes(q, cache, max_q, max_len):
+    c = _single(cache).raw
+    n = ctypes.c_size_t()
+    a = _attention(q, c.kv_heads, None)
+    check(lib().mopar_attention_cache_workspace_bytes(ctypes.byref(a), ctypes.byref(c), q.shape[0], max_q, max_len, ctypes.byref(n)))
+    return n.value
+
+
+def alloc_attention_workspace(q, cache, max_q, max_len):
+    """A workspace for mopar_attention_cache calls with as many rows, max_q and max_len as these."""
+    n = mopar_attention_cache_workspace_bytes(q, cache, max_q, max_len)
+    return torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
+
+
+def mopar_attention_cache(q, out, cache, offsets, max_q, lens, max_len, mask=None, scale=None, ws=None, stream=None):
+    """Attention of drafted tokens over the cache: of a tree (``mask`` int64 [tokens, words], bit j of a row:
+    it sees drafted token j) or, without a mask, of one new token or a chain of them."""
+    c = _single(cache).raw
+    _need(q.dim() == 3, "q: [tokens, heads, head_dim]")
+    rq, ro = _rows(q, "q", cache.k), _rows(out, "out", cache.k, q.shape)
+    off, ln = _ints(offsets, "offsets", cache.k, c.n_seq + 1), _ints(lens, "lens", cache.k, c.n_seq)
+    words, mk = 0, None
+    if mask is not None:
+        _need(mask.dim() == 2, "mask: int64 [tokens, words]")
+        words = mask.shape[1]
+        mk = _ints(mask, "mask", cache.k, q.shape[0] * words, torch.int64)
+    a = _attention(q, c.kv_heads, scale)
+    if ws is not None:
+        _need(ws.device == q.device and ws.is_contiguous(), "ws: a contiguous tensor on the same device")
+    ctx, st = _on(q.device, stream)
+    with ctx:
+        check(lib().mopar_attention_cache(ctypes.byref(a), ctypes.byref(c), q.shape[0], off, max_q, ln, max_len, mk, words, ctypes.byref(rq),
+                                          ctypes.byref(ro), None if ws is None else ws.data_ptr(),
+                                          0 if ws is None else ws.numel() * ws.element_size(), st))
+    return out
