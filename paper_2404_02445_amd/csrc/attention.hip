@@ -8,7 +8,7 @@
 // -- the k index of an MFMA may run over the keys in any order that both operands share, so P never leaves the
 // registers.  V^T fragments come from row-major V in LDS by transposing reads (bf16) or element reads (float32).
 //
-// Keys and values stream to LDS with 16-byte direct loads, two stages; a row of LDS is the head's dims, a power
+// Keys and values stream to LDS with 16-byte direct loads, two stages (K, K, V, V); a row of LDS is the head's dims, a power
 // of two of 16-byte chunks, chunk c of row r at place c ^ f(r) (swizzle()), which keeps both the fragment reads
 // of K (32 rows, one chunk) and those of V (four rows, 64 bytes) off each other's banks.
 #include <algorithm>
@@ -31,6 +31,16 @@ typedef const __attribute__((address_space(1))) void* gptr_t;
 
 // what absent keys and values are read from
 __device__ __attribute__((aligned(16))) const unsigned int kZeros[4] = {0u, 0u, 0u, 0u};
+
+constexpr int kRsrcWord3 = 0x00020000;       // raw buffer, 32-bit data format
+constexpr unsigned kOOB = 0x80000000u;       // a lane offset past every resource: reads zeros
+
+// One 16-byte chunk per lane from base + voff into place `lane` of the 1 KB block at dst; zeros where voff is kOOB.
+__device__ __forceinline__ void load_lds(const unsigned char* base, lds_ptr_t dst, unsigned voff) {
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), static_cast<short>(0),
+                                                                      0x7fffffff, kRsrcWord3);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, voff, 0, 0, 0);
+}
 
 constexpr float kNoMax = -3.40282347e38f;    // running maximum of a row that has seen no key
 
@@ -62,6 +72,8 @@ template <typename T, int D> struct Geo {
     static constexpr int CH = D / EPC;           // chunks of a row
     static constexpr int RS = pow2_up(CH);       // chunk places of a row in LDS
     static constexpr int RB = RS * 16;           // bytes of a row in LDS
+    static constexpr int KG = CH / 2 % 4 == 0 ? 4 : CH / 2 % 3 == 0 ? 3 : 2;   // K fragments read together
+    static_assert(CH / 2 % KG == 0, "whole groups");
 };
 
 // Chunk c of row r sits at place c ^ swizzle(r): linear in the bits of r.
@@ -89,7 +101,11 @@ template <int OFF> __device__ __forceinline__ unsigned lds_read4(unsigned addr) 
     asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
     return v;
 }
-__device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// until at most N of this wave's LDS reads are still in flight (they complete in order)
+template <int N = 0> __device__ __forceinline__ void lds_wait() {
+    static_assert(N >= 0 && N <= 15, "lgkmcnt range");
+    asm volatile("s_waitcnt lgkmcnt(%0)" ::"n"(N) : "memory");
+}
 template <typename V> __device__ __forceinline__ void pin(V& v) { asm volatile("" : "+v"(v)); }
 
 template <int N, typename F, int I = 0> __device__ __forceinline__ void static_for(F&& f) {
@@ -114,9 +130,44 @@ __device__ __forceinline__ void rows_of(const AttnParams& p, int s, int64_t& sta
     rows = static_cast<int>(min(max(hi - lo, int64_t(0)), static_cast<int64_t>(p.max_rows)));
 }
 
+__device__ __forceinline__ int wave_sum(int v) {
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) v += __shfl_xor(v, i, 64);
+    return v;
+}
+
+// The item-th tile of BM rows: within each 64 sequences, the tiles furthest along their sequence -- the causal
+// ones with most keys -- first, so that the long ones start early and the short ones fill the end.
+template <int BM> __device__ __forceinline__ bool pick_tile(const AttnParams& p, int item, int lane, int& s, int& tile) {
+    for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
+        int64_t start;
+        int rows = 0;
+        if (s0 + lane < p.n_seq) rows_of(p, s0 + lane, start, rows);
+        const int nt = (rows + BM - 1) / BM, all = wave_sum(nt);
+        if (item >= all) {
+            item -= all;
+            continue;
+        }
+        // the level of the item: at least `above` tiles lie higher, sum of (nt - level) over the taller sequences
+        int lo = 0, hi = (p.max_rows + BM - 1) / BM, above = 0;      // tiles at or past lo: > item; at or past hi: <= item
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2, n = wave_sum(max(nt - mid, 0));
+            if (n > item) lo = mid; else hi = mid, above = n;
+        }
+        const uint64_t have = __ballot(nt > lo);
+        const int rank = item - above;
+        const uint64_t below = have & ((uint64_t(1) << lane) - 1);
+        const uint64_t hit = __ballot(((have >> lane) & 1) && __popcll(below) == rank);
+        s = __builtin_amdgcn_readfirstlane(s0 + static_cast<int>(__builtin_ctzll(hit)));
+        tile = __builtin_amdgcn_readfirstlane(lo);
+        return true;
+    }
+    return false;
+}
+
 // WR waves take 32 RT rows each, WK waves share a row tile and take every WK-th 32-key tile.
 template <typename T, int D, int WR, int WK, int RT, int SUBS, bool PAGED>
-__global__ __launch_bounds__(WR * WK * 64) void attention_kernel(const AttnParams p) {
+__global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnParams p) {
     using G = Geo<T, D>;
     constexpr int ES = G::ES, CH = G::CH, RS = G::RS, RB = G::RB, DT = D / 32;
     constexpr int NW = WR * WK;
@@ -146,17 +197,12 @@ __global__ __launch_bounds__(WR * WK * 64) void attention_kernel(const AttnParam
         s = b / p.kv_heads;
         rows_of(p, s, start, rows);
     } else {
-        head = blockIdx.x % p.heads;
-        kvh = head / p.group;
-        int item = blockIdx.x / p.heads;
-        for (s = 0;; ++s) {
-            if (s >= p.n_seq) return;
-            rows_of(p, s, start, rows);
-            const int nt = (rows + BM - 1) / BM;
-            if (item < nt) break;
-            item -= nt;
-        }
-        tile = item;
+        // key heads fastest: the XCDs take blocks round-robin, so the query heads of a key head meet in one L2
+        const int hi = blockIdx.x % p.heads, gi = hi / p.kv_heads;
+        kvh = hi - gi * p.kv_heads;
+        head = kvh * p.group + gi;
+        if (!pick_tile<BM>(p, blockIdx.x / p.heads, lane, s, tile)) return;
+        rows_of(p, s, start, rows);
     }
     const int group = PAGED ? p.group : 1;
     const int nrow = rows * group;                    // query rows: tokens, times the heads of a group over a cache
@@ -185,34 +231,56 @@ __global__ __launch_bounds__(WR * WK * 64) void attention_kernel(const AttnParam
     }
 
     // --- loads -----------------------------------------------------------------------------------
-    // Block b of a stage is rows b * 64 / RS ..; lane l fills place l % RS of row (b * 64 + l) / RS.
+    // Block b of a stage is rows b * 64 / RS ..; lane l fills place l % RS of row (b * 64 + l) / RS.  Wave w
+    // loads blocks w LPW .. of K and of V.  A block's rows lie in one page unless pages are smaller than it.
+    constexpr int RPB = 64 / RS;                      // rows of a load block
     const unsigned char* const kbase = p.k + (PAGED ? 0 : start * p.k_ts + kvh * p.k_hs);
     const unsigned char* const vbase = p.v + (PAGED ? 0 : start * p.v_ts + kvh * p.v_hs);
-    const unsigned char* const zeros = reinterpret_cast<const unsigned char*>(kZeros);
-    auto issue = [&](int k0, int buf) __attribute__((always_inline)) {
+    const int lrow = lane / RS;                       // this lane's row in a block
+    auto chunk = [&](int b) __attribute__((always_inline)) { return (lane % RS) ^ swizzle<RS>(b * RPB + lrow); };
+    const int32_t* const pages = PAGED ? p.table + s * p.table_stride : nullptr;
+    // The pages of a stage's blocks, one a lane (-1: absent), are read a stage before its loads go out.
+    const bool small = PAGED && (1 << p.shift) < RPB;
+    auto pages_of = [&](int k0) __attribute__((always_inline)) -> int {
+        if constexpr (!PAGED) return 0;
+        const int key = k0 + lane * RPB;
+        int page = 0;
+        if (lane < NBLK && key < key1 && !small) page = pages[key >> p.shift];
+        return static_cast<unsigned>(page) < static_cast<unsigned>(p.pages) ? page : -1;
+    };
+    auto issue = [&](int k0, int buf, int pgs) __attribute__((always_inline)) {
+        const lds_ptr_t dst = (lds_ptr_t)(lds + buf * TILE);
 #pragma unroll
         for (int j = 0; j < LPW; ++j) {
-            const int b = wave + NW * j;
+            const int b = wave * LPW + j;
             if (NBLK % NW != 0 && b >= NBLK) continue;
-            const int row = (b * 64 + lane) / RS, ch = (lane % RS) ^ swizzle<RS>(row);
-            const int key = k0 + row;
-            const unsigned char *ks = zeros, *vs = zeros;
-            if (key < key1 && ch < CH) {
-                if constexpr (PAGED) {
-                    const int page = p.table[s * p.table_stride + (key >> p.shift)];
+            const int ch = chunk(b), key = k0 + b * RPB;             // first key of the block
+            unsigned char __attribute__((address_space(3)))* const kd = (unsigned char __attribute__((address_space(3)))*)dst + b * 1024;
+            bool in = (key + lrow < key1) & (ch < CH);
+            if constexpr (PAGED) {
+                if (!small) {
+                    const int page = __builtin_amdgcn_readlane(pgs, b);
+                    const int64_t at = (((static_cast<int64_t>(max(page, 0)) * p.kv_heads + kvh) << p.shift) + (key & ((1 << p.shift) - 1))) * (D * ES);
+                    const unsigned vo = in & (page >= 0) ? static_cast<unsigned>(lrow * (D * ES) + ch * 16) : kOOB;
+                    load_lds(kbase + at, (lds_ptr_t)kd, vo);
+                    load_lds(vbase + at, (lds_ptr_t)(kd + 2 * TILE), vo);
+                } else {
+                    const int page = in ? pages[(key + lrow) >> p.shift] : -1;
+                    const unsigned char *ks = reinterpret_cast<const unsigned char*>(kZeros), *vs = ks;
                     if (page >= 0 && page < p.pages) {
-                        const int64_t off = (((page * static_cast<int64_t>(p.kv_heads) + kvh) << p.shift) + (key & ((1 << p.shift) - 1))) *
+                        const int64_t off = (((static_cast<int64_t>(page) * p.kv_heads + kvh) << p.shift) + ((key + lrow) & ((1 << p.shift) - 1))) *
                                                 (D * ES) + ch * 16;
                         ks = kbase + off;
                         vs = vbase + off;
                     }
-                } else {
-                    ks = kbase + key * p.k_ts + ch * 16;
-                    vs = vbase + key * p.v_ts + ch * 16;
+                    __builtin_amdgcn_global_load_lds((gptr_t)ks, (lds_ptr_t)kd, 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)vs, (lds_ptr_t)(kd + 2 * TILE), 16, 0, 0);
                 }
+            } else {
+                const int row = b * RPB + lrow;
+                load_lds(kbase + k0 * p.k_ts, (lds_ptr_t)kd, in ? static_cast<unsigned>(row * static_cast<int>(p.k_ts)) + ch * 16 : kOOB);
+                load_lds(vbase + k0 * p.v_ts, (lds_ptr_t)(kd + 2 * TILE), in ? static_cast<unsigned>(row * static_cast<int>(p.v_ts)) + ch * 16 : kOOB);
             }
-            __builtin_amdgcn_global_load_lds((gptr_t)ks, (lds_ptr_t)(lds + buf * 2 * TILE + b * 1024), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((gptr_t)vs, (lds_ptr_t)(lds + buf * 2 * TILE + TILE + b * 1024), 16, 0, 0);
         }
     };
 
@@ -235,10 +303,10 @@ __global__ __launch_bounds__(WR * WK * 64) void attention_kernel(const AttnParam
     unsigned va;
     if constexpr (ES == 2) {
         const int row = 4 * lh + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-        va = lds0 + static_cast<unsigned>(TILE + row * RB + ((ch ^ swizzle<RS>(row)) << 4) + (lane & 1) * 8);
+        va = lds0 + static_cast<unsigned>(2 * TILE + row * RB + ((ch ^ swizzle<RS>(row)) << 4) + (lane & 1) * 8);
     } else {
         const int row = 4 * lh, ch = lr >> 2;
-        va = lds0 + static_cast<unsigned>(TILE + row * RB + ((ch ^ swizzle<RS>(row)) << 4) + (lr & 3) * 4);
+        va = lds0 + static_cast<unsigned>(2 * TILE + row * RB + ((ch ^ swizzle<RS>(row)) << 4) + (lr & 3) * 4);
     }
 
     // visible keys of a row among 64 from k0 on, one bit each
@@ -259,41 +327,68 @@ __global__ __launch_bounds__(WR * WK * 64) void attention_kernel(const AttnParam
         return bits & ones(key1 - k0);
     };
 
-    // one 32-key tile: scores, weights and products
-    auto tile32 = [&](int buf, auto sub, int k0) __attribute__((always_inline)) {
-        const int st0 = buf * 2 * TILE + (WK > 1 ? wk * 32 * RB : 0);
+    uint64_t ok = 0;                                  // blocks of the stage at hand whose page is there
+    // one 32-key tile: scores, weights and products; `cut`: some row may not see some key
+    auto tile32 = [&](int buf, auto sub, int k0, auto cut) __attribute__((always_inline)) {
+        const int st0 = buf * TILE + (WK > 1 ? wk * 32 * RB : 0);
         f32x16 sc[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[r][i] = 0.0f;
-        {
-            u32x4 kf[CH / 2];
-            static_for<CH / 2>([&](auto st) __attribute__((always_inline)) { kf[st] = lds_read16<sub * 32 * RB>((ka + st0) ^ (st << 5)); });
-            lds_wait();
-            static_for<CH / 2>([&](auto st) __attribute__((always_inline)) {
-                pin(kf[st]);
+        constexpr int KG = G::KG, NKG = CH / 2 / KG;      // K fragments of a group, groups
+        u32x4 kf[2][KG];
+        auto read_k = [&](auto g) __attribute__((always_inline)) {
+            static_for<KG>([&](auto e) __attribute__((always_inline)) {
+                constexpr int slot = g % 2, st = g * KG + e, el = e;
+                kf[slot][el] = lds_read16<sub * 32 * RB>((ka + st0) ^ (st << 5));
+            });
+        };
+        read_k(std::integral_constant<int, 0>{});
+        static_for<NKG>([&](auto g) __attribute__((always_inline)) {
+            constexpr int slot = g % 2;
+            if constexpr (g + 1 < NKG) {
+                read_k(std::integral_constant<int, g + 1>{});
+                lds_wait<KG>();
+            } else {
+                lds_wait();
+            }
+            static_for<KG>([&](auto e) __attribute__((always_inline)) {
+                constexpr int st = g * KG + e, el = e;
+                pin(kf[slot][el]);
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
                     if constexpr (ES == 2)
-                        sc[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[st]), __builtin_bit_cast(bf16x8, qf[r][st]),
-                                                                        sc[r], 0, 0, 0);
+                        sc[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[slot][el]),
+                                                                        __builtin_bit_cast(bf16x8, qf[r][st]), sc[r], 0, 0, 0);
                     else
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            sc[r] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[st][e]), __uint_as_float(qf[r][st][e]), sc[r], 0, 0, 0);
+                        for (int c = 0; c < 4; ++c)
+                            sc[r] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[slot][el][c]), __uint_as_float(qf[r][st][c]), sc[r],
+                                                                         0, 0, 0);
                 }
             });
-        }
-        // keys that some row of this wave does not see
-        const bool cut = k0 + 32 > key1 || k0 + 32 > past + (PAGED ? (p.mask ? 0 : qtok[0]) : 0);
-        bool masked = false;
+        });
         uint64_t vis[RT];
-        if (__any(cut)) {
-            masked = true;
+        if constexpr (cut) {
+            // keys of absent pages
+            uint64_t held = ~uint64_t(0);
+            if constexpr (PAGED) {
+                if (small) {
+                    const int key = k0 + lane, page = lane < 32 && key < key1 ? pages[key >> p.shift] : -1;
+                    held = __ballot(static_cast<unsigned>(page) < static_cast<unsigned>(p.pages));
+                } else {
+                    constexpr int NB = 32 / RPB;
+                    const int b0 = (WK > 1 ? wk * 32 : sub * 32) / RPB;
+                    held = 0;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+                        if ((ok >> (b0 + b)) & 1) held |= ((uint64_t(1) << RPB) - 1) << (b * RPB);
+                }
+            }
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                vis[r] = visible(r, k0);
+                vis[r] = visible(r, k0) & held;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (!((vis[r] >> (8 * (i / 4) + 4 * lh + i % 4)) & 1)) sc[r][i] = -INFINITY;
@@ -348,7 +443,7 @@ __global__ __launch_bounds__(WR * WK * 64) void attention_kernel(const AttnParam
             for (int d = 0; d < DT; ++d) pin(vf[d]);
             // Where a row does not see every key, an infinity or NaN among the values must not meet its zero weight
             bool special = false;
-            if (masked) {
+            if constexpr (cut) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -369,7 +464,7 @@ __global__ __launch_bounds__(WR * WK * 64) void attention_kernel(const AttnParam
                             for (int e = 0; e < 4; ++e)
                                 o[r][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(vf[d][e]), sc[r][4 * u + e], o[r][d], 0, 0, 0);
                     }
-            } else {
+            } else if constexpr (cut) {
                 // one key at a time, added only where it is seen
                 for (int key = 0; key < 2 * PER; ++key) {
                     const int kh = (key >> 2) & 1, kr = (key & 3) + 4 * (key >> 3);       // half and register of the key
@@ -395,6 +490,7 @@ __global__ __launch_bounds__(WR * WK * 64) void attention_kernel(const AttnParam
                             }
 #pragma unroll
                             for (int i = 0; i < 16; ++i) o[r][d][i] += seen ? one[i] : 0.0f;
+                            __builtin_amdgcn_sched_barrier(0);       // (one product's registers at a time)
                         }
                     }
                 }
@@ -402,20 +498,171 @@ __global__ __launch_bounds__(WR * WK * 64) void attention_kernel(const AttnParam
         });
     };
 
+    // a stage that every row sees whole: the 32-key tiles of this wave together
+    unsigned kr[ES == 2 ? CH / 2 : 1], vr[ES == 2 ? 2 * DT : 1];
+    if constexpr (ES == 2) {
+        static_for<CH / 2>([&](auto st) __attribute__((always_inline)) { kr[st] = ((ka + (WK > 1 ? wk * 32 * RB : 0)) ^ (st << 5)); });
+        static_for<DT>([&](auto d) __attribute__((always_inline)) {
+            vr[2 * d] = (va + (WK > 1 ? wk * 32 * RB : 0)) ^ (d << 6);
+            vr[2 * d + 1] = vr[2 * d] ^ (swizzle<RS>(8) << 4);
+        });
+    }
+    auto full = [&](auto buf) __attribute__((always_inline)) {
+        constexpr int B0 = buf * TILE;
+        constexpr int KG = G::KG, NKG = SUBS * (CH / 2) / KG;     // K fragments of a group, groups
+        f32x16 sc[SUBS][RT];
+#pragma unroll
+        for (int t = 0; t < SUBS; ++t)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[t][r][i] = 0.0f;
+        u32x4 kf[2][KG];
+        auto read_k = [&](auto g) __attribute__((always_inline)) {
+            static_for<KG>([&](auto e) __attribute__((always_inline)) {
+                constexpr int st = (g * KG + e) % (CH / 2), sub = (g * KG + e) / (CH / 2), slot = g % 2;
+                kf[slot][e] = lds_read16<B0 + sub * 32 * RB>(kr[st]);
+            });
+        };
+        read_k(std::integral_constant<int, 0>{});
+        static_for<NKG>([&](auto g) __attribute__((always_inline)) {
+            constexpr int slot = g % 2;
+            if constexpr (g + 1 < NKG) {
+                read_k(std::integral_constant<int, g + 1>{});
+                lds_wait<KG>();
+            } else {
+                lds_wait();
+            }
+            static_for<KG>([&](auto e) __attribute__((always_inline)) {
+                constexpr int st = (g * KG + e) % (CH / 2), sub = (g * KG + e) / (CH / 2);
+                pin(kf[slot][e]);
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+                    sc[sub][r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[slot][e]),
+                                                                         __builtin_bit_cast(bf16x8, qf[r][st]), sc[sub][r], 0, 0, 0);
+            });
+        });
+        // the first values on their way under the softmax
+        constexpr int NVG = 2 * SUBS;
+        u32x2 vf[2][2 * DT];
+        auto read_v = [&](auto g) __attribute__((always_inline)) {
+            static_for<DT>([&](auto d) __attribute__((always_inline)) {
+                constexpr int slot = g % 2, off = B0 + (g / 2 * 32 + g % 2 * 16) * RB;
+                vf[slot][2 * d] = lds_read_tr<off>(vr[2 * d]);
+                vf[slot][2 * d + 1] = lds_read_tr<off + 8 * RB>(vr[2 * d + 1]);
+            });
+        };
+        read_v(std::integral_constant<int, 0>{});
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float mx = sc[0][r][0];
+#pragma unroll
+            for (int t = 0; t < SUBS; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, sc[t][r][i]), sc[t][r][i + 1]);
+            mx = fmaxf(mx, other_half(mx)) * p.c;
+            // The maximum in use may lag by up to 8 (weights stay below 2^8): rescaling is rare.
+            if (__any(mx > m[r] + 8.0f)) {
+                const float mn = fmaxf(m[r], mx), f = __builtin_amdgcn_exp2f(m[r] - mn);
+                m[r] = mn;
+                l[r] *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[r][d][i] *= f;
+            }
+            float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int t = 0; t < SUBS; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    sc[t][r][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][r][i], p.c, -m[r]));
+                    sum[i & 1] += sc[t][r][i];
+                }
+            l[r] += sum[0] + sum[1];
+        }
+        static_for<NVG>([&](auto g) __attribute__((always_inline)) {
+            constexpr int slot = g % 2;
+            if constexpr (g + 1 < NVG) {
+                read_v(std::integral_constant<int, g + 1>{});
+                lds_wait<2 * DT>();
+            } else {
+                lds_wait();
+            }
+            bf16x8 pf[RT];
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) pf[r][i] = static_cast<__bf16>(sc[g / 2][r][8 * (g % 2) + i]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                pin(vf[slot][2 * d]);
+                pin(vf[slot][2 * d + 1]);
+                const u32x4 w = {vf[slot][2 * d][0], vf[slot][2 * d][1], vf[slot][2 * d + 1][0], vf[slot][2 * d + 1][1]};
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+                    o[r][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf[r], o[r][d], 0, 0, 0);
+            }
+        });
+    };
+
     // --- the keys ----------------------------------------------------------------------------------
     // rows of this wave, all of them past the last visible key of the tile: nothing to do (causal)
     const int wave_end = PAGED ? key1 : min(key1, row0 + (wr + 1) * RT * 32);
-    if (key0 < key1) issue(key0, 0);
-    int buf = 0;
-    for (int k0 = key0; k0 < key1; k0 += KT, buf ^= 1) {
+    // Stages that every row of the block sees whole come first; from an absent page on, every stage is looked at
+    // key by key.
+    constexpr uint64_t ALL = NBLK >= 64 ? ~uint64_t(0) : (uint64_t(1) << NBLK) - 1;
+    const int seen = PAGED ? min(past, key1) : row0 + 1;
+    const int full_end = seen > key0 && !small ? key0 + (seen - key0) / KT * KT : key0;
+    int pgs = 0;
+    auto stage = [&](int k0, int buf) __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (k0 + KT < key1) issue(k0 + KT, buf ^ 1);
+        const int next = pgs;
+        if (k0 + KT < key1) issue(k0 + KT, buf ^ 1, next);
+        if constexpr (PAGED) pgs = pages_of(k0 + 2 * KT);
+        return next;
+    };
+    int k0 = key0, buf = 0;
+    if (key0 < key1) {
+        pgs = pages_of(key0);
+        issue(key0, 0, pgs);
+        ok = PAGED ? __ballot(pgs >= 0) & ALL : ALL;
+        pgs = pages_of(key0 + KT);
+    }
+    // compute of a stage is done: what the next one holds
+    auto advance = [&](int next) __attribute__((always_inline)) {
+        if constexpr (PAGED) ok = __ballot(next >= 0) & ALL;
+        k0 += KT;
+        buf ^= 1;
+    };
+    if constexpr (ES == 2) {
+        while (k0 < full_end && ok == ALL) {
+            int next = stage(k0, 0);
+            full(std::integral_constant<int, 0>{});
+            advance(next);
+            if (k0 >= full_end || ok != ALL) break;
+            next = stage(k0, 1);
+            full(std::integral_constant<int, 1>{});
+            advance(next);
+        }
+    } else {
+        while (k0 < full_end && ok == ALL) {
+            const int next = stage(k0, buf);
+            static_for<SUBS>([&](auto sub) __attribute__((always_inline)) {
+                tile32(buf, sub, k0 + (WK > 1 ? wk * 32 : 0) + sub * 32, std::false_type{});
+            });
+            advance(next);
+        }
+    }
+    while (k0 < key1) {
+        const int next = stage(k0, buf);
         static_for<SUBS>([&](auto sub) __attribute__((always_inline)) {
             const int k = k0 + (WK > 1 ? wk * 32 : 0) + sub * 32;
-            if (k < wave_end) tile32(buf, sub, k);
+            if (k < wave_end) tile32(buf, sub, k, std::true_type{});
         });
+        advance(next);
     }
 
     // --- results -----------------------------------------------------------------------------------

@@ -361,6 +361,25 @@ def test_absent_pages_are_not_visible():
     over_cache(gen(5), "f32", 2, 2, 64, 16, [10, 300], [1, 1], None, absent=(0, 0, -1))      # nothing left to see
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [1, 16, 64])
+@pytest.mark.parametrize("new", [1, 20, 40])
+def test_absent_pages_take_no_weight(dt, page, new):
+    """All scores zero: every visible token weighs the same, and absent ones nothing."""
+    n = 200
+    kc = torch.zeros(n // page + 1, 2, page, 64, device="cuda", dtype=DT[dt])
+    vc = torch.ones_like(kc)
+    table = torch.arange(-(-n // page), dtype=torch.int32).reshape(1, -1)
+    table[0, 1::3] = -1
+    table[0, 0] = 10 ** 6
+    q = torch.ones(new, 4, 64, device="cuda", dtype=DT[dt])
+    out = torch.empty_like(q)
+    cache = P.PagedCache(kc, vc, table.cuda())
+    P.mopar_attention_cache(q, out, cache, ints([0, new]), new, ints([n - new]), n, ws=P.alloc_attention_workspace(q, cache, new, n))
+    # whole-number sums are exact; the reciprocal and the product round once each, by at most 2^-24
+    assert bool(((out.double() - 1).abs() <= 2.0 ** -23).all())
+
+
 def test_max_len_cuts_a_sequence():
     over_cache(gen(6), "bf16", 4, 2, 64, 16, [300, 40], [1, 1], None, max_len=200, poison=False)
 
