@@ -293,7 +293,8 @@ int mopar_attention_prompt(const mopar_attention* a, int64_t tokens, int32_t n_s
  * survive between calls, and calls that overlap need one each.
  * Errors: MOPAR_E_ARG (also a mask of fewer than ceil(max_q / 64) words),
  * MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (head_dim; heads / kv_heads * max_q of 2^20
- * and more), MOPAR_E_WORKSPACE, MOPAR_E_HIP. */
+ * and more; n_seq * kv_heads * max_len so large that their tiles reach 2^30),
+ * MOPAR_E_WORKSPACE, MOPAR_E_HIP. */
 int mopar_attention_cache_workspace_bytes(const mopar_attention* a, const mopar_cache* cache, int64_t tokens,
                                           int32_t max_q, int32_t max_len, size_t* bytes);
 int mopar_attention_cache(const mopar_attention* a, const mopar_cache* cache, int64_t tokens, const int32_t* offsets_dev,

@@ -59,10 +59,11 @@ struct AttnParams {
     int max_pages, shift, max_len;
     const uint64_t* mask;
     int mask_words;
-    // the parts of the key axis
-    int part_keys, parts;
+    // over a cache: whether blocks take equal shares of all key stages (else one unit each), the least share,
+    // partial sums [2 blocks][rows of a tile][head_dim] and their statistics, row tiles of a (sequence, key head)
+    int split, least;
     float *part, *stat;
-    int row_tiles;                   // blocks of rows per (sequence, head)
+    int row_tiles;
 };
 
 constexpr int pow2_up(int v) { int p = 1; while (p < v) p *= 2; return p; }
@@ -115,6 +116,13 @@ template <int N, typename F, int I = 0> __device__ __forceinline__ void static_f
     }
 }
 
+// the bits of the elements of a word that are infinite or NaN
+template <int ES> __device__ __forceinline__ unsigned not_finite(unsigned w) {
+    if constexpr (ES == 4) return (w & 0x7f800000u) == 0x7f800000u ? ~0u : 0u;
+    const unsigned t = ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    return (t >> 15) * 0xffffu;
+}
+
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
 
 // a sequence's rows [start, start + rows) of the packed tensors
@@ -134,6 +142,55 @@ __device__ __forceinline__ int wave_sum(int v) {
 #pragma unroll
     for (int i = 1; i < 64; i *= 2) v += __shfl_xor(v, i, 64);
     return v;
+}
+
+// A sequence over the cache: its drafted rows, tokens before them and in all, and its work -- a unit is a tile of BM
+// query rows of one key head, of nt key stages (one, empty, where there is nothing to see).
+struct SeqShape {
+    int64_t start;
+    int rows, past, total, nt, units;
+};
+template <int KT, int BM> __device__ __forceinline__ SeqShape seq_shape(const AttnParams& p, int s) {
+    SeqShape q;
+    rows_of(p, s, q.start, q.rows);
+    q.past = min(max(p.len[s], 0), p.max_len);
+    q.total = min(q.past + min(q.rows, p.max_len - q.past), p.max_pages << p.shift);
+    q.nt = max(1, (q.total + KT - 1) / KT);
+    q.units = (q.rows * p.group + BM - 1) / BM * p.kv_heads;
+    return q;
+}
+// Stages of all sequences, which come one sequence after the other, in it one unit after the other.
+template <int KT, int BM> __device__ __forceinline__ int all_stages(const AttnParams& p, int lane) {
+    int n = 0;
+    for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
+        const SeqShape q = seq_shape<KT, BM>(p, min(s0 + lane, p.n_seq - 1));
+        n += wave_sum(s0 + lane < p.n_seq ? q.nt * q.units : 0);
+    }
+    return n;
+}
+// the sequence that stage g < all_stages is in, and its first stage
+template <int KT, int BM> __device__ __forceinline__ void find_stage(const AttnParams& p, int lane, int g, int& s, int& base) {
+    base = 0;
+    for (int s0 = 0;; s0 += 64) {
+        const SeqShape q = seq_shape<KT, BM>(p, min(s0 + lane, p.n_seq - 1));
+        const int n = s0 + lane < p.n_seq ? q.nt * q.units : 0;
+        int upto = n;
+#pragma unroll
+        for (int i = 1; i < 64; i *= 2) {
+            const int v = __shfl_up(upto, i, 64);
+            if (lane >= i) upto += v;
+        }
+        const uint64_t past_g = __ballot(base + upto > g);
+        if (past_g) {
+            const int at = static_cast<int>(__builtin_ctzll(past_g));
+            s = s0 + at;
+            base += __shfl(upto - n, at, 64);
+            s = __builtin_amdgcn_readfirstlane(s);
+            base = __builtin_amdgcn_readfirstlane(base);
+            return;
+        }
+        base += __shfl(upto, 63, 64);
+    }
 }
 
 // The item-th tile of BM rows: within each 64 sequences, the tiles furthest along their sequence -- the causal
@@ -177,7 +234,8 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
     constexpr int NBLK = TILE / 1024, LPW = (NBLK + NW - 1) / NW;
     constexpr int MERGE = WK > 1 ? WK * BM * (D + 4) * 4 + WK * BM * 8 : 0;
     constexpr int LDS = 4 * TILE > MERGE ? 4 * TILE : MERGE;
-    static_assert(TILE % 1024 == 0, "whole load blocks");
+    constexpr bool OWN = WR == 1 && WK > 1;          // a wave loads the very keys it works on: no barrier a stage
+    static_assert(TILE % 1024 == 0 && (!OWN || LPW * (64 / RS) == 32), "whole load blocks");
     __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -185,17 +243,45 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
     const int lr = lane & 31, lh = lane >> 5;
 
     // --- what this block does ------------------------------------------------------------------
-    int64_t start;
-    int rows, kvh, head = 0, tile, part = 0, s;
+    // Over a cache: stages [g, gend) of the sequences' stages one after the other, so that ragged lengths leave no
+    // block with more than another; units cut by a share's end are joined by attention_join_kernel.
+    int g = 0, gend = 0, base = 0, s = 0;
+    SeqShape sq{};
     if constexpr (PAGED) {
-        int b = blockIdx.x;
-        part = b % p.parts;
-        b /= p.parts;
-        tile = b % p.row_tiles;
-        b /= p.row_tiles;
-        kvh = b % p.kv_heads;
-        s = b / p.kv_heads;
-        rows_of(p, s, start, rows);
+        if (p.split) {
+            const int all = all_stages<KT, BM>(p, lane), per = max(p.least, static_cast<int>((all + gridDim.x - 1) / gridDim.x));
+            if (static_cast<int64_t>(blockIdx.x) * per >= all) return;
+            g = blockIdx.x * per;
+            gend = min(all, g + per);
+            find_stage<KT, BM>(p, lane, g, s, base);
+            sq = seq_shape<KT, BM>(p, s);
+        } else {
+            const int units = p.kv_heads * p.row_tiles;
+            s = blockIdx.x / units;
+            sq = seq_shape<KT, BM>(p, s);
+            const int unit = blockIdx.x - s * units;
+            if (unit >= sq.units) return;
+            g = unit * sq.nt;
+            gend = g + sq.nt;
+        }
+    }
+    for (;;) {
+    int64_t start;
+    int rows, kvh, head = 0, tile, past = 0, total, key0 = 0, key1, slot = 0, took = 0;
+    bool whole = true;                                // no other block has keys of these rows
+    if constexpr (PAGED) {
+        start = sq.start;
+        rows = sq.rows;
+        past = sq.past;                               // tokens before the first query's
+        total = sq.total;
+        const int row_tiles = sq.units / p.kv_heads, unit = (g - base) / sq.nt, t0 = g - base - unit * sq.nt;
+        kvh = unit / row_tiles;
+        tile = unit - kvh * row_tiles;
+        took = min(sq.nt - t0, gend - g);
+        key0 = t0 * KT;
+        key1 = min(total, key0 + took * KT);
+        whole = took == sq.nt;
+        slot = 2 * blockIdx.x + (t0 == 0);
     } else {
         // key heads fastest: the XCDs take blocks round-robin, so the query heads of a key head meet in one L2
         const int hi = blockIdx.x % p.heads, gi = hi / p.kv_heads;
@@ -203,18 +289,12 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
         head = kvh * p.group + gi;
         if (!pick_tile<BM>(p, blockIdx.x / p.heads, lane, s, tile)) return;
         rows_of(p, s, start, rows);
+        total = rows;
+        key1 = min(total, (tile + 1) * BM);
     }
     const int group = PAGED ? p.group : 1;
     const int nrow = rows * group;                    // query rows: tokens, times the heads of a group over a cache
     const int row0 = tile * BM;
-    if (row0 >= nrow) return;
-    const int past = PAGED ? min(max(p.len[s], 0), p.max_len) : 0;     // tokens before the first query's
-    const int total = PAGED ? min(min(past + rows, p.max_len), p.max_pages << p.shift) : rows;
-    // keys of this block: [key0, key1)
-    const int key0 = PAGED ? part * p.part_keys : 0;
-    int key1 = PAGED ? min(total, key0 + p.part_keys) : min(total, row0 + BM);
-    if (PAGED && key0 >= total && part > 0) return;   // (part 0 of an empty sequence stores zeros)
-    const bool whole = !PAGED || total <= p.part_keys;   // no other part: results, not partial sums
 
     // --- rows of this wave ---------------------------------------------------------------------
     int qtok[RT];                                     // the row's token within the sequence
@@ -327,6 +407,7 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
         return bits & ones(key1 - k0);
     };
 
+    bool marred = false;                              // infinities or NaN among the values were left out
     uint64_t ok = 0;                                  // blocks of the stage at hand whose page is there
     // one 32-key tile: scores, weights and products; `cut`: some row may not see some key
     auto tile32 = [&](int buf, auto sub, int k0, auto cut) __attribute__((always_inline)) {
@@ -416,7 +497,6 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
         // O^T += V^T P^T
         constexpr int STEPS = ES == 2 ? 2 : 4;        // groups of registers whose V fragments are read together
         static_for<STEPS>([&](auto u) __attribute__((always_inline)) {
-            constexpr int PER = 16 / STEPS;           // score registers of a group
             bf16x8 pf[RT];
             if constexpr (ES == 2)
 #pragma unroll
@@ -441,60 +521,33 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
             lds_wait();
 #pragma unroll
             for (int d = 0; d < DT; ++d) pin(vf[d]);
-            // Where a row does not see every key, an infinity or NaN among the values must not meet its zero weight
-            bool special = false;
+            // Where a row does not see every key, an infinity or NaN among the values must not meet its zero weight:
+            // it is left out here and added where it is seen at the end.
             if constexpr (cut) {
+                unsigned bad = 0;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        special |= ES == 2 ? (((vf[d][e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0
-                                           : (vf[d][e] & 0x7f800000u) == 0x7f800000u;
-                special = __any(special);
-            }
-            if (!special) {
+                    for (int e = 0; e < 4; ++e) bad |= not_finite<ES>(vf[d][e]);
+                if (__any(bad != 0)) {
+                    marred = true;
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
+                    for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        if constexpr (ES == 2)
-                            o[r][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d]), pf[r], o[r][d], 0, 0, 0);
-                        else
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                o[r][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(vf[d][e]), sc[r][4 * u + e], o[r][d], 0, 0, 0);
-                    }
-            } else if constexpr (cut) {
-                // one key at a time, added only where it is seen
-                for (int key = 0; key < 2 * PER; ++key) {
-                    const int kh = (key >> 2) & 1, kr = (key & 3) + 4 * (key >> 3);       // half and register of the key
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        const bool seen = (vis[r] >> (u * 2 * PER + key)) & 1;
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            f32x16 one;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) one[i] = 0.0f;
-                            if constexpr (ES == 2) {
-                                u32x4 w = vf[d];
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    w[e] &= lh != kh || (kr >> 1) != e ? 0u : (kr & 1) ? 0xffff0000u : 0xffffu;
-                                one = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf[r], one, 0, 0, 0);
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    one = __builtin_amdgcn_mfma_f32_32x32x2f32(lh == kh && kr == e ? __uint_as_float(vf[d][e]) : 0.0f,
-                                                                               sc[r][4 * u + e], one, 0, 0, 0);
-                            }
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[r][d][i] += seen ? one[i] : 0.0f;
-                            __builtin_amdgcn_sched_barrier(0);       // (one product's registers at a time)
-                        }
-                    }
+                        for (int e = 0; e < 4; ++e) vf[d][e] &= ~not_finite<ES>(vf[d][e]);
                 }
             }
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    if constexpr (ES == 2)
+                        o[r][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d]), pf[r], o[r][d], 0, 0, 0);
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            o[r][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(vf[d][e]), sc[r][4 * u + e], o[r][d], 0, 0, 0);
+                }
         });
     };
 
@@ -617,7 +670,7 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
     int pgs = 0;
     auto stage = [&](int k0, int buf) __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
+        if constexpr (!OWN) __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         const int next = pgs;
         if (k0 + KT < key1) issue(k0 + KT, buf ^ 1, next);
@@ -656,6 +709,7 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
             advance(next);
         }
     }
+    const int looked_at = k0;                         // keys from here on: one by one
     while (k0 < key1) {
         const int next = stage(k0, buf);
         static_for<SUBS>([&](auto sub) __attribute__((always_inline)) {
@@ -663,6 +717,35 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
             if (k < wave_end) tile32(buf, sub, k, std::true_type{});
         });
         advance(next);
+    }
+
+    // what was left out, where it is seen (a weight is positive: the sum becomes infinite or NaN itself)
+    if (marred) {
+        for (int key = looked_at; key < wave_end; ++key) {
+            const unsigned char* vrow;
+            if constexpr (PAGED) {
+                const int page = pages[key >> p.shift];
+                if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.pages)) continue;
+                vrow = vbase + (((static_cast<int64_t>(page) * p.kv_heads + kvh) << p.shift) + (key & ((1 << p.shift) - 1))) * (D * ES);
+            } else {
+                vrow = vbase + key * p.v_ts;
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                if (!(visible(r, key) & 1)) continue;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const unsigned* src = reinterpret_cast<const unsigned*>(vrow + (d * 32 + 8 * i + 4 * lh) * ES);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const unsigned w = ES == 2 ? (e & 1 ? src[e / 2] & 0xffff0000u : src[e / 2] << 16) : src[e];
+                            if (not_finite<4>(w)) o[r][d][4 * i + e] += __uint_as_float(w);
+                        }
+                    }
+            }
+        }
     }
 
     // --- results -----------------------------------------------------------------------------------
@@ -689,7 +772,7 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
                             *reinterpret_cast<f32x4*>(dst + dim * 4) = v;
                     }
             } else {
-                const int64_t at = ((start + qtok[r]) * p.heads + h) * p.parts + part;
+                const int64_t at = static_cast<int64_t>(slot) * BM + (row - row0);
                 if (lh == 0) {
                     p.stat[2 * at] = m[r];
                     p.stat[2 * at + 1] = l[r];
@@ -746,7 +829,7 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
                 else
                     *reinterpret_cast<f32x4*>(dst + dim * 4) = acc;
             } else {
-                const int64_t at = ((start + tok) * p.heads + h) * p.parts + part;
+                const int64_t at = static_cast<int64_t>(slot) * BM + rr;
                 if (dim == 0) {
                     p.stat[2 * at] = top;
                     p.stat[2 * at + 1] = sum;
@@ -755,35 +838,54 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
             }
         }
     }
+    if constexpr (!PAGED) {
+        return;
+    } else {
+        g += took;
+        if (g >= gend) return;
+        while (g - base >= sq.units * sq.nt) {        // (stages are left, so there is a sequence with some)
+            base += sq.units * sq.nt;
+            sq = seq_shape<KT, BM>(p, ++s);
+        }
+        __syncthreads();                              // LDS is free again
+    }
+    }
 }
 
-// Partial sums of a row's parts, in order: 32 threads a row.  Rows whose sequence has one part are done already.
-template <typename T, int D>
+// Partial sums of the units that attention_kernel's blocks cut, in block order; the block whose share of stages holds
+// a cut unit's end joins it.
+template <typename T, int D, int KT, int BM>
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p) {
-    const int s = blockIdx.y;
-    int64_t start;
-    int rows;
-    rows_of(p, s, start, rows);
-    const int past = min(max(p.len[s], 0), p.max_len);
-    const int total = min(min(past + rows, p.max_len), p.max_pages << p.shift);
-    const int parts = (total + p.part_keys - 1) / p.part_keys;
-    if (parts <= 1) return;
-    for (int row = blockIdx.x * 8 + threadIdx.x / 32; row < rows * p.heads; row += gridDim.x * 8) {
-        const int tok = row / p.heads, h = row - tok * p.heads;
-        const int64_t at = ((start + tok) * p.heads + h) * p.parts;
+    const int lane = threadIdx.x & 63;
+    const int all = all_stages<KT, BM>(p, lane), per = max(p.least, static_cast<int>((all + gridDim.x - 1) / gridDim.x));
+    if (blockIdx.x == 0 || static_cast<int64_t>(blockIdx.x) * per >= all) return;
+    const int g = blockIdx.x * per;
+    int s, base;
+    find_stage<KT, BM>(p, lane, g, s, base);
+    const SeqShape sq = seq_shape<KT, BM>(p, s);
+    const int unit = (g - base) / sq.nt, t0 = g - base - unit * sq.nt;
+    if (t0 == 0 || g - t0 + sq.nt > g + per) return;
+    const int first = (g - t0) / per, parts = blockIdx.x - first + 1;      // slot 2 first + 1, then 2 (first + i)
+    const int row_tiles = sq.units / p.kv_heads, kvh = unit / row_tiles, row0 = (unit - kvh * row_tiles) * BM;
+    const int nrow = min(BM, sq.rows * p.group - row0);
+    for (int i = threadIdx.x; i < nrow * (D / 4); i += 256) {
+        const int rr = i / (D / 4), dim = (i - rr * (D / 4)) * 4;
+        auto at = [&](int k) { return static_cast<int64_t>(2 * (first + k) + (k == 0)) * BM + rr; };
         float top = kNoMax, sum = 0.0f;
-        for (int i = 0; i < parts; ++i) top = fmaxf(top, p.stat[2 * (at + i)]);
-        float acc[D / 32] = {};
-        for (int i = 0; i < parts; ++i) {
-            const float f = __builtin_amdgcn_exp2f(p.stat[2 * (at + i)] - top);
-            sum += p.stat[2 * (at + i) + 1] * f;
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d) acc[d] += p.part[(at + i) * D + d * 32 + (threadIdx.x & 31)] * f;
+        for (int k = 0; k < parts; ++k) top = fmaxf(top, p.stat[2 * at(k)]);
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < parts; ++k) {
+            const float f = __builtin_amdgcn_exp2f(p.stat[2 * at(k)] - top);
+            sum += p.stat[2 * at(k) + 1] * f;
+            acc += *reinterpret_cast<const f32x4*>(p.part + at(k) * D + dim) * f;
         }
-        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-        T* dst = reinterpret_cast<T*>(p.out + (start + tok) * p.o_ts + h * p.o_hs);
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) dst[d * 32 + (threadIdx.x & 31)] = static_cast<T>(acc[d] * inv);
+        acc *= sum != 0.0f ? 1.0f / sum : 0.0f;
+        const int row = row0 + rr, tok = row / p.group, h = kvh * p.group + (row - tok * p.group);
+        unsigned char* dst = p.out + (sq.start + tok) * p.o_ts + h * p.o_hs;
+        if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<bf16x4*>(dst + dim * 2) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
+        else
+            *reinterpret_cast<f32x4*>(dst + dim * 4) = acc;
     }
 }
 
@@ -808,22 +910,36 @@ template <typename F> hipError_t by_type(int dtype, int d, F&& go) {
     return dtype == MOPAR_BF16 ? dims(__bf16{}) : dims(float{});
 }
 
-// Keys of a part: the least multiple of 256 that leaves no more than about two blocks a CU over all
-// sequences at their longest.
-struct CacheSplit {
-    int part_keys, parts;
+// How a call over a cache runs: the rows of a tile by the query rows of a key head, the keys of a stage, and
+// whether the blocks take equal shares of the stages.
+struct CachePlan {
+    int bm, kt, row_tiles, split, blocks;
+    int64_t slots_bytes;
 };
-CacheSplit cache_split(int n_seq, int kv_heads, int row_tiles, int max_len) {
-    const int64_t blocks = static_cast<int64_t>(n_seq) * kv_heads * row_tiles;
-    const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(blocks, 1));
-    int64_t keys = (max_len + want - 1) / want;
-    keys = std::max<int64_t>(256, (keys + 255) / 256 * 256);
-    return {static_cast<int>(std::min<int64_t>(keys, int64_t(1) << 30)), static_cast<int>((max_len + keys - 1) / keys)};
+constexpr int kLeastStages = 2;
+CachePlan cache_plan(const mopar_attention& a, int n_seq, int max_q, int max_len) {
+    CachePlan c{};
+    const bool half = a.dtype == MOPAR_BF16;
+    const int64_t rows = static_cast<int64_t>(max_q) * (a.heads / a.kv_heads);
+    c.bm = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    c.kt = c.bm == 32 ? (half ? 128 : 64) : c.bm == 64 ? 64 : half ? 64 : 32;
+    c.row_tiles = static_cast<int>((rows + c.bm - 1) / c.bm);
+    const int64_t units = static_cast<int64_t>(n_seq) * a.kv_heads * c.row_tiles, nt = (max_len + c.kt - 1) / c.kt;
+    c.split = nt > 2 * kLeastStages;
+    const int64_t blocks = c.split ? std::min<int64_t>(512, units * nt) : units;
+    c.blocks = static_cast<int>(std::min<int64_t>(blocks, int64_t(1) << 30));
+    c.slots_bytes = c.split ? int64_t(2) * c.blocks * c.bm * (a.head_dim + 2) * 4 : 0;
+    return c;
 }
 
-int cache_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
-
 }  // namespace
+
+// stages of a call over a cache at most (they are counted in 32 bits)
+bool attention_cache_fits(const mopar_attention& a, int n_seq, int max_q, int max_len) {
+    const CachePlan c = cache_plan(a, n_seq, max_q, max_len);
+    const double stages = static_cast<double>(n_seq) * a.kv_heads * c.row_tiles * ((max_len + static_cast<double>(c.kt) - 1) / c.kt);
+    return stages < 1073741824.0;
+}
 
 hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int n_seq, const int32_t* offsets, int max_len,
                                    const mopar_rows* q, const mopar_rows* k, const mopar_rows* v, const mopar_rows* out,
@@ -857,12 +973,8 @@ hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int
     });
 }
 
-size_t attention_cache_ws_bytes(const mopar_attention& a, const mopar_cache& c, int64_t tokens, int max_q, int max_len) {
-    const int64_t rows = static_cast<int64_t>(max_q) * (a.heads / a.kv_heads);
-    const int bm = cache_rows(rows);
-    const CacheSplit sp = cache_split(c.n_seq, a.kv_heads, static_cast<int>((rows + bm - 1) / bm), max_len);
-    if (sp.parts <= 1) return 0;
-    return static_cast<size_t>(tokens) * a.heads * sp.parts * (a.head_dim + 2) * 4;
+size_t attention_cache_ws_bytes(const mopar_attention& a, const mopar_cache& c, int64_t, int max_q, int max_len) {
+    return static_cast<size_t>(cache_plan(a, c.n_seq, max_q, max_len).slots_bytes);
 }
 
 hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c, int64_t tokens, const int32_t* offsets,
@@ -891,34 +1003,27 @@ hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c
     p.max_len = max_len;
     p.mask = mask;
     p.mask_words = mask_words;
-    const int64_t rows = static_cast<int64_t>(max_q) * p.group;
-    const int bm = cache_rows(rows);
-    p.row_tiles = static_cast<int>((rows + bm - 1) / bm);
-    const CacheSplit sp = cache_split(c.n_seq, a.kv_heads, p.row_tiles, max_len);
-    p.part_keys = sp.part_keys;
-    p.parts = sp.parts;
+    const CachePlan cp = cache_plan(a, c.n_seq, max_q, max_len);
+    p.row_tiles = cp.row_tiles;
+    p.split = cp.split;
+    p.least = kLeastStages;
     p.part = static_cast<float*>(ws);
-    if (sp.parts > 1) p.stat = p.part + tokens * a.heads * sp.parts * a.head_dim;
-    const int64_t blocks = static_cast<int64_t>(c.n_seq) * a.kv_heads * p.row_tiles * p.parts;
-    if (blocks >= (int64_t(1) << 31) || c.n_seq > 65535) return hipErrorInvalidValue;
-    const dim3 grid(static_cast<unsigned>(blocks));
-    hipError_t e = by_type(a.dtype, a.head_dim, [&](auto t, auto d) {
-        using T = decltype(t);
-        constexpr int F = sizeof(T) == 2 ? 1 : 0;
-        if (bm == 32)
-            launch_kernel((attention_kernel<T, d, 1, F ? 4 : 2, 1, 1, true>), grid, dim3(F ? 256 : 128), 0, s, p);
-        else if (bm == 64)
-            launch_kernel((attention_kernel<T, d, 2, 2, 1, 1, true>), grid, dim3(256), 0, s, p);
-        else
-            launch_kernel((attention_kernel<T, d, 4, 1, 1, F ? 2 : 1, true>), grid, dim3(256), 0, s, p);
-        return hipGetLastError();
-    });
-    if (e != hipSuccess || sp.parts <= 1) return e;
-    const int64_t join_rows = static_cast<int64_t>(max_q) * a.heads;
-    const dim3 jgrid(static_cast<unsigned>(std::min<int64_t>((join_rows + 7) / 8, 4096)), static_cast<unsigned>(c.n_seq));
+    if (cp.split) p.stat = p.part + int64_t(2) * cp.blocks * cp.bm * a.head_dim;
+    const dim3 grid(static_cast<unsigned>(cp.blocks));
     return by_type(a.dtype, a.head_dim, [&](auto t, auto d) {
-        launch_kernel((attention_join_kernel<decltype(t), d>), jgrid, dim3(256), 0, s, p);
-        return hipGetLastError();
+        using T = decltype(t);
+        constexpr bool H = sizeof(T) == 2;
+        auto go = [&](auto kernel, auto join, int threads) {
+            launch_kernel(kernel, grid, dim3(threads), 0, s, p);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess || !cp.split) return e;
+            launch_kernel(join, grid, dim3(256), 0, s, p);
+            return hipGetLastError();
+        };
+        if (cp.bm == 32)
+            return go(attention_kernel<T, d, 1, H ? 4 : 2, 1, 1, true>, attention_join_kernel<T, d, H ? 128 : 64, 32>, H ? 256 : 128);
+        if (cp.bm == 64) return go(attention_kernel<T, d, 2, 2, 1, 1, true>, attention_join_kernel<T, d, 64, 64>, 256);
+        return go(attention_kernel<T, d, 4, 1, 1, H ? 2 : 1, true>, attention_join_kernel<T, d, H ? 64 : 32, 128>, 256);
     });
 }
 

@@ -218,8 +218,8 @@ hipError_t launch_cache_keep(const mopar_cache& c, int layers, int64_t layer_str
 hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int n_seq, const int32_t* offsets, int max_len,
                                    const mopar_rows* q, const mopar_rows* k, const mopar_rows* v, const mopar_rows* out,
                                    hipStream_t s);
-// Attention over the paged cache: the parts that its key axis is split into (a function of what the host
-// knows) and the launches; `ws` holds attention_cache_ws_bytes.
+// Attention over the paged cache; `ws` holds attention_cache_ws_bytes.
+bool attention_cache_fits(const mopar_attention& a, int n_seq, int max_q, int max_len);
 size_t attention_cache_ws_bytes(const mopar_attention& a, const mopar_cache& c, int64_t tokens, int max_q, int max_len);
 hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c, int64_t tokens, const int32_t* offsets,
                                   int max_q, const int32_t* len, int max_len, const uint64_t* mask, int mask_words,

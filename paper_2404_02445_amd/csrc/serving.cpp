@@ -75,7 +75,8 @@ int check_cache_attention(const mopar_attention* a, const mopar_cache* c, int64_
     if (tokens < 0 || tokens >= (int64_t(1) << 31) || max_q < 0 || max_len < 1) return bad("attention: tokens, max_q or max_len");
     if (static_cast<int64_t>(max_q) * (a->heads / a->kv_heads) >= (int64_t(1) << 20))
         return set_error(MOPAR_E_UNSUPPORTED, "attention: 2^20 query rows a key head and more");
-    if (c->n_seq > 65535) return set_error(MOPAR_E_UNSUPPORTED, "attention: more than 65535 sequences");
+    if (!attention_cache_fits(*a, c->n_seq, max_q, max_len))
+        return set_error(MOPAR_E_UNSUPPORTED, "attention: sequences, key heads and max_len make 2^30 stages and more");
     return MOPAR_OK;
 }
 

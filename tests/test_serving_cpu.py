@@ -209,7 +209,7 @@ def test_cache_attention_refusals():
                dict(q=rows(None)), dict(out=rows(A, 1024, 64)), dict(max_len=100000, ws=None), dict(max_len=100000, ws=A + 8)):
         assert cache_status(**kw) == E, kw
     assert cache_status(max_q=1 << 18) == L.MOPAR_E_UNSUPPORTED
-    assert cache_status(c=cache(n_seq=65536)) == L.MOPAR_E_UNSUPPORTED
+    assert cache_status(c=cache(n_seq=1 << 30), max_len=1 << 20) == L.MOPAR_E_UNSUPPORTED
     st, need = ws_bytes(max_len=100000)
     assert st == 0 and need > 0
     assert cache_status(max_len=100000, ws_n=need - 1) == L.MOPAR_E_WORKSPACE
