@@ -44,6 +44,12 @@ __device__ __forceinline__ void load_lds(const unsigned char* base, lds_ptr_t ds
 
 constexpr float kNoMax = -3.40282347e38f;    // running maximum of a row that has seen no key
 
+// A unit that several blocks had keys of: its partial sums are slot 2 first + 1, then 2 (first + i), i < parts.
+struct CutUnit {
+    int parts, first, rows, row0, kvh, reserved;
+    int64_t start;
+};
+
 struct AttnParams {
     const unsigned char *q, *k, *v;
     unsigned char* out;
@@ -63,8 +69,17 @@ struct AttnParams {
     // partial sums [2 blocks][rows of a tile][head_dim] and their statistics, row tiles of a (sequence, key head)
     int split, least;
     float *part, *stat;
+    CutUnit* cuts;                   // a block's: the unit that it ends and did not begin (parts 0: none)
     int row_tiles;
 };
+
+// The kernel's arguments, read again: what is needed once in a while is not kept in scalar registers.
+typedef const __attribute__((address_space(4))) AttnParams* ArgsPtr;
+__device__ __forceinline__ ArgsPtr args_again() {
+    ArgsPtr a = (ArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(a));
+    return a;
+}
 
 constexpr int pow2_up(int v) { int p = 1; while (p < v) p *= 2; return p; }
 
@@ -84,22 +99,57 @@ template <int RS> __host__ __device__ constexpr int swizzle(int r) {
     return (r >> 2) & 3;
 }
 
-template <int OFF> __device__ __forceinline__ u32x4 lds_read16(unsigned addr) {
+// LDS fragment reads, in inline asm so that the compiler does not take them for readers of the direct loads in flight
+// (it would wait for all of those first).  The plain forms wait within the asm.  The `start` forms return at once: a
+// value may be touched only after an lds_wait and its pin -- nothing guards it against a spill or a copy in between, so
+// they are for the one loop whose registers all fit.
+template <int N, int OFF> __device__ __forceinline__ void lds_read16(u32x4 (&v)[N], const unsigned (&a)[N]) {
+    static_assert(OFF >= 0 && OFF < 65536 && N >= 2 && N <= 4, "ds offset");
+    if constexpr (N == 4)
+        asm volatile("ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%8\n\tds_read_b128 %2, %6 offset:%8\n\t"
+                     "ds_read_b128 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+                     : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(OFF)
+                     : "memory");
+    else if constexpr (N == 3)
+        asm volatile("ds_read_b128 %0, %3 offset:%6\n\tds_read_b128 %1, %4 offset:%6\n\tds_read_b128 %2, %5 offset:%6\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2])
+                     : "v"(a[0]), "v"(a[1]), "v"(a[2]), "n"(OFF)
+                     : "memory");
+    else
+        asm volatile("ds_read_b128 %0, %2 offset:%4\n\tds_read_b128 %1, %3 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1])
+                     : "v"(a[0]), "v"(a[1]), "n"(OFF)
+                     : "memory");
+}
+// two transposing reads: lanes 4 i .. 4 i + 3 of 16 read 4 x 4 elements of a row each, lane i gets column i of the four rows
+template <int OFF0, int OFF1> __device__ __forceinline__ void lds_read_tr(u32x2& v0, u32x2& v1, unsigned a0, unsigned a1) {
+    static_assert(OFF0 >= 0 && OFF0 < 65536 && OFF1 >= 0 && OFF1 < 65536, "ds offset");
+    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%4\n\tds_read_b64_tr_b16 %1, %3 offset:%5\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(v0), "=&v"(v1)
+                 : "v"(a0), "v"(a1), "n"(OFF0), "n"(OFF1)
+                 : "memory");
+}
+template <int O0, int O1, int O2, int O3> __device__ __forceinline__ void lds_read4(u32x4& v, const unsigned (&a)[4]) {
+    static_assert(O0 >= 0 && O3 < 65536, "ds offset");
+    unsigned w0, w1, w2, w3;
+    asm volatile("ds_read_b32 %0, %4 offset:%8\n\tds_read_b32 %1, %5 offset:%9\n\tds_read_b32 %2, %6 offset:%10\n\t"
+                 "ds_read_b32 %3, %7 offset:%11\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(w0), "=&v"(w1), "=&v"(w2), "=&v"(w3)
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(O0), "n"(O1), "n"(O2), "n"(O3)
+                 : "memory");
+    v = u32x4{w0, w1, w2, w3};
+}
+template <int OFF> __device__ __forceinline__ u32x4 lds_start16(unsigned addr) {
     static_assert(OFF >= 0 && OFF < 65536, "ds offset");
     u32x4 v;
     asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
     return v;
 }
-template <int OFF> __device__ __forceinline__ u32x2 lds_read_tr(unsigned addr) {
+template <int OFF> __device__ __forceinline__ u32x2 lds_start_tr(unsigned addr) {
     static_assert(OFF >= 0 && OFF < 65536, "ds offset");
     u32x2 v;
     asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
-    return v;
-}
-template <int OFF> __device__ __forceinline__ unsigned lds_read4(unsigned addr) {
-    static_assert(OFF >= 0 && OFF < 65536, "ds offset");
-    unsigned v;
-    asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
     return v;
 }
 // until at most N of this wave's LDS reads are still in flight (they complete in order)
@@ -159,37 +209,41 @@ template <int KT, int BM> __device__ __forceinline__ SeqShape seq_shape(const At
     q.units = (q.rows * p.group + BM - 1) / BM * p.kv_heads;
     return q;
 }
-// Stages of all sequences, which come one sequence after the other, in it one unit after the other.
-template <int KT, int BM> __device__ __forceinline__ int all_stages(const AttnParams& p, int lane) {
-    int n = 0;
-    for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
-        const SeqShape q = seq_shape<KT, BM>(p, min(s0 + lane, p.n_seq - 1));
-        n += wave_sum(s0 + lane < p.n_seq ? q.nt * q.units : 0);
-    }
-    return n;
-}
-// the sequence that stage g < all_stages is in, and its first stage
-template <int KT, int BM> __device__ __forceinline__ void find_stage(const AttnParams& p, int lane, int g, int& s, int& base) {
-    base = 0;
-    for (int s0 = 0;; s0 += 64) {
-        const SeqShape q = seq_shape<KT, BM>(p, min(s0 + lane, p.n_seq - 1));
-        const int n = s0 + lane < p.n_seq ? q.nt * q.units : 0;
+// All sequences' stages, one sequence after the other and in it one unit after the other, cut into equal shares for
+// the blocks of a grid: this block's share [g, gend), the sequence that it starts in and that one's first stage.
+// False: no share.
+struct Share {
+    int per, g, gend, s, base;
+};
+template <int KT, int BM> __device__ __forceinline__ bool take_share(const AttnParams& p, int lane, Share& sh) {
+    auto stages = [&](int s) {
+        const SeqShape q = seq_shape<KT, BM>(p, min(s, p.n_seq - 1));
+        return s < p.n_seq ? q.nt * q.units : 0;
+    };
+    const int head = stages(lane);                     // the first 64 sequences are looked up once
+    int all = wave_sum(head);
+    for (int s0 = 64; s0 < p.n_seq; s0 += 64) all += wave_sum(stages(s0 + lane));
+    all = __builtin_amdgcn_readfirstlane(all);         // (what follows is the same in every lane: scalar registers)
+    sh.per = max(p.least, static_cast<int>((all + gridDim.x - 1) / gridDim.x));
+    if (static_cast<int64_t>(blockIdx.x) * sh.per >= all) return false;
+    sh.g = blockIdx.x * sh.per;
+    sh.gend = min(all, sh.g + sh.per);
+    for (int s0 = 0, base = 0;; s0 += 64) {
+        const int n = s0 == 0 ? head : stages(s0 + lane);
         int upto = n;
 #pragma unroll
         for (int i = 1; i < 64; i *= 2) {
             const int v = __shfl_up(upto, i, 64);
             if (lane >= i) upto += v;
         }
-        const uint64_t past_g = __ballot(base + upto > g);
-        if (past_g) {
+        const uint64_t past_g = __ballot(base + upto > sh.g);
+        if (past_g) {                                  // (g < all: some chunk has it)
             const int at = static_cast<int>(__builtin_ctzll(past_g));
-            s = s0 + at;
-            base += __shfl(upto - n, at, 64);
-            s = __builtin_amdgcn_readfirstlane(s);
-            base = __builtin_amdgcn_readfirstlane(base);
-            return;
+            sh.s = __builtin_amdgcn_readfirstlane(s0 + at);
+            sh.base = __builtin_amdgcn_readfirstlane(base + __shfl(upto - n, at, 64));
+            return true;
         }
-        base += __shfl(upto, 63, 64);
+        base += __builtin_amdgcn_readlane(upto, 63);
     }
 }
 
@@ -222,38 +276,43 @@ template <int BM> __device__ __forceinline__ bool pick_tile(const AttnParams& p,
     return false;
 }
 
-// WR waves take 32 RT rows each, WK waves share a row tile and take every WK-th 32-key tile.
-template <typename T, int D, int WR, int WK, int RT, int SUBS, bool PAGED>
-__global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnParams p) {
+// A block of WR waves takes WR tiles of 32 rows.  The keys come in stages of KT through a ring of NS stages in LDS: while
+// one is worked on, NS - 1 (a single wave: all NS, each stage's place being filled again as soon as it is done) are on
+// their way.  A block of one wave needs no barrier.
+template <typename T, int D, int WR, int SUBS, int NS, bool PAGED>
+__global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams p) {
     using G = Geo<T, D>;
-    constexpr int ES = G::ES, CH = G::CH, RS = G::RS, RB = G::RB, DT = D / 32;
-    constexpr int NW = WR * WK;
-    constexpr int BM = WR * RT * 32;                 // rows of a block
-    constexpr int KT = 32 * SUBS * WK;               // keys of a stage
+    constexpr int ES = G::ES, CH = G::CH, RS = G::RS, RB = G::RB, DT = D / 32, KG = G::KG;
+    constexpr int BM = WR * 32;                      // rows of a block
+    constexpr int KT = 32 * SUBS;                    // keys of a stage
     constexpr int TILE = KT * RB;                    // bytes of K (or V) in a stage
-    constexpr int NBLK = TILE / 1024, LPW = (NBLK + NW - 1) / NW;
-    constexpr int MERGE = WK > 1 ? WK * BM * (D + 4) * 4 + WK * BM * 8 : 0;
-    constexpr int LDS = 4 * TILE > MERGE ? 4 * TILE : MERGE;
-    constexpr bool OWN = WR == 1 && WK > 1;          // a wave loads the very keys it works on: no barrier a stage
-    static_assert(TILE % 1024 == 0 && (!OWN || LPW * (64 / RS) == 32), "whole load blocks");
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
+    constexpr int NBLK = TILE / 1024, LPW = (NBLK + WR - 1) / WR;
+    constexpr int RPB = 64 / RS;                     // rows of a load block
+    constexpr bool OWN = WR == 1;
+    static_assert(TILE % 1024 == 0 && NBLK <= 64 && NS >= 2 && (NS & (NS - 1)) == 0, "stages");
+    static_assert(PAGED || NS == 2, "the loop over prompts knows its two stages at compile time");
+    static_assert((NS - 1) * 2 * LPW <= 63, "vmcnt range");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * NS * TILE];
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wr = wave % WR, wk = wave / WR;
+    const int lane = threadIdx.x & 63, wave = OWN ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lr = lane & 31, lh = lane >> 5;
 
     // --- what this block does ------------------------------------------------------------------
     // Over a cache: stages [g, gend) of the sequences' stages one after the other, so that ragged lengths leave no
     // block with more than another; units cut by a share's end are joined by attention_join_kernel.
-    int g = 0, gend = 0, base = 0, s = 0;
+    int per = 0, g = 0, gend = 0, base = 0, s = 0;
     SeqShape sq{};
     if constexpr (PAGED) {
         if (p.split) {
-            const int all = all_stages<KT, BM>(p, lane), per = max(p.least, static_cast<int>((all + gridDim.x - 1) / gridDim.x));
-            if (static_cast<int64_t>(blockIdx.x) * per >= all) return;
-            g = blockIdx.x * per;
-            gend = min(all, g + per);
-            find_stage<KT, BM>(p, lane, g, s, base);
+            Share sh;
+            const bool any = take_share<KT, BM>(p, lane, sh);
+            if (threadIdx.x == 0) p.cuts[blockIdx.x].parts = 0;       // (set below where this block ends a cut unit)
+            if (!any) return;
+            per = sh.per;
+            g = sh.g;
+            gend = sh.gend;
+            s = sh.s;
+            base = sh.base;
             sq = seq_shape<KT, BM>(p, s);
         } else {
             const int units = p.kv_heads * p.row_tiles;
@@ -266,473 +325,458 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
         }
     }
     for (;;) {
-    int64_t start;
-    int rows, kvh, head = 0, tile, past = 0, total, key0 = 0, key1, slot = 0, took = 0;
-    bool whole = true;                                // no other block has keys of these rows
-    if constexpr (PAGED) {
-        start = sq.start;
-        rows = sq.rows;
-        past = sq.past;                               // tokens before the first query's
-        total = sq.total;
-        const int row_tiles = sq.units / p.kv_heads, unit = (g - base) / sq.nt, t0 = g - base - unit * sq.nt;
-        kvh = unit / row_tiles;
-        tile = unit - kvh * row_tiles;
-        took = min(sq.nt - t0, gend - g);
-        key0 = t0 * KT;
-        key1 = min(total, key0 + took * KT);
-        whole = took == sq.nt;
-        slot = 2 * blockIdx.x + (t0 == 0);
-    } else {
-        // key heads fastest: the XCDs take blocks round-robin, so the query heads of a key head meet in one L2
-        const int hi = blockIdx.x % p.heads, gi = hi / p.kv_heads;
-        kvh = hi - gi * p.kv_heads;
-        head = kvh * p.group + gi;
-        if (!pick_tile<BM>(p, blockIdx.x / p.heads, lane, s, tile)) return;
-        rows_of(p, s, start, rows);
-        total = rows;
-        key1 = min(total, (tile + 1) * BM);
-    }
-    const int group = PAGED ? p.group : 1;
-    const int nrow = rows * group;                    // query rows: tokens, times the heads of a group over a cache
-    const int row0 = tile * BM;
+        int64_t start;
+        int rows, kvh, head = 0, tile, past = 0, total, key0 = 0, key1, slot = 0, took = 0;
+        bool whole = true;                            // no other block has keys of these rows
+        if constexpr (PAGED) {
+            start = sq.start;
+            rows = sq.rows;
+            past = sq.past;                           // tokens before the first query's
+            total = sq.total;
+            const int row_tiles = sq.units / p.kv_heads, unit = (g - base) / sq.nt, t0 = g - base - unit * sq.nt;
+            kvh = unit / row_tiles;
+            tile = unit - kvh * row_tiles;
+            took = min(sq.nt - t0, gend - g);
+            key0 = t0 * KT;
+            key1 = min(total, key0 + took * KT);
+            whole = took == sq.nt;
+            slot = 2 * blockIdx.x + (t0 == 0);
+            if (t0 > 0 && t0 + took == sq.nt && threadIdx.x == 0) {
+                const int first = (g - t0) / per;
+                args_again()->cuts[blockIdx.x] =
+                    CutUnit{static_cast<int>(blockIdx.x) - first + 1, first, min(BM, rows * p.group - tile * BM), tile * BM, kvh, 0, start};
+            }
+        } else {
+            // key heads fastest: the XCDs take blocks round-robin, so the query heads of a key head meet in one L2
+            const int hi = blockIdx.x % p.heads, gi = hi / p.kv_heads;
+            kvh = hi - gi * p.kv_heads;
+            head = kvh * p.group + gi;
+            if (!pick_tile<BM>(p, blockIdx.x / p.heads, lane, s, tile)) return;
+            rows_of(p, s, start, rows);
+            total = rows;
+            key1 = min(total, (tile + 1) * BM);
+        }
+        const int group = PAGED ? p.group : 1;
+        const int nrow = rows * group;                // query rows: tokens, times the heads of a group over a cache
+        const int row0 = tile * BM;
 
-    // --- rows of this wave ---------------------------------------------------------------------
-    int qtok[RT];                                     // the row's token within the sequence
-    u32x4 qf[RT][CH / 2];
-    const unsigned char* qrow[RT];
+        // --- this wave's rows: row lr of its 32 (past the last: that one again, never stored) ------------
+        const int row = min(row0 + wave * 32 + lr, nrow - 1);
+        const int qtok = PAGED ? row / group : row;   // the row's token within the sequence
+        const int qhead = PAGED ? kvh * group + (row - qtok * group) : head;
+        u32x4 qf[CH / 2];
+        {
+            const ArgsPtr ar = args_again();
+            const unsigned char* q = ar->q + (start + qtok) * ar->q_ts + qhead * ar->q_hs + lh * 16;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const int row = min(row0 + (wr * RT + r) * 32 + lr, nrow - 1);
-        qtok[r] = row / group;
-        const int h = PAGED ? kvh * group + (row - qtok[r] * group) : head;
-        qrow[r] = p.q + (start + qtok[r]) * p.q_ts + h * p.q_hs;
-#pragma unroll
-        for (int i = 0; i < CH / 2; ++i) qf[r][i] = *reinterpret_cast<const u32x4*>(qrow[r] + (2 * i + lh) * 16);
-    }
+            for (int i = 0; i < CH / 2; ++i) qf[i] = *reinterpret_cast<const u32x4*>(q + i * 32);
+        }
 
-    // --- loads -----------------------------------------------------------------------------------
-    // Block b of a stage is rows b * 64 / RS ..; lane l fills place l % RS of row (b * 64 + l) / RS.  Wave w
-    // loads blocks w LPW .. of K and of V.  A block's rows lie in one page unless pages are smaller than it.
-    constexpr int RPB = 64 / RS;                      // rows of a load block
-    const unsigned char* const kbase = p.k + (PAGED ? 0 : start * p.k_ts + kvh * p.k_hs);
-    const unsigned char* const vbase = p.v + (PAGED ? 0 : start * p.v_ts + kvh * p.v_hs);
-    const int lrow = lane / RS;                       // this lane's row in a block
-    auto chunk = [&](int b) __attribute__((always_inline)) { return (lane % RS) ^ swizzle<RS>(b * RPB + lrow); };
-    const int32_t* const pages = PAGED ? p.table + s * p.table_stride : nullptr;
-    // The pages of a stage's blocks, one a lane (-1: absent), are read a stage before its loads go out.
-    const bool small = PAGED && (1 << p.shift) < RPB;
-    auto pages_of = [&](int k0) __attribute__((always_inline)) -> int {
-        if constexpr (!PAGED) return 0;
-        const int key = k0 + lane * RPB;
-        int page = 0;
-        if (lane < NBLK && key < key1 && !small) page = pages[key >> p.shift];
-        return static_cast<unsigned>(page) < static_cast<unsigned>(p.pages) ? page : -1;
-    };
-    auto issue = [&](int k0, int buf, int pgs) __attribute__((always_inline)) {
-        const lds_ptr_t dst = (lds_ptr_t)(lds + buf * TILE);
-#pragma unroll
-        for (int j = 0; j < LPW; ++j) {
-            const int b = wave * LPW + j;
-            if (NBLK % NW != 0 && b >= NBLK) continue;
-            const int ch = chunk(b), key = k0 + b * RPB;             // first key of the block
-            unsigned char __attribute__((address_space(3)))* const kd = (unsigned char __attribute__((address_space(3)))*)dst + b * 1024;
-            bool in = (key + lrow < key1) & (ch < CH);
-            if constexpr (PAGED) {
-                if (!small) {
-                    const int page = __builtin_amdgcn_readlane(pgs, b);
-                    const int64_t at = (((static_cast<int64_t>(max(page, 0)) * p.kv_heads + kvh) << p.shift) + (key & ((1 << p.shift) - 1))) * (D * ES);
-                    const unsigned vo = in & (page >= 0) ? static_cast<unsigned>(lrow * (D * ES) + ch * 16) : kOOB;
-                    load_lds(kbase + at, (lds_ptr_t)kd, vo);
-                    load_lds(vbase + at, (lds_ptr_t)(kd + 2 * TILE), vo);
-                } else {
-                    const int page = in ? pages[(key + lrow) >> p.shift] : -1;
+        // --- loads -----------------------------------------------------------------------------------
+        // Block b of a stage is rows b RPB ..; lane l fills place l % RS of row b RPB + l / RS.  Wave w loads blocks
+        // w LPW .. of K and of V.  A block's rows lie in one page unless pages are smaller than it (`small`).
+        const int64_t page_bytes = (static_cast<int64_t>(p.kv_heads) << p.shift) * (D * ES);
+        const int64_t in_page = (static_cast<int64_t>(kvh) << p.shift) * (D * ES);     // of this head
+        const unsigned char* const kbase = p.k + (PAGED ? in_page : start * p.k_ts + kvh * p.k_hs);
+        const unsigned char* const vbase = p.v + (PAGED ? in_page : start * p.v_ts + kvh * p.v_hs);
+        const int lrow = lane / RS;
+        const int32_t* const pages = PAGED ? p.table + s * p.table_stride : nullptr;
+        const int page_mask = (1 << p.shift) - 1;
+        const bool small = PAGED && page_mask + 1 < RPB;
+        auto page_at = [&](unsigned page, int key) __attribute__((always_inline)) {    // byte offset of a key's row
+            return static_cast<int64_t>(page) * page_bytes + (key & page_mask) * (D * ES);
+        };
+        // The pages of a stage's blocks, one a lane, are read a stage before its loads go out.  From the first absent
+        // one on (bad_from), keys are looked at one by one.
+        int bad_from = small ? key0 : 0x7fffffff;
+        auto pages_of = [&](int k0) __attribute__((always_inline)) -> int {
+            if constexpr (!PAGED) return 0;
+            const int key = k0 + lane * RPB;
+            int page = 0;
+            if (lane < NBLK && key < key1 && !small) page = pages[key >> p.shift];
+            return page;
+        };
+        auto look_at = [&](int pgs, int k0) __attribute__((always_inline)) {
+            if constexpr (PAGED)
+                if (__any(static_cast<unsigned>(pgs) >= static_cast<unsigned>(p.pages))) bad_from = min(bad_from, k0);
+        };
+        auto issue = [&](int k0, int at, int pgs) __attribute__((always_inline)) {
+            unsigned char __attribute__((address_space(3)))* const place = (unsigned char __attribute__((address_space(3)))*)(lds_ptr_t)lds + at * TILE;
+            if (PAGED && small) {
+                for (int j = 0; j < LPW; ++j) {
+                    const int b = wave * LPW + j;
+                    if (NBLK % WR != 0 && b >= NBLK) break;
+                    const int rrow = b * RPB + lrow, ch = (lane % RS) ^ swizzle<RS>(rrow), key = k0 + rrow;
+                    const unsigned page = (key < key1) & (ch < CH) ? pages[key >> p.shift] : ~0u;
                     const unsigned char *ks = reinterpret_cast<const unsigned char*>(kZeros), *vs = ks;
-                    if (page >= 0 && page < p.pages) {
-                        const int64_t off = (((static_cast<int64_t>(page) * p.kv_heads + kvh) << p.shift) + ((key + lrow) & ((1 << p.shift) - 1))) *
-                                                (D * ES) + ch * 16;
+                    if (page < static_cast<unsigned>(p.pages)) {
+                        const int64_t off = page_at(page, key) + ch * 16;
                         ks = kbase + off;
                         vs = vbase + off;
                     }
-                    __builtin_amdgcn_global_load_lds((gptr_t)ks, (lds_ptr_t)kd, 16, 0, 0);
-                    __builtin_amdgcn_global_load_lds((gptr_t)vs, (lds_ptr_t)(kd + 2 * TILE), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)ks, (lds_ptr_t)(place + b * 1024), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)vs, (lds_ptr_t)(place + NS * TILE + b * 1024), 16, 0, 0);
                 }
-            } else {
-                const int row = b * RPB + lrow;
-                load_lds(kbase + k0 * p.k_ts, (lds_ptr_t)kd, in ? static_cast<unsigned>(row * static_cast<int>(p.k_ts)) + ch * 16 : kOOB);
-                load_lds(vbase + k0 * p.v_ts, (lds_ptr_t)(kd + 2 * TILE), in ? static_cast<unsigned>(row * static_cast<int>(p.v_ts)) + ch * 16 : kOOB);
+                return;
             }
-        }
-    };
-
-    // --- state -----------------------------------------------------------------------------------
-    f32x16 o[RT][DT];
-    float m[RT], l[RT];                               // maximum (times c) so far; this lane's share of the sum
+            // Over a cache lane b works out where block b starts.  Rows past the last key and absent pages (page 0
+            // stands for them) load what is there: keys looked at one by one leave it out.
+            unsigned lo = 0, hi = 0;
+            if constexpr (PAGED) {
+                const unsigned page = static_cast<unsigned>(pgs) < static_cast<unsigned>(p.pages) ? pgs : 0;
+                const uint64_t off = page_at(page, k0 + lane * RPB);
+                lo = static_cast<unsigned>(off), hi = static_cast<unsigned>(off >> 32);
+            }
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        m[r] = kNoMax;
-        l[r] = 0.0f;
+            for (int j = 0; j < LPW; ++j) {
+                const int b = wave * LPW + j;
+                if (NBLK % WR != 0 && b >= NBLK) continue;
+                const int rrow = b * RPB + lrow, ch = (lane % RS) ^ swizzle<RS>(rrow);
+                const lds_ptr_t kd = (lds_ptr_t)(place + b * 1024), vd = (lds_ptr_t)(place + NS * TILE + b * 1024);
+                if constexpr (PAGED) {
+                    const int64_t off = static_cast<int64_t>(__builtin_amdgcn_readlane(lo, b)) |
+                                        static_cast<int64_t>(__builtin_amdgcn_readlane(hi, b)) << 32;
+                    const unsigned vo = CH == RS || ch < CH ? static_cast<unsigned>(lrow * (D * ES) + ch * 16) : kOOB;
+                    load_lds(kbase + off, kd, vo);
+                    load_lds(vbase + off, vd, vo);
+                } else {
+                    const bool in = (k0 + rrow < key1) & (ch < CH);
+                    load_lds(kbase + k0 * p.k_ts, kd, in ? static_cast<unsigned>(rrow * static_cast<int>(p.k_ts)) + ch * 16 : kOOB);
+                    load_lds(vbase + k0 * p.v_ts, vd, in ? static_cast<unsigned>(rrow * static_cast<int>(p.v_ts)) + ch * 16 : kOOB);
+                }
+            }
+        };
+
+        // --- state -----------------------------------------------------------------------------------
+        f32x16 o[DT];
+        float m = kNoMax, l = 0.0f;                   // maximum (times c) in use; this lane's share of the sum
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[r][d][i] = 0.0f;
-    }
-    const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_ptr_t)lds));
-    // K fragment: row lr, chunk 2 st + lh;  V fragment (bf16): row 4 lh + (lane % 16) / 4 of eight, dims 16 ((lane / 16) % 2)
-    // + 4 (lane % 4) of 32; (float32): row 4 lh, dim lr of 32
-    const unsigned ka = lds0 + static_cast<unsigned>(lr * RB + ((lh ^ swizzle<RS>(lr)) << 4));
-    unsigned va;
-    if constexpr (ES == 2) {
-        const int row = 4 * lh + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-        va = lds0 + static_cast<unsigned>(2 * TILE + row * RB + ((ch ^ swizzle<RS>(row)) << 4) + (lane & 1) * 8);
-    } else {
-        const int row = 4 * lh, ch = lr >> 2;
-        va = lds0 + static_cast<unsigned>(2 * TILE + row * RB + ((ch ^ swizzle<RS>(row)) << 4) + (lr & 3) * 4);
-    }
-
-    // visible keys of a row among 64 from k0 on, one bit each
-    auto visible = [&](int r, int k0) -> uint64_t {
-        const int own = total - past;                 // drafted tokens within bounds
-        auto ones = [](int n) -> uint64_t { return n <= 0 ? 0 : n >= 64 ? ~uint64_t(0) : (uint64_t(1) << n) - 1; };
-        if (!PAGED || !p.mask) return ones(min(past + qtok[r] + 1, key1) - k0);
-        const uint64_t* mrow = p.mask + (start + qtok[r]) * p.mask_words;
-        const int j0 = k0 - past;
-        uint64_t bits;
-        if (j0 >= 0) {
-            const int w = j0 >> 6, sh = j0 & 63;
-            const uint64_t lo = w < p.mask_words ? mrow[w] : 0, hi = w + 1 < p.mask_words ? mrow[w + 1] : 0;
-            bits = (sh ? (lo >> sh) | (hi << (64 - sh)) : lo) & ones(own - j0);
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+        const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_ptr_t)lds));
+        // K fragment: row lr, chunk 2 st + lh;  V fragment (bf16): row 4 lh + (lane % 16) / 4 of eight, dims 16 ((lane / 16) % 2)
+        // + 4 (lane % 4) of 32; (float32): row 4 lh, dim lr of 32
+        const unsigned ka = lds0 + static_cast<unsigned>(lr * RB + ((lh ^ swizzle<RS>(lr)) << 4));
+        unsigned va;
+        if constexpr (ES == 2) {
+            const int vrow = 4 * lh + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+            va = lds0 + static_cast<unsigned>(NS * TILE + vrow * RB + ((ch ^ swizzle<RS>(vrow)) << 4) + (lane & 1) * 8);
         } else {
-            bits = ones(-j0) | (-j0 < 64 ? (mrow[0] & ones(own)) << -j0 : 0);
+            const int vrow = 4 * lh, ch = lr >> 2;
+            va = lds0 + static_cast<unsigned>(NS * TILE + vrow * RB + ((ch ^ swizzle<RS>(vrow)) << 4) + (lr & 3) * 4);
         }
-        return bits & ones(key1 - k0);
-    };
 
-    bool marred = false;                              // infinities or NaN among the values were left out
-    uint64_t ok = 0;                                  // blocks of the stage at hand whose page is there
-    // one 32-key tile: scores, weights and products; `cut`: some row may not see some key
-    auto tile32 = [&](int buf, auto sub, int k0, auto cut) __attribute__((always_inline)) {
-        const int st0 = buf * TILE + (WK > 1 ? wk * 32 * RB : 0);
-        f32x16 sc[RT];
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[r][i] = 0.0f;
-        constexpr int KG = G::KG, NKG = CH / 2 / KG;      // K fragments of a group, groups
-        u32x4 kf[2][KG];
-        auto read_k = [&](auto g) __attribute__((always_inline)) {
-            static_for<KG>([&](auto e) __attribute__((always_inline)) {
-                constexpr int slot = g % 2, st = g * KG + e, el = e;
-                kf[slot][el] = lds_read16<sub * 32 * RB>((ka + st0) ^ (st << 5));
-            });
-        };
-        read_k(std::integral_constant<int, 0>{});
-        static_for<NKG>([&](auto g) __attribute__((always_inline)) {
-            constexpr int slot = g % 2;
-            if constexpr (g + 1 < NKG) {
-                read_k(std::integral_constant<int, g + 1>{});
-                lds_wait<KG>();
+        // visible keys of this lane's row among 64 from k0 on, one bit each
+        auto visible = [&](int k0) -> uint64_t {
+            auto ones = [](int n) -> uint64_t { return n <= 0 ? 0 : n >= 64 ? ~uint64_t(0) : (uint64_t(1) << n) - 1; };
+            const ArgsPtr ar = args_again();
+            const uint64_t* mrow = PAGED ? ar->mask : nullptr;
+            if (!mrow) return ones(min(past + qtok + 1, key1) - k0);
+            const int words = ar->mask_words;
+            mrow += (start + qtok) * words;
+            const int j0 = k0 - past, own = total - past;       // drafted tokens within bounds
+            uint64_t bits;
+            if (j0 >= 0) {
+                const int w = j0 >> 6, sh = j0 & 63;
+                const uint64_t lo = w < words ? mrow[w] : 0, hi = w + 1 < words ? mrow[w + 1] : 0;
+                bits = (sh ? (lo >> sh) | (hi << (64 - sh)) : lo) & ones(own - j0);
             } else {
-                lds_wait();
+                bits = ones(-j0) | (-j0 < 64 ? (mrow[0] & ones(own)) << -j0 : 0);
             }
-            static_for<KG>([&](auto e) __attribute__((always_inline)) {
-                constexpr int st = g * KG + e, el = e;
-                pin(kf[slot][el]);
+            return bits & ones(key1 - k0);
+        };
+
+        bool marred = false;                          // infinities or NaN among the values were left out
+        // one 32-key tile of the stage at place `at`; `cut`: some row may not see some key
+        auto tile32 = [&](int at, auto sub, int k0, auto cut) __attribute__((always_inline)) {
+            const int st0 = at * TILE;
+            f32x16 sc;
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
+            for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+            constexpr int NKG = CH / 2 / KG;          // groups of K fragments
+            static_for<NKG>([&](auto gr) __attribute__((always_inline)) {
+                u32x4 kf[KG];
+                unsigned a[KG];
+#pragma unroll
+                for (int e = 0; e < KG; ++e) a[e] = (ka + st0) ^ ((gr * KG + e) << 5);
+                lds_read16<KG, sub * 32 * RB>(kf, a);
+#pragma unroll
+                for (int e = 0; e < KG; ++e) {
                     if constexpr (ES == 2)
-                        sc[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[slot][el]),
-                                                                        __builtin_bit_cast(bf16x8, qf[r][st]), sc[r], 0, 0, 0);
+                        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[e]), __builtin_bit_cast(bf16x8, qf[gr * KG + e]),
+                                                                     sc, 0, 0, 0);
                     else
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
-                            sc[r] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[slot][el][c]), __uint_as_float(qf[r][st][c]), sc[r],
-                                                                         0, 0, 0);
+                            sc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e][c]), __uint_as_float(qf[gr * KG + e][c]), sc, 0, 0, 0);
                 }
             });
-        });
-        uint64_t vis[RT];
-        if constexpr (cut) {
-            // keys of absent pages
-            uint64_t held = ~uint64_t(0);
-            if constexpr (PAGED) {
-                if (small) {
-                    const int key = k0 + lane, page = lane < 32 && key < key1 ? pages[key >> p.shift] : -1;
-                    held = __ballot(static_cast<unsigned>(page) < static_cast<unsigned>(p.pages));
-                } else {
-                    constexpr int NB = 32 / RPB;
-                    const int b0 = (WK > 1 ? wk * 32 : sub * 32) / RPB;
-                    held = 0;
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-                        if ((ok >> (b0 + b)) & 1) held |= ((uint64_t(1) << RPB) - 1) << (b * RPB);
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                vis[r] = visible(r, k0) & held;
+            if constexpr (cut) {
+                uint64_t vis = visible(k0);
+                if constexpr (PAGED)
+                    if (k0 + 32 > bad_from) {         // keys of absent pages
+                        const int key = k0 + lane;
+                        const unsigned page = lane < 32 && key < key1 ? pages[key >> p.shift] : ~0u;
+                        vis &= __ballot(page < static_cast<unsigned>(p.pages));
+                    }
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (!((vis[r] >> (8 * (i / 4) + 4 * lh + i % 4)) & 1)) sc[r][i] = -INFINITY;
+                    if (!((vis >> (8 * (i / 4) + 4 * lh + i % 4)) & 1)) sc[i] = -INFINITY;
             }
-        }
+            float mx = sc[0];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            float mx = sc[r][0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[r][i]);
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
             mx = fmaxf(mx, other_half(mx)) * p.c;
-            const float mn = fmaxf(m[r], mx), f = __builtin_amdgcn_exp2f(m[r] - mn);
-            m[r] = mn;
-            l[r] *= f;
+            const float mn = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= f;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[r][d][i] *= f;
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                sc[r][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r][i], p.c, -mn));
-                l[r] += sc[r][i];
+                sc[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], p.c, -mn));
+                l += sc[i];
             }
-        }
-        // O^T += V^T P^T
-        constexpr int STEPS = ES == 2 ? 2 : 4;        // groups of registers whose V fragments are read together
-        static_for<STEPS>([&](auto u) __attribute__((always_inline)) {
-            bf16x8 pf[RT];
-            if constexpr (ES == 2)
+            // O^T += V^T P^T
+            constexpr int STEPS = ES == 2 ? 2 : 4;    // groups of registers whose V fragments are read together
+            static_for<STEPS>([&](auto u) __attribute__((always_inline)) {
+                bf16x8 pf;
+                if constexpr (ES == 2)
 #pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) pf[r][i] = static_cast<__bf16>(sc[r][8 * u + i]);
-            u32x4 vf[DT];
-            if constexpr (ES == 2) {
+                    for (int i = 0; i < 8; ++i) pf[i] = static_cast<__bf16>(sc[8 * u + i]);
+                u32x4 vf[DT];
                 static_for<DT>([&](auto d) __attribute__((always_inline)) {
-                    const u32x2 lo = lds_read_tr<(sub * 32 + u * 16) * RB>((va + st0) ^ (d << 6));
-                    const u32x2 hi = lds_read_tr<(sub * 32 + u * 16 + 8) * RB>((va + st0) ^ ((d << 6) | (swizzle<RS>(8) << 4)));
-                    vf[d] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                    if constexpr (ES == 2) {
+                        constexpr int R0 = (sub * 32 + u * 16) * RB;
+                        u32x2 lo, hi;
+                        lds_read_tr<R0, R0 + 8 * RB>(lo, hi, (va + st0) ^ (d << 6), (va + st0) ^ ((d << 6) | (swizzle<RS>(8) << 4)));
+                        vf[d] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                    } else {
+                        constexpr int R0 = sub * 32 + 8 * u;
+                        unsigned a[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) a[e] = (va + st0) ^ ((d << 7) ^ (swizzle<RS>(8 * u + e) << 4));
+                        lds_read4<R0 * RB, (R0 + 1) * RB, (R0 + 2) * RB, (R0 + 3) * RB>(vf[d], a);
+                    }
                 });
-            } else {
-                static_for<DT>([&](auto d) __attribute__((always_inline)) {
-                    static_for<4>([&](auto e) __attribute__((always_inline)) {
-                        constexpr int row = 8 * u + e, el = e;
-                        vf[d][el] = lds_read4<(sub * 32 + row) * RB>((va + st0) ^ ((d << 7) ^ (swizzle<RS>(row) << 4)));
-                    });
-                });
-            }
-            lds_wait();
-#pragma unroll
-            for (int d = 0; d < DT; ++d) pin(vf[d]);
-            // Where a row does not see every key, an infinity or NaN among the values must not meet its zero weight:
-            // it is left out here and added where it is seen at the end.
-            if constexpr (cut) {
-                unsigned bad = 0;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) bad |= not_finite<ES>(vf[d][e]);
-                if (__any(bad != 0)) {
-                    marred = true;
+                // Where a row does not see every key, an infinity or NaN among the values must not meet its zero weight:
+                // it is left out here and added where it is seen at the end.
+                if constexpr (cut) {
+                    unsigned bad = 0;
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) vf[d][e] &= ~not_finite<ES>(vf[d][e]);
+                        for (int e = 0; e < 4; ++e) bad |= not_finite<ES>(vf[d][e]);
+                    if (__any(bad != 0)) {
+                        marred = true;
+#pragma unroll
+                        for (int d = 0; d < DT; ++d)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) vf[d][e] &= ~not_finite<ES>(vf[d][e]);
+                    }
                 }
-            }
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
+                for (int d = 0; d < DT; ++d) {
                     if constexpr (ES == 2)
-                        o[r][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d]), pf[r], o[r][d], 0, 0, 0);
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d]), pf, o[d], 0, 0, 0);
                     else
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            o[r][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(vf[d][e]), sc[r][4 * u + e], o[r][d], 0, 0, 0);
+                            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(vf[d][e]), sc[4 * u + e], o[d], 0, 0, 0);
                 }
-        });
-    };
+            });
+        };
 
-    // a stage that every row sees whole: the 32-key tiles of this wave together
-    unsigned kr[ES == 2 ? CH / 2 : 1], vr[ES == 2 ? 2 * DT : 1];
-    if constexpr (ES == 2) {
-        static_for<CH / 2>([&](auto st) __attribute__((always_inline)) { kr[st] = ((ka + (WK > 1 ? wk * 32 * RB : 0)) ^ (st << 5)); });
-        static_for<DT>([&](auto d) __attribute__((always_inline)) {
-            vr[2 * d] = (va + (WK > 1 ? wk * 32 * RB : 0)) ^ (d << 6);
-            vr[2 * d + 1] = vr[2 * d] ^ (swizzle<RS>(8) << 4);
-        });
-    }
-    auto full = [&](auto buf) __attribute__((always_inline)) {
-        constexpr int B0 = buf * TILE;
-        constexpr int KG = G::KG, NKG = SUBS * (CH / 2) / KG;     // K fragments of a group, groups
-        f32x16 sc[SUBS][RT];
-#pragma unroll
-        for (int t = 0; t < SUBS; ++t)
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sc[t][r][i] = 0.0f;
-        u32x4 kf[2][KG];
-        auto read_k = [&](auto g) __attribute__((always_inline)) {
-            static_for<KG>([&](auto e) __attribute__((always_inline)) {
-                constexpr int st = (g * KG + e) % (CH / 2), sub = (g * KG + e) / (CH / 2), slot = g % 2;
-                kf[slot][e] = lds_read16<B0 + sub * 32 * RB>(kr[st]);
-            });
-        };
-        read_k(std::integral_constant<int, 0>{});
-        static_for<NKG>([&](auto g) __attribute__((always_inline)) {
-            constexpr int slot = g % 2;
-            if constexpr (g + 1 < NKG) {
-                read_k(std::integral_constant<int, g + 1>{});
-                lds_wait<KG>();
-            } else {
-                lds_wait();
-            }
-            static_for<KG>([&](auto e) __attribute__((always_inline)) {
-                constexpr int st = (g * KG + e) % (CH / 2), sub = (g * KG + e) / (CH / 2);
-                pin(kf[slot][e]);
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-                    sc[sub][r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[slot][e]),
-                                                                         __builtin_bit_cast(bf16x8, qf[r][st]), sc[sub][r], 0, 0, 0);
-            });
-        });
-        // the first values on their way under the softmax
-        constexpr int NVG = 2 * SUBS;
-        u32x2 vf[2][2 * DT];
-        auto read_v = [&](auto g) __attribute__((always_inline)) {
+        // a stage that every row sees whole (bf16): its 32-key tiles together.  `at` is its place in the ring, a
+        // compile-time constant over prompts (folded into the reads' offsets).
+        unsigned kr[ES == 2 && !PAGED ? CH / 2 : 1], vr[ES == 2 && !PAGED ? 2 * DT : 1];
+        if constexpr (ES == 2 && !PAGED) {
+            static_for<CH / 2>([&](auto st) __attribute__((always_inline)) { kr[st] = ka ^ (st << 5); });
             static_for<DT>([&](auto d) __attribute__((always_inline)) {
-                constexpr int slot = g % 2, off = B0 + (g / 2 * 32 + g % 2 * 16) * RB;
-                vf[slot][2 * d] = lds_read_tr<off>(vr[2 * d]);
-                vf[slot][2 * d + 1] = lds_read_tr<off + 8 * RB>(vr[2 * d + 1]);
+                vr[2 * d] = va ^ (d << 6);
+                vr[2 * d + 1] = vr[2 * d] ^ (swizzle<RS>(8) << 4);
             });
-        };
-        read_v(std::integral_constant<int, 0>{});
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            float mx = sc[0][r][0];
+        }
+        auto full = [&](auto at) __attribute__((always_inline)) {
+            constexpr int B0 = [] { if constexpr (PAGED) return 0; else return decltype(at)::value * TILE; }();
+            unsigned kd = 0, vd = 0;                  // the reads' bases in this stage
+            if constexpr (PAGED) kd = ka + at * TILE, vd = va + at * TILE;
+            constexpr int NKG = SUBS * (CH / 2) / KG; // groups of K fragments
+            f32x16 sc[SUBS];
 #pragma unroll
             for (int t = 0; t < SUBS; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, sc[t][r][i]), sc[t][r][i + 1]);
+                for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
+            u32x4 kf[2][KG];
+            auto read_k = [&](auto gr) __attribute__((always_inline)) {
+                static_for<KG>([&](auto e) __attribute__((always_inline)) {
+                    constexpr int st = (gr * KG + e) % (CH / 2), sub = (gr * KG + e) / (CH / 2), half = gr % 2;
+                    kf[half][e] = lds_start16<B0 + sub * 32 * RB>(PAGED ? kd ^ (st << 5) : kr[PAGED ? 0 : st]);
+                });
+            };
+            read_k(std::integral_constant<int, 0>{});
+            static_for<NKG>([&](auto gr) __attribute__((always_inline)) {
+                constexpr int half = gr % 2;
+                if constexpr (gr + 1 < NKG) {
+                    read_k(std::integral_constant<int, gr + 1>{});
+                    lds_wait<KG>();
+                } else {
+                    lds_wait();
+                }
+                static_for<KG>([&](auto e) __attribute__((always_inline)) {
+                    constexpr int st = (gr * KG + e) % (CH / 2), sub = (gr * KG + e) / (CH / 2);
+                    pin(kf[half][e]);
+                    sc[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[half][e]), __builtin_bit_cast(bf16x8, qf[st]),
+                                                                      sc[sub], 0, 0, 0);
+                });
+            });
+            // the first values on their way under the softmax
+            constexpr int NVG = 2 * SUBS;
+            u32x2 vf[2][2 * DT];
+            auto read_v = [&](auto gr) __attribute__((always_inline)) {
+                static_for<DT>([&](auto d) __attribute__((always_inline)) {
+                    constexpr int half = gr % 2, off = B0 + gr * 16 * RB;
+                    vf[half][2 * d] = lds_start_tr<off>(PAGED ? vd ^ (d << 6) : vr[PAGED ? 0 : 2 * d]);
+                    vf[half][2 * d + 1] = lds_start_tr<off + 8 * RB>(PAGED ? vd ^ ((d << 6) | (swizzle<RS>(8) << 4)) : vr[PAGED ? 0 : 2 * d + 1]);
+                });
+            };
+            read_v(std::integral_constant<int, 0>{});
+            float mx = sc[0][0];
+#pragma unroll
+            for (int t = 0; t < SUBS; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, sc[t][i]), sc[t][i + 1]);
             mx = fmaxf(mx, other_half(mx)) * p.c;
             // The maximum in use may lag by up to 8 (weights stay below 2^8): rescaling is rare.
-            if (__any(mx > m[r] + 8.0f)) {
-                const float mn = fmaxf(m[r], mx), f = __builtin_amdgcn_exp2f(m[r] - mn);
-                m[r] = mn;
-                l[r] *= f;
+            if (__any(mx > m + 8.0f)) {
+                const float mn = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                l *= f;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[r][d][i] *= f;
+                    for (int i = 0; i < 16; ++i) o[d][i] *= f;
             }
             float sum[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int t = 0; t < SUBS; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    sc[t][r][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][r][i], p.c, -m[r]));
-                    sum[i & 1] += sc[t][r][i];
+                    sc[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][i], p.c, -m));
+                    sum[i & 1] += sc[t][i];
                 }
-            l[r] += sum[0] + sum[1];
-        }
-        static_for<NVG>([&](auto g) __attribute__((always_inline)) {
-            constexpr int slot = g % 2;
-            if constexpr (g + 1 < NVG) {
-                read_v(std::integral_constant<int, g + 1>{});
-                lds_wait<2 * DT>();
-            } else {
-                lds_wait();
-            }
-            bf16x8 pf[RT];
+            l += sum[0] + sum[1];
+            static_for<NVG>([&](auto gr) __attribute__((always_inline)) {
+                constexpr int half = gr % 2;
+                if constexpr (gr + 1 < NVG) {
+                    read_v(std::integral_constant<int, gr + 1>{});
+                    lds_wait<2 * DT>();
+                } else {
+                    lds_wait();
+                }
+                bf16x8 pf;
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
+                for (int i = 0; i < 8; ++i) pf[i] = static_cast<__bf16>(sc[gr / 2][8 * (gr % 2) + i]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) pf[r][i] = static_cast<__bf16>(sc[g / 2][r][8 * (g % 2) + i]);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                pin(vf[slot][2 * d]);
-                pin(vf[slot][2 * d + 1]);
-                const u32x4 w = {vf[slot][2 * d][0], vf[slot][2 * d][1], vf[slot][2 * d + 1][0], vf[slot][2 * d + 1][1]};
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-                    o[r][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf[r], o[r][d], 0, 0, 0);
-            }
-        });
-    };
-
-    // --- the keys ----------------------------------------------------------------------------------
-    // rows of this wave, all of them past the last visible key of the tile: nothing to do (causal)
-    const int wave_end = PAGED ? key1 : min(key1, row0 + (wr + 1) * RT * 32);
-    // Stages that every row of the block sees whole come first; from an absent page on, every stage is looked at
-    // key by key.
-    constexpr uint64_t ALL = NBLK >= 64 ? ~uint64_t(0) : (uint64_t(1) << NBLK) - 1;
-    const int seen = PAGED ? min(past, key1) : row0 + 1;
-    const int full_end = seen > key0 && !small ? key0 + (seen - key0) / KT * KT : key0;
-    int pgs = 0;
-    auto stage = [&](int k0, int buf) __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if constexpr (!OWN) __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        const int next = pgs;
-        if (k0 + KT < key1) issue(k0 + KT, buf ^ 1, next);
-        if constexpr (PAGED) pgs = pages_of(k0 + 2 * KT);
-        return next;
-    };
-    int k0 = key0, buf = 0;
-    if (key0 < key1) {
-        pgs = pages_of(key0);
-        issue(key0, 0, pgs);
-        ok = PAGED ? __ballot(pgs >= 0) & ALL : ALL;
-        pgs = pages_of(key0 + KT);
-    }
-    // compute of a stage is done: what the next one holds
-    auto advance = [&](int next) __attribute__((always_inline)) {
-        if constexpr (PAGED) ok = __ballot(next >= 0) & ALL;
-        k0 += KT;
-        buf ^= 1;
-    };
-    if constexpr (ES == 2) {
-        while (k0 < full_end && ok == ALL) {
-            int next = stage(k0, 0);
-            full(std::integral_constant<int, 0>{});
-            advance(next);
-            if (k0 >= full_end || ok != ALL) break;
-            next = stage(k0, 1);
-            full(std::integral_constant<int, 1>{});
-            advance(next);
-        }
-    } else {
-        while (k0 < full_end && ok == ALL) {
-            const int next = stage(k0, buf);
-            static_for<SUBS>([&](auto sub) __attribute__((always_inline)) {
-                tile32(buf, sub, k0 + (WK > 1 ? wk * 32 : 0) + sub * 32, std::false_type{});
+                for (int d = 0; d < DT; ++d) {
+                    pin(vf[half][2 * d]);
+                    pin(vf[half][2 * d + 1]);
+                    const u32x4 w = {vf[half][2 * d][0], vf[half][2 * d][1], vf[half][2 * d + 1][0], vf[half][2 * d + 1][1]};
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf, o[d], 0, 0, 0);
+                }
             });
-            advance(next);
-        }
-    }
-    const int looked_at = k0;                         // keys from here on: one by one
-    while (k0 < key1) {
-        const int next = stage(k0, buf);
-        static_for<SUBS>([&](auto sub) __attribute__((always_inline)) {
-            const int k = k0 + (WK > 1 ? wk * 32 : 0) + sub * 32;
-            if (k < wave_end) tile32(buf, sub, k, std::true_type{});
-        });
-        advance(next);
-    }
+        };
 
-    // what was left out, where it is seen (a weight is positive: the sum becomes infinite or NaN itself)
-    if (marred) {
-        for (int key = looked_at; key < wave_end; ++key) {
-            const unsigned char* vrow;
-            if constexpr (PAGED) {
-                const int page = pages[key >> p.shift];
-                if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.pages)) continue;
-                vrow = vbase + (((static_cast<int64_t>(page) * p.kv_heads + kvh) << p.shift) + (key & ((1 << p.shift) - 1))) * (D * ES);
-            } else {
-                vrow = vbase + key * p.v_ts;
-            }
+        // --- the keys ----------------------------------------------------------------------------------
+        // keys past the last that this wave's rows see (causal): nothing to do
+        const int wave_end = PAGED ? (row0 + wave * 32 < nrow ? key1 : key0) : min(key1, row0 + (wave + 1) * 32);
+        // stages that every row of the block sees whole come first
+        const int seen = PAGED ? min(past, key1) : row0 + 1;
+        const int full_end = seen > key0 ? key0 + (seen - key0) / KT * KT : key0;
+        constexpr int AHEAD = OWN ? NS : NS - 1;      // stages on their way when one is begun
+        int k0 = key0, at = 0, pgs = 0;               // the stage at hand, its place, the pages of stage k0 + AHEAD KT
+        if (key0 < key1) {
+            int first[AHEAD];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                if (!(visible(r, key) & 1)) continue;
+            for (int i = 0; i < AHEAD; ++i) first[i] = pages_of(key0 + i * KT);
+            pgs = pages_of(key0 + AHEAD * KT);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                look_at(first[i], key0 + i * KT);
+                if (key0 + i * KT < key1) issue(key0 + i * KT, i, first[i]);
+            }
+        }
+        // stage k0 + AHEAD KT to its place, and the pages of the one after it
+        auto ahead = [&]() __attribute__((always_inline)) {
+            const int now = pgs;
+            pgs = pages_of(k0 + (AHEAD + 1) * KT);
+            look_at(now, k0 + AHEAD * KT);
+            if (k0 + AHEAD * KT < key1) issue(k0 + AHEAD * KT, (at + AHEAD) & (NS - 1), now);
+        };
+        // the stage at hand has arrived once only the loads of the AHEAD - 1 after it (or later ones) are on their way
+        auto begin = [&]() __attribute__((always_inline)) {
+            if (AHEAD > 1 && k0 + (AHEAD - 1) * KT < key1)
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NBLK % WR == 0 ? (AHEAD - 1) * 2 * LPW : 0) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if constexpr (!OWN) {
+                __builtin_amdgcn_s_barrier();         // for every wave, and none works on the stage before any more
+                asm volatile("" ::: "memory");
+                ahead();
+            }
+        };
+        auto end = [&]() __attribute__((always_inline)) {
+            if constexpr (OWN) ahead();
+            k0 += KT;
+            at = (at + 1) & (NS - 1);
+        };
+        if constexpr (!PAGED && ES == 2) {
+            while (k0 < full_end) {
+                begin();
+                full(std::integral_constant<int, 0>{});
+                end();
+                if (k0 >= full_end) break;
+                begin();
+                full(std::integral_constant<int, 1>{});
+                end();
+            }
+        } else {
+            while (k0 < full_end && k0 + KT <= bad_from) {
+                begin();
+                if constexpr (ES == 2) {
+                    if (OWN || k0 < wave_end) full(at);
+                } else {
+                    static_for<SUBS>([&](auto sub) __attribute__((always_inline)) {
+                        if (OWN || k0 < wave_end) tile32(at, sub, k0 + sub * 32, std::false_type{});
+                    });
+                }
+                end();
+            }
+        }
+        const int looked_at = k0;                     // keys from here on: one by one
+        while (k0 < key1) {
+            begin();
+            static_for<SUBS>([&](auto sub) __attribute__((always_inline)) {
+                if (k0 + sub * 32 < wave_end) tile32(at, sub, k0 + sub * 32, std::true_type{});
+            });
+            end();
+        }
+
+        // what was left out, where it is seen (a weight is positive: the sum becomes infinite or NaN itself)
+        if (marred) {
+            for (int key = looked_at; key < wave_end; ++key) {
+                const unsigned char* vrow;
+                if constexpr (PAGED) {
+                    const unsigned page = pages[key >> p.shift];
+                    if (page >= static_cast<unsigned>(p.pages)) continue;
+                    vrow = vbase + page_at(page, key);
+                } else {
+                    vrow = vbase + key * p.v_ts;
+                }
+                if (!(visible(key) & 1)) continue;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -741,30 +785,24 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const unsigned w = ES == 2 ? (e & 1 ? src[e / 2] & 0xffff0000u : src[e / 2] << 16) : src[e];
-                            if (not_finite<4>(w)) o[r][d][4 * i + e] += __uint_as_float(w);
+                            if (not_finite<4>(w)) o[d][4 * i + e] += __uint_as_float(w);
                         }
                     }
             }
         }
-    }
 
-    // --- results -----------------------------------------------------------------------------------
-#pragma unroll
-    for (int r = 0; r < RT; ++r) l[r] += other_half(l[r]);
-    if constexpr (WK == 1) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const int row = row0 + (wr * RT + r) * 32 + lr;
-            if (row >= nrow) continue;
-            const int h = PAGED ? kvh * group + (row - qtok[r] * group) : head;
+        // --- results -----------------------------------------------------------------------------------
+        l += other_half(l);
+        const ArgsPtr ar = args_again();
+        if (row0 + wave * 32 + lr < nrow) {
             if (whole) {
-                const float inv = l[r] != 0.0f ? 1.0f / l[r] : 0.0f;
-                unsigned char* dst = p.out + (start + qtok[r]) * p.o_ts + h * p.o_hs;
+                const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+                unsigned char* dst = ar->out + (start + qtok) * ar->o_ts + qhead * ar->o_hs;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const f32x4 v = {o[r][d][4 * i] * inv, o[r][d][4 * i + 1] * inv, o[r][d][4 * i + 2] * inv, o[r][d][4 * i + 3] * inv};
+                        const f32x4 v = {o[d][4 * i] * inv, o[d][4 * i + 1] * inv, o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv};
                         const int dim = d * 32 + 8 * i + 4 * lh;
                         if constexpr (ES == 2)
                             *reinterpret_cast<bf16x4*>(dst + dim * 2) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
@@ -772,120 +810,78 @@ __global__ __launch_bounds__(WR * WK * 64, 2) void attention_kernel(const AttnPa
                             *reinterpret_cast<f32x4*>(dst + dim * 4) = v;
                     }
             } else {
-                const int64_t at = static_cast<int64_t>(slot) * BM + (row - row0);
+                const int64_t to = static_cast<int64_t>(slot) * BM + wave * 32 + lr;
                 if (lh == 0) {
-                    p.stat[2 * at] = m[r];
-                    p.stat[2 * at + 1] = l[r];
+                    ar->stat[2 * to] = m;
+                    ar->stat[2 * to + 1] = l;
                 }
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<f32x4*>(p.part + at * D + d * 32 + 8 * i + 4 * lh) =
-                            f32x4{o[r][d][4 * i], o[r][d][4 * i + 1], o[r][d][4 * i + 2], o[r][d][4 * i + 3]};
+                        *reinterpret_cast<f32x4*>(ar->part + to * D + d * 32 + 8 * i + 4 * lh) =
+                            f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
             }
         }
-    } else {
-        // the waves of a row tile meet in LDS
-        static_assert(RT == 1 || WK == 1, "one row tile a wave");
-        constexpr int LD = D + 4;
-        __syncthreads();                              // the last stage has been read
-        float* const os = reinterpret_cast<float*>(lds);
-        float* const ms = os + WK * BM * LD;
-        {
-            const int row = wr * 32 + lr;
-            float* dst = os + (wk * BM + row) * LD + 4 * lh;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<f32x4*>(dst + d * 32 + 8 * i) = f32x4{o[0][d][4 * i], o[0][d][4 * i + 1], o[0][d][4 * i + 2], o[0][d][4 * i + 3]};
-            if (lh == 0) {
-                ms[(wk * BM + row) * 2] = m[0];
-                ms[(wk * BM + row) * 2 + 1] = l[0];
+        if constexpr (!PAGED) {
+            return;
+        } else {
+            g += took;
+            if (g >= gend) return;
+            while (g - base >= sq.units * sq.nt) {    // (stages are left, so there is a sequence with some)
+                base += sq.units * sq.nt;
+                sq = seq_shape<KT, BM>(p, ++s);
             }
+            if constexpr (!OWN) __syncthreads();      // every wave is done with the ring
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < BM * (D / 4); i += NW * 64) {
-            const int rr = i / (D / 4), dim = (i - rr * (D / 4)) * 4, row = row0 + rr;
-            if (row >= nrow) continue;
-            float top = kNoMax, sum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < WK; ++w) top = fmaxf(top, ms[(w * BM + rr) * 2]);
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < WK; ++w) {
-                const float f = __builtin_amdgcn_exp2f(ms[(w * BM + rr) * 2] - top);
-                sum += ms[(w * BM + rr) * 2 + 1] * f;
-                acc += *reinterpret_cast<const f32x4*>(os + (w * BM + rr) * LD + dim) * f;
-            }
-            const int tok = row / group, h = PAGED ? kvh * group + (row - tok * group) : head;
-            if (whole) {
-                const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-                unsigned char* dst = p.out + (start + tok) * p.o_ts + h * p.o_hs;
-                acc *= inv;
-                if constexpr (ES == 2)
-                    *reinterpret_cast<bf16x4*>(dst + dim * 2) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
-                else
-                    *reinterpret_cast<f32x4*>(dst + dim * 4) = acc;
-            } else {
-                const int64_t at = static_cast<int64_t>(slot) * BM + rr;
-                if (dim == 0) {
-                    p.stat[2 * at] = top;
-                    p.stat[2 * at + 1] = sum;
-                }
-                *reinterpret_cast<f32x4*>(p.part + at * D + dim) = acc;
-            }
-        }
-    }
-    if constexpr (!PAGED) {
-        return;
-    } else {
-        g += took;
-        if (g >= gend) return;
-        while (g - base >= sq.units * sq.nt) {        // (stages are left, so there is a sequence with some)
-            base += sq.units * sq.nt;
-            sq = seq_shape<KT, BM>(p, ++s);
-        }
-        __syncthreads();                              // LDS is free again
-    }
     }
 }
 
-// Partial sums of the units that attention_kernel's blocks cut, in block order; the block whose share of stages holds
-// a cut unit's end joins it.
-template <typename T, int D, int KT, int BM>
+// Partial sums of the units that attention_kernel's blocks cut, in block order: a wave takes a row, its lanes the
+// parts' statistics, then D / 64 dims each (two for D = 32, half of the wave).
+template <typename T, int D, int BM>
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p) {
+    const CutUnit u = p.cuts[blockIdx.x];
     const int lane = threadIdx.x & 63;
-    const int all = all_stages<KT, BM>(p, lane), per = max(p.least, static_cast<int>((all + gridDim.x - 1) / gridDim.x));
-    if (blockIdx.x == 0 || static_cast<int64_t>(blockIdx.x) * per >= all) return;
-    const int g = blockIdx.x * per;
-    int s, base;
-    find_stage<KT, BM>(p, lane, g, s, base);
-    const SeqShape sq = seq_shape<KT, BM>(p, s);
-    const int unit = (g - base) / sq.nt, t0 = g - base - unit * sq.nt;
-    if (t0 == 0 || g - t0 + sq.nt > g + per) return;
-    const int first = (g - t0) / per, parts = blockIdx.x - first + 1;      // slot 2 first + 1, then 2 (first + i)
-    const int row_tiles = sq.units / p.kv_heads, kvh = unit / row_tiles, row0 = (unit - kvh * row_tiles) * BM;
-    const int nrow = min(BM, sq.rows * p.group - row0);
-    for (int i = threadIdx.x; i < nrow * (D / 4); i += 256) {
-        const int rr = i / (D / 4), dim = (i - rr * (D / 4)) * 4;
-        auto at = [&](int k) { return static_cast<int64_t>(2 * (first + k) + (k == 0)) * BM + rr; };
+    constexpr int PER = D >= 64 ? D / 64 + (D % 64 != 0) : 1, LANES = D / PER;      // dims a lane, lanes
+    typedef float fv __attribute__((ext_vector_type(PER)));
+    auto at = [&](int k) { return static_cast<int64_t>(2 * (u.first + k) + (k == 0)) * BM; };
+    if (u.parts == 0) return;
+    for (int rr = blockIdx.y * 4 + (threadIdx.x >> 6); rr < u.rows; rr += gridDim.y * 4) {
         float top = kNoMax, sum = 0.0f;
-        for (int k = 0; k < parts; ++k) top = fmaxf(top, p.stat[2 * at(k)]);
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < parts; ++k) {
-            const float f = __builtin_amdgcn_exp2f(p.stat[2 * at(k)] - top);
-            sum += p.stat[2 * at(k) + 1] * f;
-            acc += *reinterpret_cast<const f32x4*>(p.part + at(k) * D + dim) * f;
+        for (int k0 = 0; k0 < u.parts; k0 += 64)
+            top = fmaxf(top, k0 + lane < u.parts ? p.stat[2 * (at(k0 + lane) + rr)] : kNoMax);
+#pragma unroll
+        for (int i = 1; i < 64; i *= 2) top = fmaxf(top, __shfl_xor(top, i, 64));
+        float acc[PER] = {};
+        for (int k0 = 0; k0 < u.parts; k0 += 64) {
+            float f = 0.0f;                           // this lane's part: its weight
+            if (k0 + lane < u.parts) {
+                f = __builtin_amdgcn_exp2f(p.stat[2 * (at(k0 + lane) + rr)] - top);
+                sum += p.stat[2 * (at(k0 + lane) + rr) + 1] * f;
+            }
+            const int n = min(64, u.parts - k0);
+            for (int k = 0; k < n; k += 8) {
+                fv v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)           // (past the last part: that one again, with weight 0)
+                    if (lane < LANES) v[i] = *reinterpret_cast<const fv*>(p.part + (at(min(k0 + k + i, u.parts - 1)) + rr) * D + lane * PER);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float w = __shfl(f, min(k + i, 63), 64);
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) acc[e] += k + i < n ? v[i][e] * w : 0.0f;
+                }
+            }
         }
-        acc *= sum != 0.0f ? 1.0f / sum : 0.0f;
-        const int row = row0 + rr, tok = row / p.group, h = kvh * p.group + (row - tok * p.group);
-        unsigned char* dst = p.out + (sq.start + tok) * p.o_ts + h * p.o_hs;
-        if constexpr (sizeof(T) == 2)
-            *reinterpret_cast<bf16x4*>(dst + dim * 2) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
-        else
-            *reinterpret_cast<f32x4*>(dst + dim * 4) = acc;
+#pragma unroll
+        for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i, 64);
+        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+        const int row = u.row0 + rr, tok = row / p.group, h = u.kvh * p.group + (row - tok * p.group);
+        T* dst = reinterpret_cast<T*>(p.out + (u.start + tok) * p.o_ts + h * p.o_hs);
+        if (lane < LANES)
+#pragma unroll
+            for (int e = 0; e < PER; ++e) dst[lane * PER + e] = static_cast<T>(acc[e] * inv);
     }
 }
 
@@ -917,18 +913,25 @@ struct CachePlan {
     int64_t slots_bytes;
 };
 constexpr int kLeastStages = 2;
+// stages in the ring of a block of 64 to 256 rows: as many as 64 KB hold (128 KB of 256 rows), two to four
+constexpr int ring_of(int wr, int stage_bytes) {
+    const int room = (wr == 8 ? 128 : 64) * 1024 / stage_bytes;
+    return wr == 1 ? 2 : room >= 4 ? 4 : 2;
+}
 CachePlan cache_plan(const mopar_attention& a, int n_seq, int max_q, int max_len) {
     CachePlan c{};
-    const bool half = a.dtype == MOPAR_BF16;
     const int64_t rows = static_cast<int64_t>(max_q) * (a.heads / a.kv_heads);
-    c.bm = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
-    c.kt = c.bm == 32 ? (half ? 128 : 64) : c.bm == 64 ? 64 : half ? 64 : 32;
+    c.bm = rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+    c.kt = 32;
     c.row_tiles = static_cast<int>((rows + c.bm - 1) / c.bm);
+    // blocks that a CU holds at once, by LDS and two waves a SIMD
+    const int stage = 2 * c.kt * (a.head_dim > 64 ? 128 : a.head_dim) * static_cast<int>(dtype_size(a.dtype));
+    const int per_cu = std::min(256 / c.bm, 160 * 1024 / (ring_of(c.bm / 32, stage) * stage));
     const int64_t units = static_cast<int64_t>(n_seq) * a.kv_heads * c.row_tiles, nt = (max_len + c.kt - 1) / c.kt;
     c.split = nt > 2 * kLeastStages;
-    const int64_t blocks = c.split ? std::min<int64_t>(512, units * nt) : units;
+    const int64_t blocks = c.split ? std::min<int64_t>(256 * per_cu, units * nt) : units;
     c.blocks = static_cast<int>(std::min<int64_t>(blocks, int64_t(1) << 30));
-    c.slots_bytes = c.split ? int64_t(2) * c.blocks * c.bm * (a.head_dim + 2) * 4 : 0;
+    c.slots_bytes = c.split ? c.blocks * (int64_t(2) * c.bm * (a.head_dim + 2) * 4 + static_cast<int64_t>(sizeof(CutUnit))) : 0;
     return c;
 }
 
@@ -968,7 +971,7 @@ hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int
     const dim3 grid(static_cast<unsigned>(items * a.heads));
     return by_type(a.dtype, a.head_dim, [&](auto t, auto d) {
         using T = decltype(t);
-        launch_kernel((attention_kernel<T, d, 4, 1, 1, sizeof(T) == 2 ? 2 : 1, false>), grid, dim3(256), 0, s, p);
+        launch_kernel((attention_kernel<T, d, 4, sizeof(T) == 2 ? 2 : 1, 2, false>), grid, dim3(256), 0, s, p);
         return hipGetLastError();
     });
 }
@@ -1008,22 +1011,29 @@ hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c
     p.split = cp.split;
     p.least = kLeastStages;
     p.part = static_cast<float*>(ws);
-    if (cp.split) p.stat = p.part + int64_t(2) * cp.blocks * cp.bm * a.head_dim;
+    if (cp.split) {
+        p.stat = p.part + int64_t(2) * cp.blocks * cp.bm * a.head_dim;
+        p.cuts = reinterpret_cast<CutUnit*>(p.stat + int64_t(2) * cp.blocks * cp.bm * 2);
+    }
     const dim3 grid(static_cast<unsigned>(cp.blocks));
     return by_type(a.dtype, a.head_dim, [&](auto t, auto d) {
         using T = decltype(t);
-        constexpr bool H = sizeof(T) == 2;
         auto go = [&](auto kernel, auto join, int threads) {
             launch_kernel(kernel, grid, dim3(threads), 0, s, p);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess || !cp.split) return e;
-            launch_kernel(join, grid, dim3(256), 0, s, p);
+            launch_kernel(join, dim3(grid.x, cp.bm / 16), dim3(256), 0, s, p);
             return hipGetLastError();
         };
-        if (cp.bm == 32)
-            return go(attention_kernel<T, d, 1, H ? 4 : 2, 1, 1, true>, attention_join_kernel<T, d, H ? 128 : 64, 32>, H ? 256 : 128);
-        if (cp.bm == 64) return go(attention_kernel<T, d, 2, 2, 1, 1, true>, attention_join_kernel<T, d, 64, 64>, 256);
-        return go(attention_kernel<T, d, 4, 1, 1, H ? 2 : 1, true>, attention_join_kernel<T, d, H ? 64 : 32, 128>, 256);
+        constexpr int STAGE = 2 * 32 * Geo<T, d>::RB;
+        auto of = [&](auto wr) {
+            constexpr int WR = wr;
+            return go(attention_kernel<T, d, WR, 1, ring_of(WR, STAGE), true>, attention_join_kernel<T, d, WR * 32>, WR * 64);
+        };
+        if (cp.bm == 32) return of(std::integral_constant<int, 1>{});
+        if (cp.bm == 64) return of(std::integral_constant<int, 2>{});
+        if (cp.bm == 128) return of(std::integral_constant<int, 4>{});
+        return of(std::integral_constant<int, 8>{});
     });
 }
 
