@@ -140,6 +140,11 @@ template <int O0, int O1, int O2, int O3> __device__ __forceinline__ void lds_re
                  : "memory");
     v = u32x4{w0, w1, w2, w3};
 }
+__device__ __forceinline__ unsigned lds_read_word(unsigned a) {
+    unsigned v;
+    asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(a) : "memory");
+    return v;
+}
 template <int OFF> __device__ __forceinline__ u32x4 lds_start16(unsigned addr) {
     static_assert(OFF >= 0 && OFF < 65536, "ds offset");
     u32x4 v;
@@ -291,8 +296,11 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
     constexpr bool OWN = WR == 1;
     static_assert(TILE % 1024 == 0 && NBLK <= 64 && NS >= 2 && (NS & (NS - 1)) == 0, "stages");
     static_assert(PAGED || NS == 2, "the loop over prompts knows its two stages at compile time");
-    static_assert((NS - 1) * 2 * LPW <= 63, "vmcnt range");
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * NS * TILE];
+    static_assert((NS - 1) * (2 * LPW + 1) <= 63, "vmcnt range");
+    constexpr int AHEAD = OWN ? NS : NS - 1;         // stages on their way when one is begun
+    constexpr int RING = 2 * NS * TILE;              // then, over a cache, each wave's pages of four stages
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[RING + (PAGED ? WR * 1024 : 0)];
+    static_assert(AHEAD <= 3, "places for the pages");
 
     const int lane = threadIdx.x & 63, wave = OWN ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lr = lane & 31, lh = lane >> 5;
@@ -386,15 +394,20 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         auto page_at = [&](unsigned page, int key) __attribute__((always_inline)) {    // byte offset of a key's row
             return static_cast<int64_t>(page) * page_bytes + (key & page_mask) * (D * ES);
         };
-        // The pages of a stage's blocks, one a lane, are read a stage before its loads go out.  From the first absent
-        // one on (bad_from), keys are looked at one by one.
+        // The pages of a stage's blocks, one a lane.  They go to LDS as the keys do, AHEAD stages before the stage's own
+        // loads: a plain load carried round the loop would make the compiler wait for every load in flight.  From the
+        // first absent page on (bad_from), keys are looked at one by one.
         int bad_from = small ? key0 : 0x7fffffff;
-        auto pages_of = [&](int k0) __attribute__((always_inline)) -> int {
+        auto page_of = [&](int k0) __attribute__((always_inline)) {    // (lanes past the stage or the keys: the last key's)
+            return pages + (min(k0 + min(lane, NBLK - 1) * RPB, key1 - 1) >> p.shift);
+        };
+        auto send_pages = [&](int k0) __attribute__((always_inline)) {
+            if constexpr (PAGED)
+                __builtin_amdgcn_global_load_lds((gptr_t)page_of(k0), (lds_ptr_t)(lds + RING + wave * 1024 + (k0 / KT & 3) * 256), 4, 0, 0);
+        };
+        auto sent_pages = [&](int k0) __attribute__((always_inline)) -> int {
             if constexpr (!PAGED) return 0;
-            const int key = k0 + lane * RPB;
-            int page = 0;
-            if (lane < NBLK && key < key1 && !small) page = pages[key >> p.shift];
-            return page;
+            return lds_read_word(static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_ptr_t)lds)) + RING + wave * 1024 + (k0 / KT & 3) * 256 + lane * 4);
         };
         auto look_at = [&](int pgs, int k0) __attribute__((always_inline)) {
             if constexpr (PAGED)
@@ -696,30 +709,34 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         // stages that every row of the block sees whole come first
         const int seen = PAGED ? min(past, key1) : row0 + 1;
         const int full_end = seen > key0 ? key0 + (seen - key0) / KT * KT : key0;
-        constexpr int AHEAD = OWN ? NS : NS - 1;      // stages on their way when one is begun
-        int k0 = key0, at = 0, pgs = 0;               // the stage at hand, its place, the pages of stage k0 + AHEAD KT
+        int k0 = key0, at = 0;                        // the stage at hand and its place
         if (key0 < key1) {
             int first[AHEAD];
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) first[i] = pages_of(key0 + i * KT);
-            pgs = pages_of(key0 + AHEAD * KT);
+            for (int i = 0; i < AHEAD; ++i) first[i] = PAGED ? *page_of(key0 + i * KT) : 0;
+            // the queries are waited for here, or the compiler would do it, for every load in flight, in the loop
+#pragma unroll
+            for (int i = 0; i < CH / 2; ++i) pin(qf[i]);
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
                 look_at(first[i], key0 + i * KT);
+                send_pages(key0 + (i + AHEAD) * KT);
                 if (key0 + i * KT < key1) issue(key0 + i * KT, i, first[i]);
             }
         }
-        // stage k0 + AHEAD KT to its place, and the pages of the one after it
+        // stage k0 + AHEAD KT to its place; its pages were sent before the loads of stage k0, which are done
         auto ahead = [&]() __attribute__((always_inline)) {
-            const int now = pgs;
-            pgs = pages_of(k0 + (AHEAD + 1) * KT);
-            look_at(now, k0 + AHEAD * KT);
-            if (k0 + AHEAD * KT < key1) issue(k0 + AHEAD * KT, (at + AHEAD) & (NS - 1), now);
+            const int now = sent_pages(k0 + AHEAD * KT);
+            send_pages(k0 + 2 * AHEAD * KT);
+            if (k0 + AHEAD * KT < key1) {
+                look_at(now, k0 + AHEAD * KT);
+                issue(k0 + AHEAD * KT, (at + AHEAD) & (NS - 1), now);
+            }
         };
         // the stage at hand has arrived once only the loads of the AHEAD - 1 after it (or later ones) are on their way
         auto begin = [&]() __attribute__((always_inline)) {
             if (AHEAD > 1 && k0 + (AHEAD - 1) * KT < key1)
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NBLK % WR == 0 ? (AHEAD - 1) * 2 * LPW : 0) : "memory");
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NBLK % WR == 0 ? (AHEAD - 1) * (2 * LPW + PAGED) : 0) : "memory");
             else
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             if constexpr (!OWN) {
@@ -926,7 +943,7 @@ CachePlan cache_plan(const mopar_attention& a, int n_seq, int max_q, int max_len
     c.row_tiles = static_cast<int>((rows + c.bm - 1) / c.bm);
     // blocks that a CU holds at once, by LDS and two waves a SIMD
     const int stage = 2 * c.kt * (a.head_dim > 64 ? 128 : a.head_dim) * static_cast<int>(dtype_size(a.dtype));
-    const int per_cu = std::min(256 / c.bm, 160 * 1024 / (ring_of(c.bm / 32, stage) * stage));
+    const int per_cu = std::min(256 / c.bm, 160 * 1024 / (ring_of(c.bm / 32, stage) * stage + c.bm / 32 * 1024));
     const int64_t units = static_cast<int64_t>(n_seq) * a.kv_heads * c.row_tiles, nt = (max_len + c.kt - 1) / c.kt;
     c.split = nt > 2 * kLeastStages;
     const int64_t blocks = c.split ? std::min<int64_t>(256 * per_cu, units * nt) : units;
