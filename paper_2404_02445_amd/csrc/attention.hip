@@ -193,10 +193,18 @@ __device__ __forceinline__ void rows_of(const AttnParams& p, int s, int64_t& sta
     rows = static_cast<int>(min(max(hi - lo, int64_t(0)), static_cast<int64_t>(p.max_rows)));
 }
 
+// the same in every lane: kept in scalar registers, and branches on it are scalar ones (a resource in vector registers
+// would cost a loop over the lanes at each load)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    return static_cast<int64_t>(static_cast<uint64_t>(static_cast<unsigned>(uniform(static_cast<int>(v >> 32)))) << 32 |
+                                static_cast<unsigned>(uniform(static_cast<int>(v))));
+}
+
 __device__ __forceinline__ int wave_sum(int v) {
 #pragma unroll
     for (int i = 1; i < 64; i *= 2) v += __shfl_xor(v, i, 64);
-    return v;
+    return uniform(v);
 }
 
 // A sequence over the cache: its drafted rows, tokens before them and in all, and its work -- a unit is a tile of BM
@@ -214,6 +222,14 @@ template <int KT, int BM> __device__ __forceinline__ SeqShape seq_shape(const At
     q.units = (q.rows * p.group + BM - 1) / BM * p.kv_heads;
     return q;
 }
+// ... of a sequence that every lane asks for
+template <int KT, int BM> __device__ __forceinline__ SeqShape seq_shape_of_block(const AttnParams& p, int s) {
+    SeqShape q = seq_shape<KT, BM>(p, uniform(s));
+    q.start = uniform(q.start);
+    q.rows = uniform(q.rows), q.past = uniform(q.past), q.total = uniform(q.total), q.nt = uniform(q.nt), q.units = uniform(q.units);
+    return q;
+}
+
 // All sequences' stages, one sequence after the other and in it one unit after the other, cut into equal shares for
 // the blocks of a grid: this block's share [g, gend), the sequence that it starts in and that one's first stage.
 // False: no share.
@@ -228,7 +244,6 @@ template <int KT, int BM> __device__ __forceinline__ bool take_share(const AttnP
     const int head = stages(lane);                     // the first 64 sequences are looked up once
     int all = wave_sum(head);
     for (int s0 = 64; s0 < p.n_seq; s0 += 64) all += wave_sum(stages(s0 + lane));
-    all = __builtin_amdgcn_readfirstlane(all);         // (what follows is the same in every lane: scalar registers)
     sh.per = max(p.least, static_cast<int>((all + gridDim.x - 1) / gridDim.x));
     if (static_cast<int64_t>(blockIdx.x) * sh.per >= all) return false;
     sh.g = blockIdx.x * sh.per;
@@ -321,11 +336,11 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             gend = sh.gend;
             s = sh.s;
             base = sh.base;
-            sq = seq_shape<KT, BM>(p, s);
+            sq = seq_shape_of_block<KT, BM>(p, s);
         } else {
             const int units = p.kv_heads * p.row_tiles;
             s = blockIdx.x / units;
-            sq = seq_shape<KT, BM>(p, s);
+            sq = seq_shape_of_block<KT, BM>(p, s);
             const int unit = blockIdx.x - s * units;
             if (unit >= sq.units) return;
             g = unit * sq.nt;
@@ -360,7 +375,11 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             kvh = hi - gi * p.kv_heads;
             head = kvh * p.group + gi;
             if (!pick_tile<BM>(p, blockIdx.x / p.heads, lane, s, tile)) return;
+            s = uniform(s);
+            tile = uniform(tile);
             rows_of(p, s, start, rows);
+            start = uniform(start);
+            rows = uniform(rows);
             total = rows;
             key1 = min(total, (tile + 1) * BM);
         }
@@ -847,7 +866,7 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             if (g >= gend) return;
             while (g - base >= sq.units * sq.nt) {    // (stages are left, so there is a sequence with some)
                 base += sq.units * sq.nt;
-                sq = seq_shape<KT, BM>(p, ++s);
+                sq = seq_shape_of_block<KT, BM>(p, ++s);
             }
             if constexpr (!OWN) __syncthreads();      // every wave is done with the ring
         }
