@@ -520,9 +520,21 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         };
 
         bool marred = false;                          // infinities or NaN among the values were left out
-        // one 32-key tile of the stage at place `at`; `cut`: some row may not see some key
-        auto tile32 = [&](int at, auto sub, int k0, auto cut) __attribute__((always_inline)) {
-            const int st0 = at * TILE;
+        int looked_at = key1;                         // keys from here on may have been looked at one by one
+        // The maximum in use may lag by up to 8 (weights stay below 2^8), so that rescaling is rare.
+        auto keep_max = [&](float mx) __attribute__((always_inline)) {
+            if (__any(mx > m + 8.0f)) {
+                const float mn = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] *= f;
+            }
+        };
+        // one 32-key tile, st0 bytes into the ring; `cut`: some row may not see some key
+        auto tile32 = [&](int st0, int k0, bool cut) __attribute__((always_inline)) {
             f32x16 sc;
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
@@ -532,7 +544,7 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
                 unsigned a[KG];
 #pragma unroll
                 for (int e = 0; e < KG; ++e) a[e] = (ka + st0) ^ ((gr * KG + e) << 5);
-                lds_read16<KG, sub * 32 * RB>(kf, a);
+                lds_read16<KG, 0>(kf, a);
 #pragma unroll
                 for (int e = 0; e < KG; ++e) {
                     if constexpr (ES == 2)
@@ -544,7 +556,8 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
                             sc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e][c]), __uint_as_float(qf[gr * KG + e][c]), sc, 0, 0, 0);
                 }
             });
-            if constexpr (cut) {
+            if (cut) {
+                looked_at = min(looked_at, k0);
                 uint64_t vis = visible(k0);
                 if constexpr (PAGED)
                     if (k0 + 32 > bad_from) {         // keys of absent pages
@@ -558,18 +571,13 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             }
             float mx = sc[0];
 #pragma unroll
-            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+            for (int i = 1; i < 15; i += 2) mx = fmaxf(fmaxf(mx, sc[i]), sc[i + 1]);
+            mx = fmaxf(mx, sc[15]);
             mx = fmaxf(mx, other_half(mx)) * p.c;
-            const float mn = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - mn);
-            m = mn;
-            l *= f;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+            keep_max(mx);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                sc[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], p.c, -mn));
+                sc[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], p.c, -m));
                 l += sc[i];
             }
             // O^T += V^T P^T
@@ -582,12 +590,12 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
                 u32x4 vf[DT];
                 static_for<DT>([&](auto d) __attribute__((always_inline)) {
                     if constexpr (ES == 2) {
-                        constexpr int R0 = (sub * 32 + u * 16) * RB;
+                        constexpr int R0 = u * 16 * RB;
                         u32x2 lo, hi;
                         lds_read_tr<R0, R0 + 8 * RB>(lo, hi, (va + st0) ^ (d << 6), (va + st0) ^ ((d << 6) | (swizzle<RS>(8) << 4)));
                         vf[d] = u32x4{lo[0], lo[1], hi[0], hi[1]};
                     } else {
-                        constexpr int R0 = sub * 32 + 8 * u;
+                        constexpr int R0 = 8 * u;
                         unsigned a[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) a[e] = (va + st0) ^ ((d << 7) ^ (swizzle<RS>(8 * u + e) << 4));
@@ -596,7 +604,7 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
                 });
                 // Where a row does not see every key, an infinity or NaN among the values must not meet its zero weight:
                 // it is left out here and added where it is seen at the end.
-                if constexpr (cut) {
+                if (cut) {
                     unsigned bad = 0;
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
@@ -682,16 +690,7 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
 #pragma unroll
                 for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, sc[t][i]), sc[t][i + 1]);
             mx = fmaxf(mx, other_half(mx)) * p.c;
-            // The maximum in use may lag by up to 8 (weights stay below 2^8): rescaling is rare.
-            if (__any(mx > m + 8.0f)) {
-                const float mn = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - mn);
-                m = mn;
-                l *= f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= f;
-            }
+            keep_max(mx);
             float sum[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int t = 0; t < SUBS; ++t)
@@ -723,11 +722,10 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         };
 
         // --- the keys ----------------------------------------------------------------------------------
-        // keys past the last that this wave's rows see (causal): nothing to do
-        const int wave_end = PAGED ? (row0 + wave * 32 < nrow ? key1 : key0) : min(key1, row0 + (wave + 1) * 32);
-        // stages that every row of the block sees whole come first
-        const int seen = PAGED ? min(past, key1) : row0 + 1;
-        const int full_end = seen > key0 ? key0 + (seen - key0) / KT * KT : key0;
+        // Of this wave's rows: the keys that all of them see, and the end of those that any sees.
+        const int wave0 = row0 + wave * 32;
+        const int all_see = PAGED ? past : wave0 + 1;
+        const int wave_end = PAGED ? (wave0 < nrow ? key1 : key0) : min(key1, wave0 + 32);
         int k0 = key0, at = 0;                        // the stage at hand and its place
         if (key0 < key1) {
             int first[AHEAD];
@@ -769,35 +767,32 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             k0 += KT;
             at = (at + 1) & (NS - 1);
         };
-        if constexpr (!PAGED && ES == 2) {
-            while (k0 < full_end) {
-                begin();
-                full(std::integral_constant<int, 0>{});
-                end();
-                if (k0 >= full_end) break;
-                begin();
-                full(std::integral_constant<int, 1>{});
-                end();
-            }
-        } else {
-            while (k0 < full_end && k0 + KT <= bad_from) {
-                begin();
-                if constexpr (ES == 2) {
-                    if (OWN || k0 < wave_end) full(at);
-                } else {
-                    static_for<SUBS>([&](auto sub) __attribute__((always_inline)) {
-                        if (OWN || k0 < wave_end) tile32(at, sub, k0 + sub * 32, std::false_type{});
-                    });
+        // stages that every row of the block sees whole, then (from an absent page on at the latest) the others
+        if constexpr (ES == 2) {
+            const int seen = PAGED ? min(past, key1) : row0 + 1;
+            const int full_end = key0 + max(seen - key0, 0) / KT * KT;
+            if constexpr (!PAGED) {
+                while (k0 < full_end) {
+                    begin();
+                    full(std::integral_constant<int, 0>{});
+                    end();
+                    if (k0 >= full_end) break;
+                    begin();
+                    full(std::integral_constant<int, 1>{});
+                    end();
                 }
-                end();
+            } else {
+                while (k0 < full_end && k0 + KT <= bad_from) {
+                    begin();
+                    if (OWN || k0 < wave_end) full(at);
+                    end();
+                }
             }
         }
-        const int looked_at = k0;                     // keys from here on: one by one
         while (k0 < key1) {
             begin();
-            static_for<SUBS>([&](auto sub) __attribute__((always_inline)) {
-                if (k0 + sub * 32 < wave_end) tile32(at, sub, k0 + sub * 32, std::true_type{});
-            });
+            for (int k = k0; k < min(k0 + KT, wave_end); k += 32)
+                tile32(at * TILE + (k - k0) * RB, k, k + 32 > min(min(all_see, key1), bad_from));
             end();
         }
 
@@ -958,7 +953,7 @@ CachePlan cache_plan(const mopar_attention& a, int n_seq, int max_q, int max_len
     CachePlan c{};
     const int64_t rows = static_cast<int64_t>(max_q) * (a.heads / a.kv_heads);
     c.bm = rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-    c.kt = 32;
+    c.kt = a.dtype == MOPAR_BF16 && c.bm >= 128 ? 64 : 32;
     c.row_tiles = static_cast<int>((rows + c.bm - 1) / c.bm);
     // blocks that a CU holds at once, by LDS and two waves a SIMD
     const int stage = 2 * c.kt * (a.head_dim > 64 ? 128 : a.head_dim) * static_cast<int>(dtype_size(a.dtype));
@@ -1061,10 +1056,9 @@ hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c
             launch_kernel(join, dim3(grid.x, cp.bm / 16), dim3(256), 0, s, p);
             return hipGetLastError();
         };
-        constexpr int STAGE = 2 * 32 * Geo<T, d>::RB;
-        auto of = [&](auto wr) {
-            constexpr int WR = wr;
-            return go(attention_kernel<T, d, WR, 1, ring_of(WR, STAGE), true>, attention_join_kernel<T, d, WR * 32>, WR * 64);
+                auto of = [&](auto wr) {
+            constexpr int WR = wr, SUBS = sizeof(T) == 2 && WR >= 4 ? 2 : 1, STAGE = 2 * 32 * SUBS * Geo<T, d>::RB;
+            return go(attention_kernel<T, d, WR, SUBS, ring_of(WR, STAGE), true>, attention_join_kernel<T, d, WR * 32>, WR * 64);
         };
         if (cp.bm == 32) return of(std::integral_constant<int, 1>{});
         if (cp.bm == 64) return of(std::integral_constant<int, 2>{});
