@@ -511,10 +511,14 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             uint64_t bits;
             if (j0 >= 0) {
                 const int w = j0 >> 6, sh = j0 & 63;
-                const uint64_t lo = w < words ? mrow[w] : 0, hi = w + 1 < words ? mrow[w + 1] : 0;
+                uint64_t lo = w < words ? mrow[w] : 0, hi = w + 1 < words ? mrow[w + 1] : 0;
+                pin(lo);                              // (waited for here on every path, and so nowhere in the loop)
+                pin(hi);
                 bits = (sh ? (lo >> sh) | (hi << (64 - sh)) : lo) & ones(own - j0);
             } else {
-                bits = ones(-j0) | (-j0 < 64 ? (mrow[0] & ones(own)) << -j0 : 0);
+                uint64_t lo = mrow[0];
+                pin(lo);
+                bits = ones(-j0) | (-j0 < 64 ? (lo & ones(own)) << -j0 : 0);
             }
             return bits & ones(key1 - k0);
         };
@@ -562,7 +566,8 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
                 if constexpr (PAGED)
                     if (k0 + 32 > bad_from) {         // keys of absent pages
                         const int key = k0 + lane;
-                        const unsigned page = lane < 32 && key < key1 ? pages[key >> p.shift] : ~0u;
+                        unsigned page = lane < 32 && key < key1 ? pages[key >> p.shift] : ~0u;
+                        pin(page);
                         vis &= __ballot(page < static_cast<unsigned>(p.pages));
                     }
 #pragma unroll
@@ -727,13 +732,13 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         const int all_see = PAGED ? past : wave0 + 1;
         const int wave_end = PAGED ? (wave0 < nrow ? key1 : key0) : min(key1, wave0 + 32);
         int k0 = key0, at = 0;                        // the stage at hand and its place
+        int first[AHEAD];                             // pages of the first stages
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) first[i] = PAGED && key0 < key1 ? *page_of(key0 + i * KT) : 0;
+        // the queries are waited for here, or the compiler would do it, for every load in flight, in the loop
+#pragma unroll
+        for (int i = 0; i < CH / 2; ++i) pin(qf[i]);
         if (key0 < key1) {
-            int first[AHEAD];
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) first[i] = PAGED ? *page_of(key0 + i * KT) : 0;
-            // the queries are waited for here, or the compiler would do it, for every load in flight, in the loop
-#pragma unroll
-            for (int i = 0; i < CH / 2; ++i) pin(qf[i]);
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
                 look_at(first[i], key0 + i * KT);
