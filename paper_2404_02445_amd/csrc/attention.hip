@@ -897,13 +897,13 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p)
                 sum += p.stat[2 * (at(k0 + lane) + rr) + 1] * f;
             }
             const int n = min(64, u.parts - k0);
-            for (int k = 0; k < n; k += 8) {
-                fv v[8];
+            for (int k = 0; k < n; k += 16) {
+                fv v[16];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)           // (past the last part: that one again, with weight 0)
+                for (int i = 0; i < 16; ++i)           // (past the last part: that one again, with weight 0)
                     if (lane < LANES) v[i] = *reinterpret_cast<const fv*>(p.part + (at(min(k0 + k + i, u.parts - 1)) + rr) * D + lane * PER);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < 16; ++i) {
                     const float w = __shfl(f, min(k + i, 63), 64);
 #pragma unroll
                     for (int e = 0; e < PER; ++e) acc[e] += k + i < n ? v[i][e] * w : 0.0f;

@@ -8,7 +8,6 @@ and raise ``ValueError``; the library's own refusals raise ``MoparError``.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 
 import torch
@@ -26,16 +25,24 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _on(device, stream):
-    """The stream's handle, and a context in which the device is the current one."""
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)    # (torch's own handle lookup without a Stream object)
+
+
+def _call(fn, device, stream, *args):
+    """The entry point with the stream's handle as its last argument, the tensors' device being the current one."""
     _need(device.type == "cuda", "the tensors must be on a GPU")
-    same = device.index is None or device.index == torch.cuda.current_device()
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
+    now = torch.cuda.current_device()
+    index = now if device.index is None else device.index
+    if stream is not None:
+        _need(stream.device.index == index, "the stream is on another device than the tensors")
+        handle = stream.cuda_stream
     else:
-        _need(stream.device.index == (torch.cuda.current_device() if device.index is None else device.index),
-              "the stream is on another device than the tensors")
-    return contextlib.nullcontext() if same else torch.cuda.device(device), stream.cuda_stream
+        handle = _raw_stream(index) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
+    if index == now:
+        check(fn(*args, handle))
+    else:
+        with torch.cuda.device(index):
+            check(fn(*args, handle))
 
 
 def _dtype(t):
@@ -45,15 +52,21 @@ def _dtype(t):
 
 def _rows(t, name, like, shape=None):
     """A mopar_rows of t; `like` is the tensor whose device and dtype it shares."""
-    _need(t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] == 1), f"{name}: [tokens, heads, head_dim] with contiguous dims")
-    _need(t.device == like.device and t.dtype == like.dtype, f"{name}: device or dtype differs")
-    _need(shape is None or tuple(t.shape) == tuple(shape), f"{name}: shape must be {tuple(shape or ())}")
-    return L.Rows(t.data_ptr(), t.stride(0), t.stride(1))
+    st = t.stride()
+    if len(st) != 3 or (st[2] != 1 and t.shape[2] != 1):
+        raise ValueError(f"{name}: [tokens, heads, head_dim] with contiguous dims")
+    if t is not like and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name}: device or dtype differs")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: shape must be {tuple(shape)}")
+    return L.Rows(t.data_ptr(), st[0], st[1])
 
 
 def _ints(t, name, like, n, dtype=torch.int32):
-    _need(t.dtype == dtype and t.device == like.device and t.is_contiguous(), f"{name}: a contiguous {dtype} tensor on the same device")
-    _need(t.numel() == n, f"{name}: {n} entries expected")
+    if t.dtype != dtype or not t.is_contiguous() or t.device != like.device:
+        raise ValueError(f"{name}: a contiguous {dtype} tensor on the same device")
+    if t.numel() != n:
+        raise ValueError(f"{name}: {n} entries expected")
     return t.data_ptr()
 
 
@@ -71,7 +84,7 @@ class Rotary:
 
     def __del__(self):
         h = getattr(self, "handle", None)
-        if h is not None and h.value and L._lib is not None:
+        if h is not None and h.value and L is not None and L._lib is not None:
             L._lib.mopar_rotary_destroy(h)
             self.handle = None
 
@@ -109,11 +122,10 @@ def _single(cache):
 def mopar_rotary_apply(rotary, x, y, pos, stream=None):
     """y = x with every head turned to its row's position."""
     rx, ry = _rows(x, "x", x), _rows(y, "y", x, x.shape)
-    _need(x.shape[2] == rotary.head_dim, "x: head_dim is not the rotary's")
-    p = _ints(pos, "pos", x, x.shape[0])
-    ctx, st = _on(x.device, stream)
-    with ctx:
-        check(lib().mopar_rotary_apply(rotary.handle, _dtype(x), x.shape[0], x.shape[1], p, ctypes.byref(rx), ctypes.byref(ry), st))
+    t, heads, d = x.shape
+    _need(d == rotary.head_dim, "x: head_dim is not the rotary's")
+    p = _ints(pos, "pos", x, t)
+    _call(lib().mopar_rotary_apply, x.device, stream, rotary.handle, _dtype(x), t, heads, p, rx, ry)
     return y
 
 
@@ -135,11 +147,8 @@ def mopar_cache_append(cache, k, v, seq, slot, rotary=None, pos=None, q=None, q_
         _need(pos is None and q is None and q_out is None, "pos, q and q_out go with a rotary")
     ps = None if pos is None else _ints(pos, "pos", cache.k, t)
     sq, sl = _ints(seq, "seq", cache.k, t), _ints(slot, "slot", cache.k, t)
-    ctx, st = _on(cache.k.device, stream)
-    with ctx:
-        check(lib().mopar_cache_append(ctypes.byref(c), None if rotary is None else rotary.handle, t, heads, ps, sq, sl,
-                                       None if rq is None else ctypes.byref(rq), None if ro is None else ctypes.byref(ro),
-                                       ctypes.byref(rk), ctypes.byref(rv), st))
+    _call(lib().mopar_cache_append, cache.k.device, stream, c, None if rotary is None else rotary.handle, t, heads, ps, sq, sl, rq, ro,
+          rk, rv)
 
 
 def mopar_cache_keep(cache, lens, path_offsets, path, max_path, stream=None):
@@ -147,9 +156,7 @@ def mopar_cache_keep(cache, lens, path_offsets, path, max_path, stream=None):
     c = cache.raw
     ln, po = _ints(lens, "lens", cache.k, c.n_seq), _ints(path_offsets, "path_offsets", cache.k, c.n_seq + 1)
     pa = _ints(path, "path", cache.k, path.numel())
-    ctx, st = _on(cache.k.device, stream)
-    with ctx:
-        check(lib().mopar_cache_keep(ctypes.byref(c), cache.layers, cache.layer_stride, ln, po, path.numel(), pa, max_path, st))
+    _call(lib().mopar_cache_keep, cache.k.device, stream, c, cache.layers, cache.layer_stride, ln, po, path.numel(), pa, max_path)
 
 
 def _attention(q, kv_heads, scale):
@@ -166,10 +173,7 @@ def mopar_attention_prompt(q, k, v, out, offsets, max_len, scale=None, stream=No
     off = _ints(offsets, "offsets", q, offsets.numel())
     _need(offsets.numel() >= 1, "offsets: one more than sequences")
     a = _attention(q, k.shape[1], scale)
-    ctx, st = _on(q.device, stream)
-    with ctx:
-        check(lib().mopar_attention_prompt(ctypes.byref(a), t, offsets.numel() - 1, off, max_len, ctypes.byref(rq), ctypes.byref(rk),
-                                           ctypes.byref(rv), ctypes.byref(ro), st))
+    _call(lib().mopar_attention_prompt, q.device, stream, a, t, offsets.numel() - 1, off, max_len, rq, rk, rv, ro)
     return out
 
 
@@ -202,9 +206,6 @@ def mopar_attention_cache(q, out, cache, offsets, max_q, lens, max_len, mask=Non
     a = _attention(q, c.kv_heads, scale)
     if ws is not None:
         _need(ws.device == q.device and ws.is_contiguous(), "ws: a contiguous tensor on the same device")
-    ctx, st = _on(q.device, stream)
-    with ctx:
-        check(lib().mopar_attention_cache(ctypes.byref(a), ctypes.byref(c), q.shape[0], off, max_q, ln, max_len, mk, words, ctypes.byref(rq),
-                                          ctypes.byref(ro), None if ws is None else ws.data_ptr(),
-                                          0 if ws is None else ws.numel() * ws.element_size(), st))
+    _call(lib().mopar_attention_cache, q.device, stream, a, c, q.shape[0], off, max_q, ln, max_len, mk, words, rq, ro,
+          None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes)
     return out
