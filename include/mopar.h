@@ -343,10 +343,16 @@ typedef enum {
     MOPAR_OP_EMBED = 8,      /* ids (B,S) -> table[id]; w: table [V][F].  For both embeddings an
                                 id outside [0, V) is clamped to the nearest row (no error, no
                                 access past the table); V < 2^31                                 */
-    MOPAR_OP_LSTM = 9        /* in0 (B,T,E) -> out (B,T,H) hidden sequence, h0 = c0 = 0;
+    MOPAR_OP_LSTM = 9,       /* in0 (B,T,E) -> out (B,T,H) hidden sequence, h0 = c0 = 0;
                                 w: W_ih [4H][E], w2: W_hh [4H][H], b: b_ih [4H], w3: b_hh [4H];
                                 rows interleaved by unit: row 4u+g holds gate g (i,f,g,o) of
                                 hidden unit u.  c is kept in float32.                              */
+    MOPAR_OP_ROTARY = 10,    /* in0 (B,S,F) -> out (B,S,F), rows of F / rotary.head_dim heads: the first
+                                `heads` heads turned to the token's position in its sequence
+                                (0 .. S-1), the others as they are; see mopar_rotary_desc           */
+    MOPAR_OP_CAUSAL_ATTENTION = 11 /* in0 (B,S,(heads + 2 kv_heads) head_dim) = [Q|K|V] -> out
+                                (B,S,heads head_dim): mopar_attention_prompt over the B sequences;
+                                heads; kv_heads (divides heads); head_dim 32, 64, 96 or 128; scale */
 } mopar_op_kind;
 
 typedef enum { MOPAR_ACT_NONE = 0, MOPAR_ACT_RELU = 1, MOPAR_ACT_GELU = 2 } mopar_act;
@@ -374,6 +380,8 @@ typedef struct {
     float scale;
     int64_t rows[3];            /* table rows: EMBED_BERT vocab, positions, token types; EMBED vocab */
     int64_t w, b, w2, w3, w4, w5;
+    int32_t kv_heads, head_dim; /* causal attention */
+    mopar_rotary_desc rotary;   /* rotary           */
 } mopar_op;
 
 typedef struct {
@@ -405,7 +413,7 @@ void mopar_model_destroy(mopar_model_t model);
 /* Layer profiles (Eq. 1-4) of the model: op memory = bytes of parameters +
  * inputs + output; op time = max(FLOP / peak, bytes / 8e12), peak 2.5e15
  * (bf16) or 157.3e12 (f32) FLOP/s; FLOP counted for conv, linear, attention
- * and LSTM.  out_bytes of node j < n_layers - 1 is the size of every tensor
+ * (causal: the visible pairs) and LSTM.  out_bytes of node j < n_layers - 1 is the size of every tensor
  * crossing the cut after it (mopar_model_cut_tensors), of the last node its
  * output.  `out` has n_layers entries. */
 int mopar_model_profile(mopar_model_t model, mopar_layer_profile* out);

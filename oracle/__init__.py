@@ -154,6 +154,51 @@ def attention(qkv, heads, scale, rnd="none"):
     return y
 
 
+def rotary_angles(r, base=10000.0, scaling="none", factor=1.0, context=0.0, beta_slow=0.0, beta_fast=0.0):
+    """Angle per position of each of the r / 2 pairs (rotary positions, scaled as named; float64)."""
+    j = np.arange(r // 2, dtype=np.float64)
+    if scaling == "ntk":
+        base = base * factor ** (r / (r - 2))
+    w = base ** (-2.0 * j / r)
+    if scaling == "linear":
+        w = w / factor
+    if scaling == "yarn":
+        slow, fast = (1.0, 32.0) if beta_slow == 0 and beta_fast == 0 else (beta_slow, beta_fast)
+        g = np.clip((context * w / (2 * np.pi) - slow) / (fast - slow), 0.0, 1.0)
+        w = w * (g + (1 - g) / factor)
+    return w
+
+
+def rotary(x, heads, head_dim, rot_dim=None, layout="half", mscale=0.0, rnd="none", **scaling):
+    """x [B, S, F], rows of F / head_dim heads: the first `heads` turned to their position in the sequence."""
+    x = _d(x)
+    b, s, f = x.shape
+    r = head_dim if rot_dim is None else rot_dim
+    m = mscale or (0.1 * np.log(scaling["factor"]) + 1.0 if scaling.get("scaling") == "yarn" else 1.0)
+    z = np.exp(1j * np.arange(s)[:, None] * rotary_angles(r, **scaling)[None]) * m          # [S, r / 2]
+    y = x.reshape(b, s, f // head_dim, head_dim).copy()
+    lo, hi = (slice(0, r // 2), slice(r // 2, r)) if layout == "half" else (slice(0, r, 2), slice(1, r, 2))
+    t = (y[:, :, :heads, lo] + 1j * y[:, :, :heads, hi]) * z[None, :, None]
+    y[:, :, :heads, lo], y[:, :, :heads, hi] = t.real, t.imag
+    return round_to(y.reshape(b, s, f), rnd)
+
+
+def causal_attention(qkv, heads, kv_heads, head_dim, scale, rnd="none"):
+    """[Q|K|V] rows: each token attends to the tokens up to itself; query head h reads key head h // (heads / kv_heads)."""
+    qkv = _d(qkv)
+    b, s, _ = qkv.shape
+    t = qkv.reshape(b, s, heads + 2 * kv_heads, head_dim)
+    y = np.zeros((b, s, heads, head_dim))
+    for h in range(heads):
+        g = h // (heads // kv_heads)
+        q, k, v = t[:, :, h], t[:, :, heads + g], t[:, :, heads + kv_heads + g]
+        for i in range(s):
+            w = (k[:, :i + 1] @ q[:, i, :, None])[..., 0] * scale
+            w = np.exp(w - w.max(axis=1, keepdims=True))
+            y[:, i, h] = ((w / w.sum(axis=1, keepdims=True))[:, None] @ v[:, :i + 1])[:, 0]
+    return round_to(y.reshape(b, s, heads * head_dim), rnd)
+
+
 def embed_bert(ids, tok, pos, typ, g, beta, eps, rnd="none"):
     ids = np.ascontiguousarray(ids, dtype=np.int32)
     b, s = ids.shape
@@ -256,6 +301,10 @@ def run_op(model, op, env, w_rows=None, rnd=None):
         return layernorm(ins[0], W[op["g"]], W[op["beta"]], op["eps"], res, rnd)
     if k == "attention":
         return attention(ins[0], op["heads"], op["scale"], rnd)
+    if k == "rotary":
+        return rotary(ins[0], op["heads"], op["head_dim"], rnd=rnd, **op["rotary"])
+    if k == "causal_attention":
+        return causal_attention(ins[0], op["heads"], op["kv_heads"], op["head_dim"], op["scale"], rnd)
     if k == "embed_bert":
         return embed_bert(ins[0], W[op["w_tok"]], W[op["w_pos"]], W[op["w_type"]], W[op["g"]], W[op["beta"]],
                           op["eps"], rnd)

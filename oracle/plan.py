@@ -54,7 +54,7 @@ def op_profile(model, op):
     time = max(FLOP / peak, bytes / HBM bandwidth) -- an analytic stand-in for the
     learned operator predictor of Sec. III-B (which needs production traces).
 
-    FLOP counts only the contractions (conv, linear, attention, LSTM); every
+    FLOP counts only the contractions (conv, linear, attention -- causal: its visible pairs --, LSTM); every
     other op is priced by its bytes.  Returns (mem_bytes, time_s, flop).
     """
     dt = model.dtype
@@ -77,6 +77,9 @@ def op_profile(model, op):
     elif k == "attention":
         b, s, f = out_shape
         flop = 4 * b * s * s * f
+    elif k == "causal_attention":
+        b, s, f = out_shape
+        flop = 2 * b * s * (s + 1) * f
     elif k == "lstm":
         b, t, h = out_shape
         flop = 2 * b * t * 4 * h * (in_shape[2] + h)

@@ -19,6 +19,8 @@ MOPAR_E_INFEASIBLE, MOPAR_E_WORKSPACE, MOPAR_E_HIP = 5, 6, 7
 MOPAR_F32, MOPAR_BF16, MOPAR_I32 = 0, 1, 2
 OP_CONV, OP_LINEAR, OP_MAXPOOL, OP_AVGPOOL, OP_LAYERNORM = 1, 2, 3, 4, 5
 OP_ATTENTION, OP_EMBED_BERT, OP_EMBED, OP_LSTM = 6, 7, 8, 9
+OP_ROTARY, OP_CAUSAL_ATTENTION = 10, 11
+ROTARY_LAYOUT, ROTARY_SCALING = {"half": 0, "interleaved": 1}, {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 ACT = {"none": 0, "relu": 1, "gelu": 2}
 CODEC_RAW, CODEC_AE = 0, 1
 # MOPAR_STATIC_WORKSPACE_BYTES of include/mopar.h: the static workspace of mopar_model_forward_static
@@ -50,12 +52,18 @@ class TensorDesc(ctypes.Structure):
     _fields_ = [("dtype", c_i32), ("rank", c_i32), ("dims", c_i64 * 4)]
 
 
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("layout", c_i32), ("scaling", c_i32), ("head_dim", c_i32), ("rot_dim", c_i32), ("base", c_f64),
+                ("factor", c_f64), ("context", c_f64), ("beta_slow", c_f64), ("beta_fast", c_f64), ("mscale", c_f64)]
+
+
 class Op(ctypes.Structure):
     _fields_ = [("kind", c_i32), ("act", c_i32), ("layer", c_i32), ("branch", c_i32), ("pos", c_i32),
                 ("rd", c_i32), ("in0", c_i32), ("in1", c_i32), ("out", c_i32), ("kh", c_i32), ("kw", c_i32),
                 ("stride", c_i32), ("pad", c_i32), ("heads", c_i32), ("n_out", c_i32), ("out_off", c_i32),
                 ("eps", c_f32), ("scale", c_f32), ("rows", c_i64 * 3), ("w", c_i64), ("b", c_i64),
-                ("w2", c_i64), ("w3", c_i64), ("w4", c_i64), ("w5", c_i64)]
+                ("w2", c_i64), ("w3", c_i64), ("w4", c_i64), ("w5", c_i64), ("kv_heads", c_i32), ("head_dim", c_i32),
+                ("rotary", RotaryDesc)]
 
 
 class ModelDesc(ctypes.Structure):
@@ -73,9 +81,13 @@ class Rows(ctypes.Structure):
     _fields_ = [("data", c_vp), ("token_stride", c_i64), ("head_stride", c_i64)]
 
 
-class RotaryDesc(ctypes.Structure):
-    _fields_ = [("layout", c_i32), ("scaling", c_i32), ("head_dim", c_i32), ("rot_dim", c_i32), ("base", c_f64),
-                ("factor", c_f64), ("context", c_f64), ("beta_slow", c_f64), ("beta_fast", c_f64), ("mscale", c_f64)]
+def rotary_desc(head_dim, rot_dim=None, layout="half", base=10000.0, scaling="none", factor=1.0, context=0.0,
+                beta_slow=0.0, beta_fast=0.0, mscale=0.0):
+    """A mopar_rotary_desc; layout and scaling by name (ValueError for an unknown one)."""
+    if layout not in ROTARY_LAYOUT or scaling not in ROTARY_SCALING:
+        raise ValueError(f"layout of {list(ROTARY_LAYOUT)} and scaling of {list(ROTARY_SCALING)}")
+    return RotaryDesc(ROTARY_LAYOUT[layout], ROTARY_SCALING[scaling], head_dim, head_dim if rot_dim is None else rot_dim, base,
+                      factor, context, beta_slow, beta_fast, mscale)
 
 
 class Cache(ctypes.Structure):

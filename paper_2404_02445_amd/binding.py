@@ -230,6 +230,11 @@ def _pack(model):
             o.w, o.b = blob.add(W[op["g"]]), blob.add(W[op["beta"]])
         elif k == "attention":
             o.kind, o.heads, o.scale = L.OP_ATTENTION, op["heads"], op["scale"]
+        elif k == "rotary":
+            o.kind, o.heads, o.rotary = L.OP_ROTARY, op["heads"], L.rotary_desc(op["head_dim"], **op["rotary"])
+        elif k == "causal_attention":
+            o.kind, o.heads, o.kv_heads, o.head_dim = L.OP_CAUSAL_ATTENTION, op["heads"], op["kv_heads"], op["head_dim"]
+            o.scale = op["scale"]
         elif k == "embed_bert":
             o.kind, o.eps = L.OP_EMBED_BERT, op["eps"]
             tok, pos, typ = W[op["w_tok"]], W[op["w_pos"]], W[op["w_type"]]

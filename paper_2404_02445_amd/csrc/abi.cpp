@@ -1,6 +1,5 @@
 // extern "C" entry points: argument checks live in the *_impl functions, this
 // file only turns C++ exceptions into status codes and keeps the error text.
-#include <exception>
 #include <string>
 
 #include "internal.h"
@@ -33,19 +32,6 @@ int timing_slots_impl(const mopar_model_s*, int32_t*);
 int op_times_impl(const mopar_model_s*, float*, int32_t);
 int cut_tensors_impl(const mopar_model_s*, int32_t, int32_t*, int32_t, int32_t*);
 int measure_impl(mopar_model_s*, int32_t, int32_t, const void*, void*, void*, size_t, void*, double*);
-int rotary_create_impl(const mopar_rotary_desc*, mopar_rotary_t*);
-void rotary_destroy_impl(mopar_rotary_s*);
-int rotary_apply_impl(const mopar_rotary_s*, int32_t, int64_t, int32_t, const int32_t*, const mopar_rows*, const mopar_rows*,
-                      void*);
-int cache_append_impl(const mopar_cache*, const mopar_rotary_s*, int64_t, int32_t, const int32_t*, const int32_t*,
-                      const int32_t*, const mopar_rows*, const mopar_rows*, const mopar_rows*, const mopar_rows*, void*);
-int cache_keep_impl(const mopar_cache*, int32_t, int64_t, const int32_t*, const int32_t*, int64_t, const int32_t*, int32_t,
-                    void*);
-int attention_prompt_impl(const mopar_attention*, int64_t, int32_t, const int32_t*, int32_t, const mopar_rows*,
-                          const mopar_rows*, const mopar_rows*, const mopar_rows*, void*);
-int attention_cache_ws_impl(const mopar_attention*, const mopar_cache*, int64_t, int32_t, int32_t, size_t*);
-int attention_cache_impl(const mopar_attention*, const mopar_cache*, int64_t, const int32_t*, int32_t, const int32_t*, int32_t,
-                         const uint64_t*, int32_t, const mopar_rows*, const mopar_rows*, void*, size_t, void*);
 
 static thread_local std::string g_error;
 
@@ -59,17 +45,7 @@ int hip_check(hipError_t e, const char* what) {
     return set_error(MOPAR_E_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
-template <typename F>
-static int guarded(const char* who, F&& f) {
-    try {
-        g_error.clear();
-        return f();
-    } catch (const std::exception& e) {
-        return set_error(MOPAR_E_ARG, std::string(who) + ": " + e.what());
-    } catch (...) {
-        return set_error(MOPAR_E_ARG, std::string(who) + ": unknown exception");
-    }
-}
+void clear_error() { g_error.clear(); }
 
 }  // namespace mopar
 
@@ -181,53 +157,6 @@ int mopar_model_measure(mopar_model_t model, int32_t k_max, int32_t reps, const 
                         void* ws, size_t ws_bytes, void* stream, double* tp_out) {
     return guarded("mopar_model_measure",
                    [&] { return measure_impl(model, k_max, reps, in_dev, out_dev, ws, ws_bytes, stream, tp_out); });
-}
-
-int mopar_rotary_create(const mopar_rotary_desc* desc, mopar_rotary_t* out) {
-    return guarded("mopar_rotary_create", [&] { return rotary_create_impl(desc, out); });
-}
-
-void mopar_rotary_destroy(mopar_rotary_t rotary) { rotary_destroy_impl(rotary); }
-
-int mopar_rotary_apply(mopar_rotary_t rotary, int32_t dtype, int64_t tokens, int32_t heads, const int32_t* pos_dev,
-                       const mopar_rows* x, const mopar_rows* y, void* stream) {
-    return guarded("mopar_rotary_apply", [&] { return rotary_apply_impl(rotary, dtype, tokens, heads, pos_dev, x, y, stream); });
-}
-
-int mopar_cache_append(const mopar_cache* cache, mopar_rotary_t rotary, int64_t tokens, int32_t heads, const int32_t* pos_dev,
-                       const int32_t* seq_dev, const int32_t* slot_dev, const mopar_rows* q, const mopar_rows* q_out,
-                       const mopar_rows* k, const mopar_rows* v, void* stream) {
-    return guarded("mopar_cache_append", [&] {
-        return cache_append_impl(cache, rotary, tokens, heads, pos_dev, seq_dev, slot_dev, q, q_out, k, v, stream);
-    });
-}
-
-int mopar_cache_keep(const mopar_cache* cache, int32_t layers, int64_t layer_stride, const int32_t* len_dev,
-                     const int32_t* path_offsets_dev, int64_t entries, const int32_t* path_dev, int32_t max_path, void* stream) {
-    return guarded("mopar_cache_keep", [&] {
-        return cache_keep_impl(cache, layers, layer_stride, len_dev, path_offsets_dev, entries, path_dev, max_path, stream);
-    });
-}
-
-int mopar_attention_prompt(const mopar_attention* a, int64_t tokens, int32_t n_seq, const int32_t* offsets_dev, int32_t max_len,
-                           const mopar_rows* q, const mopar_rows* k, const mopar_rows* v, const mopar_rows* out, void* stream) {
-    return guarded("mopar_attention_prompt",
-                   [&] { return attention_prompt_impl(a, tokens, n_seq, offsets_dev, max_len, q, k, v, out, stream); });
-}
-
-int mopar_attention_cache_workspace_bytes(const mopar_attention* a, const mopar_cache* cache, int64_t tokens, int32_t max_q,
-                                          int32_t max_len, size_t* bytes) {
-    return guarded("mopar_attention_cache_workspace_bytes",
-                   [&] { return attention_cache_ws_impl(a, cache, tokens, max_q, max_len, bytes); });
-}
-
-int mopar_attention_cache(const mopar_attention* a, const mopar_cache* cache, int64_t tokens, const int32_t* offsets_dev,
-                          int32_t max_q, const int32_t* len_dev, int32_t max_len, const uint64_t* mask_dev, int32_t mask_words,
-                          const mopar_rows* q, const mopar_rows* out, void* ws, size_t ws_bytes, void* stream) {
-    return guarded("mopar_attention_cache", [&] {
-        return attention_cache_impl(a, cache, tokens, offsets_dev, max_q, len_dev, max_len, mask_dev, mask_words, q, out, ws,
-                                    ws_bytes, stream);
-    });
 }
 
 const char* mopar_last_error(void) { return g_error.c_str(); }

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cstdint>
+#include <exception>
 #include <string>
 #include <utility>
 #include <vector>
@@ -16,6 +17,19 @@ namespace mopar {
 // Thread-local error text; set_error returns the status for `return set_error(...)`.
 int set_error(int status, const std::string& msg);
 int hip_check(hipError_t e, const char* what);
+void clear_error();
+
+// f() of an extern "C" entry point, C++ exceptions turned into a status.
+template <typename F> int guarded(const char* who, F&& f) {
+    try {
+        clear_error();
+        return f();
+    } catch (const std::exception& e) {
+        return set_error(MOPAR_E_ARG, std::string(who) + ": " + e.what());
+    } catch (...) {
+        return set_error(MOPAR_E_ARG, std::string(who) + ": unknown exception");
+    }
+}
 
 // ---------------------------------------------------------------------------
 // Kernel launches.  While a model measures op times, the calling thread has a
@@ -205,9 +219,14 @@ struct RotaryTable {
     int d, rot;            // head dim, dims that turn (0: none)
     int interleaved;
 };
-// Rows of `heads` heads turned, row t at position pos[t] (pos null: t mod period).
-hipError_t launch_rotary(const RotaryTable& tab, int dtype, int64_t tokens, int heads, const int32_t* pos, int period,
-                         const mopar_rows* x, const mopar_rows* y, hipStream_t s);
+// The angles of a rotary descriptor, or an error status.
+int rotary_table(const mopar_rotary_desc& d, RotaryTable* out);
+// Rows of `heads` heads, the first `turned` of them turned and the others copied; row t at position pos[t]
+// (pos null: t mod period).  (Weak, as launch_attention_prompt: host-only programs link the model code without
+// the decoding kernels, which only a forward of a model with such operators calls.)
+__attribute__((weak)) hipError_t launch_rotary(const RotaryTable& tab, int dtype, int64_t tokens, int heads, int turned,
+                                               const int32_t* pos, int period, const mopar_rows* x, const mopar_rows* y,
+                                               hipStream_t s);
 // Keys (turned, with a table) and values into their pages; with a table also q turned into q_out.
 hipError_t launch_cache_append(const mopar_cache& c, const RotaryTable* tab, int64_t tokens, int heads, const int32_t* pos,
                                const int32_t* seq, const int32_t* slot, const mopar_rows* q, const mopar_rows* q_out,
@@ -215,7 +234,7 @@ hipError_t launch_cache_append(const mopar_cache& c, const RotaryTable* tab, int
 hipError_t launch_cache_keep(const mopar_cache& c, int layers, int64_t layer_stride, const int32_t* len, const int32_t* offsets,
                              int64_t entries, const int32_t* path, int max_path, hipStream_t s);
 // Causal attention over packed prompts; offsets null: n_seq sequences of max_len rows each.
-hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int n_seq, const int32_t* offsets, int max_len,
+__attribute__((weak)) hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int n_seq, const int32_t* offsets, int max_len,
                                    const mopar_rows* q, const mopar_rows* k, const mopar_rows* v, const mopar_rows* out,
                                    hipStream_t s);
 // Attention over the paged cache; `ws` holds attention_cache_ws_bytes.

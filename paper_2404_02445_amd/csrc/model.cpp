@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <map>
+#include <memory>
 #include <string>
 #include <vector>
 
@@ -41,6 +42,7 @@ struct OpInfo {
     bool stem = false;             // conv: runs on the first-layer kernel
     bool pool_next = false;        // ... and the next op is the only reader of its result, a pool it can do in the same pass
     int64_t K = 0, M = 0;          // GEMM sizes (conv / linear)
+    std::shared_ptr<RotaryTable> rotary;   // rotary: its angles
     std::vector<size_t> temps;     // scratch buffers needed while this op runs
     std::vector<size_t> temp_off;  // their workspace offsets
 };
@@ -83,6 +85,50 @@ struct mopar_model_s {
 namespace mopar {
 
 thread_local LaunchTimer* t_timer = nullptr;
+
+// An angle per position w (radians, 0 <= w < 2 pi) as a fraction of a turn, 64 bits.
+static uint64_t turn_fraction(long double w) {
+    const long double t = w / (2.0L * 3.14159265358979323846264338327950288L);
+    return static_cast<uint64_t>(std::floor(t * 18446744073709551616.0L + 0.5L));
+}
+
+// The angles of a rotary descriptor, or an error.
+int rotary_table(const mopar_rotary_desc& d, RotaryTable* out) {
+    if (d.layout != MOPAR_ROTARY_HALF && d.layout != MOPAR_ROTARY_INTERLEAVED) return set_error(MOPAR_E_ARG, "rotary: layout");
+    if (d.scaling < MOPAR_ROTARY_NONE || d.scaling > MOPAR_ROTARY_YARN) return set_error(MOPAR_E_ARG, "rotary: scaling");
+    if (d.head_dim < 2 || d.head_dim > 256) return set_error(MOPAR_E_ARG, "rotary: head_dim must be 2 to 256");
+    if (d.rot_dim < 2 || d.rot_dim > d.head_dim || d.rot_dim % 2 != 0) return set_error(MOPAR_E_ARG, "rotary: rot_dim must be even, 2 to head_dim");
+    if (!(d.base >= 1.0) || !std::isfinite(d.base)) return set_error(MOPAR_E_ARG, "rotary: base must be at least 1");
+    if (!(d.mscale >= 0.0) || !std::isfinite(d.mscale)) return set_error(MOPAR_E_ARG, "rotary: mscale must not be negative");
+    const bool scaled = d.scaling != MOPAR_ROTARY_NONE;
+    if (scaled && (!(d.factor >= 1.0) || !std::isfinite(d.factor))) return set_error(MOPAR_E_ARG, "rotary: factor must be at least 1");
+    if (d.scaling == MOPAR_ROTARY_NTK && d.rot_dim <= 2) return set_error(MOPAR_E_ARG, "rotary: NTK scaling needs a rot_dim above 2");
+    long double slow = d.beta_slow, fast = d.beta_fast;
+    if (d.scaling == MOPAR_ROTARY_YARN) {
+        if (slow == 0 && fast == 0) slow = 1, fast = 32;
+        if (!(d.context > 0) || !std::isfinite(d.context)) return set_error(MOPAR_E_ARG, "rotary: YaRN scaling needs a context");
+        if (!(slow >= 0) || !(fast > slow) || !std::isfinite(static_cast<double>(fast))) return set_error(MOPAR_E_ARG, "rotary: beta_slow must be below beta_fast");
+    }
+    *out = RotaryTable{};
+    const long double r = d.rot_dim, f = scaled ? d.factor : 1.0L, pi = 3.14159265358979323846264338327950288L;
+    long double base = d.base;
+    if (d.scaling == MOPAR_ROTARY_NTK) base *= std::pow(f, r / (r - 2));
+    for (int j = 0; j < d.rot_dim / 2; ++j) {
+        long double w = std::pow(base, -2.0L * j / r);
+        if (d.scaling == MOPAR_ROTARY_LINEAR) w /= f;
+        if (d.scaling == MOPAR_ROTARY_YARN) {
+            long double g = (d.context * w / (2 * pi) - slow) / (fast - slow);
+            g = g < 0 ? 0 : g > 1 ? 1 : g;
+            w *= g + (1 - g) / f;
+        }
+        out->w[j] = turn_fraction(w);
+    }
+    out->m = static_cast<float>(d.mscale > 0 ? d.mscale : d.scaling == MOPAR_ROTARY_YARN ? 0.1L * std::log(f) + 1.0L : 1.0L);
+    out->d = d.head_dim;
+    out->rot = d.rot_dim;
+    out->interleaved = d.layout == MOPAR_ROTARY_INTERLEAVED;
+    return MOPAR_OK;
+}
 
 namespace {
 
@@ -144,6 +190,7 @@ static void op_profile(const mopar_model_s& m, const mopar_op& op, double* mem, 
             break;
         }
         case MOPAR_OP_ATTENTION: flop = 4 * o.dims[0] * o.dims[1] * o.dims[1] * o.dims[2]; break;
+        case MOPAR_OP_CAUSAL_ATTENTION: flop = 2 * o.dims[0] * o.dims[1] * (o.dims[1] + 1) * o.dims[2]; break;
         case MOPAR_OP_LSTM: flop = 2 * o.dims[0] * o.dims[1] * 4 * o.dims[2] * (in.dims[2] + o.dims[2]); break;
         default: break;
     }
@@ -404,6 +451,30 @@ static int validate_and_build(mopar_model_s& m) {
                     !shape_eq(y, {x.dims[0], x.dims[1], 64 * static_cast<int64_t>(op.heads)}))
                     return set_error(MOPAR_E_SHAPE, nm + ": attention needs (B,S,3*64*heads) -> (B,S,64*heads)");
                 if (x.dims[1] > 128) return set_error(MOPAR_E_UNSUPPORTED, nm + ": attention seq > 128");
+                break;
+            }
+            case MOPAR_OP_ROTARY: {
+                const int64_t d = op.rotary.head_dim;
+                inf.rotary = std::make_shared<RotaryTable>();
+                if (int e = rotary_table(op.rotary, inf.rotary.get())) return e;
+                if (x.rank != 3 || !shape_eq(y, {x.dims[0], x.dims[1], x.dims[2]}) || x.dims[2] % d != 0 || op.heads < 1 ||
+                    op.heads > x.dims[2] / d)
+                    return set_error(MOPAR_E_SHAPE, nm + ": rotary needs (B,S,n*head_dim) -> the same, 1 <= heads <= n");
+                if (d % epc != 0) return set_error(MOPAR_E_UNSUPPORTED, nm + ": head_dim must be a multiple of " + std::to_string(epc));
+                if (x.dims[1] >= (int64_t(1) << 31) || numel(x) / d >= (int64_t(1) << 31) || x.dims[2] * es >= size_t(1) << 25)
+                    return set_error(MOPAR_E_UNSUPPORTED, nm + ": 2^31 heads of tokens or rows of 32 MiB");
+                break;
+            }
+            case MOPAR_OP_CAUSAL_ATTENTION: {
+                const int64_t h = op.heads, kv = op.kv_heads, d = op.head_dim;
+                if (x.rank != 3 || h < 1 || kv < 1 || h > 65536 || h % kv != 0 || d < 1 || d > 128 || x.dims[2] != (h + 2 * kv) * d ||
+                    !shape_eq(y, {x.dims[0], x.dims[1], h * d}))
+                    return set_error(MOPAR_E_SHAPE, nm + ": causal attention needs (B,S,(heads+2*kv_heads)*head_dim) -> (B,S,heads*head_dim)");
+                if (d % 32 != 0) return set_error(MOPAR_E_UNSUPPORTED, nm + ": head_dim must be 32, 64, 96 or 128");
+                if (!(op.scale > 0.0f) || !std::isfinite(op.scale)) return set_error(MOPAR_E_ARG, nm + ": scale must be positive and finite");
+                const int64_t tokens = x.dims[0] * x.dims[1];
+                if (tokens >= (int64_t(1) << 31) || (tokens / 32 + x.dims[0]) * h >= (int64_t(1) << 31) || x.dims[2] * es >= size_t(1) << 25)
+                    return set_error(MOPAR_E_UNSUPPORTED, nm + ": too many rows of heads, or rows of 32 MiB");
                 break;
             }
             case MOPAR_OP_EMBED_BERT: {
@@ -697,6 +768,21 @@ static hipError_t run_op(const mopar_model_s& m, int i, const Ptrs& P, int ksub,
         case MOPAR_OP_ATTENTION:
             return launch_attention(P.get(op.in0), P.get(op.out), static_cast<int>(x.dims[0]),
                                     static_cast<int>(x.dims[1]), op.heads, op.scale, dt, s);
+        case MOPAR_OP_ROTARY: {
+            const int64_t f = x.dims[2], d = op.rotary.head_dim;
+            const mopar_rows in{P.get(op.in0), f, d}, out{P.get(op.out), f, d};
+            return launch_rotary(*inf.rotary, dt, x.dims[0] * x.dims[1], static_cast<int>(f / d), op.heads, nullptr,
+                                 static_cast<int>(x.dims[1]), &in, &out, s);
+        }
+        case MOPAR_OP_CAUSAL_ATTENTION: {
+            const int64_t f = x.dims[2], d = op.head_dim, es = static_cast<int64_t>(elt_bytes(dt));
+            auto* const qkv = static_cast<unsigned char*>(P.get(op.in0));
+            const mopar_attention a{dt, op.heads, op.kv_heads, op.head_dim, op.scale, 0};
+            const mopar_rows q{qkv, f, d}, k{qkv + op.heads * d * es, f, d}, v{qkv + (op.heads + op.kv_heads) * d * es, f, d};
+            const mopar_rows out{P.get(op.out), op.heads * d, d};
+            return launch_attention_prompt(a, x.dims[0] * x.dims[1], static_cast<int>(x.dims[0]), nullptr,
+                                           static_cast<int>(x.dims[1]), &q, &k, &v, &out, s);
+        }
         case MOPAR_OP_EMBED_BERT:
             return launch_embed_bert(static_cast<const int32_t*>(P.get(op.in0)), W(m, op.w), W(m, op.w2), W(m, op.w3),
                                      W(m, op.w4), W(m, op.w5), P.get(op.out), static_cast<int>(x.dims[0]),

@@ -73,7 +73,8 @@ struct RotaryParams {
     int period;
     int units;           // units of a head: what one thread turns (see rotary_kernel)
     int rot_units;       // of them, the first that turn
-    int heads, groups;   // query heads (all heads without a cache); threads that share a token's heads
+    int heads, turned;   // query heads (all heads without a cache); of them, the first that turn
+    int groups;          // threads that share a token's heads
     int64_t tokens;
     RowView x, y;
     // cache
@@ -133,6 +134,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryParams p) {
         unsigned char* dst;
         bool turn = turns;
         if (!CACHE || h < p.heads) {
+            turn = turns && h < p.turned;
             src = p.x.data + t * p.x.ts + h * p.x.hs;
             dst = p.y.data + t * p.y.ts + h * p.y.hs;
         } else {
@@ -288,8 +290,8 @@ __global__ __launch_bounds__(256) void keep_kernel(const KeepParams p) {
 
 }  // namespace
 
-hipError_t launch_rotary(const RotaryTable& tab, int dtype, int64_t tokens, int heads, const int32_t* pos, int period,
-                         const mopar_rows* x, const mopar_rows* y, hipStream_t s) {
+hipError_t launch_rotary(const RotaryTable& tab, int dtype, int64_t tokens, int heads, int turned, const int32_t* pos,
+                         int period, const mopar_rows* x, const mopar_rows* y, hipStream_t s) {
     if (tokens == 0 || heads == 0) return hipSuccess;
     const int es = static_cast<int>(dtype_size(dtype));
     RotaryParams p{};
@@ -297,6 +299,7 @@ hipError_t launch_rotary(const RotaryTable& tab, int dtype, int64_t tokens, int 
     p.pos = pos;
     p.period = period;
     p.heads = heads;
+    p.turned = turned;
     p.tokens = tokens;
     p.x = view(x, es);
     p.y = view(y, es);
@@ -314,6 +317,7 @@ hipError_t launch_cache_append(const mopar_cache& c, const RotaryTable* tab, int
     p.pos = pos;
     p.period = 1;
     p.heads = heads;
+    p.turned = heads;
     p.tokens = tokens;
     p.x = view(q, es);
     p.y = view(q_out, es);

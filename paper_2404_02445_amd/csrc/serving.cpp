@@ -1,4 +1,4 @@
-// Entry points of decoding with a paged cache: argument checks, the rotary's angles, and the launches.
+// Entry points of decoding with a paged cache: argument checks and launches.
 #include <cmath>
 #include <string>
 
@@ -80,53 +80,9 @@ int check_cache_attention(const mopar_attention* a, const mopar_cache* c, int64_
     return MOPAR_OK;
 }
 
-// An angle per position w (radians, 0 <= w < 2 pi) as a fraction of a turn, 64 bits.
-uint64_t turn_fraction(long double w) {
-    const long double t = w / (2.0L * 3.14159265358979323846264338327950288L);
-    return static_cast<uint64_t>(std::floor(t * 18446744073709551616.0L + 0.5L));
-}
-
 }  // namespace
 
-// The angles of a rotary descriptor, or an error.
-int rotary_table(const mopar_rotary_desc& d, RotaryTable* out) {
-    if (d.layout != MOPAR_ROTARY_HALF && d.layout != MOPAR_ROTARY_INTERLEAVED) return bad("rotary: layout");
-    if (d.scaling < MOPAR_ROTARY_NONE || d.scaling > MOPAR_ROTARY_YARN) return bad("rotary: scaling");
-    if (d.head_dim < 2 || d.head_dim > 256) return bad("rotary: head_dim must be 2 to 256");
-    if (d.rot_dim < 2 || d.rot_dim > d.head_dim || d.rot_dim % 2 != 0) return bad("rotary: rot_dim must be even, 2 to head_dim");
-    if (!(d.base >= 1.0) || !std::isfinite(d.base)) return bad("rotary: base must be at least 1");
-    if (!(d.mscale >= 0.0) || !std::isfinite(d.mscale)) return bad("rotary: mscale must not be negative");
-    const bool scaled = d.scaling != MOPAR_ROTARY_NONE;
-    if (scaled && (!(d.factor >= 1.0) || !std::isfinite(d.factor))) return bad("rotary: factor must be at least 1");
-    if (d.scaling == MOPAR_ROTARY_NTK && d.rot_dim <= 2) return bad("rotary: NTK scaling needs a rot_dim above 2");
-    long double slow = d.beta_slow, fast = d.beta_fast;
-    if (d.scaling == MOPAR_ROTARY_YARN) {
-        if (slow == 0 && fast == 0) slow = 1, fast = 32;
-        if (!(d.context > 0) || !std::isfinite(d.context)) return bad("rotary: YaRN scaling needs a context");
-        if (!(slow >= 0) || !(fast > slow) || !std::isfinite(static_cast<double>(fast))) return bad("rotary: beta_slow must be below beta_fast");
-    }
-    *out = RotaryTable{};
-    const long double r = d.rot_dim, f = scaled ? d.factor : 1.0L, pi = 3.14159265358979323846264338327950288L;
-    long double base = d.base;
-    if (d.scaling == MOPAR_ROTARY_NTK) base *= std::pow(f, r / (r - 2));
-    for (int j = 0; j < d.rot_dim / 2; ++j) {
-        long double w = std::pow(base, -2.0L * j / r);
-        if (d.scaling == MOPAR_ROTARY_LINEAR) w /= f;
-        if (d.scaling == MOPAR_ROTARY_YARN) {
-            long double g = (d.context * w / (2 * pi) - slow) / (fast - slow);
-            g = g < 0 ? 0 : g > 1 ? 1 : g;
-            w *= g + (1 - g) / f;
-        }
-        out->w[j] = turn_fraction(w);
-    }
-    out->m = static_cast<float>(d.mscale > 0 ? d.mscale : d.scaling == MOPAR_ROTARY_YARN ? 0.1L * std::log(f) + 1.0L : 1.0L);
-    out->d = d.head_dim;
-    out->rot = d.rot_dim;
-    out->interleaved = d.layout == MOPAR_ROTARY_INTERLEAVED;
-    return MOPAR_OK;
-}
-
-int rotary_create_impl(const mopar_rotary_desc* desc, mopar_rotary_t* out) {
+static int rotary_create_impl(const mopar_rotary_desc* desc, mopar_rotary_t* out) {
     if (!out) return bad("rotary: null out");
     *out = nullptr;
     if (!desc) return bad("rotary: null");
@@ -136,9 +92,7 @@ int rotary_create_impl(const mopar_rotary_desc* desc, mopar_rotary_t* out) {
     return MOPAR_OK;
 }
 
-void rotary_destroy_impl(mopar_rotary_s* r) { delete r; }
-
-int rotary_apply_impl(const mopar_rotary_s* rot, int32_t dtype, int64_t tokens, int32_t heads, const int32_t* pos, const mopar_rows* x,
+static int rotary_apply_impl(const mopar_rotary_s* rot, int32_t dtype, int64_t tokens, int32_t heads, const int32_t* pos, const mopar_rows* x,
                       const mopar_rows* y, void* stream) {
     if (!rot) return bad("rotary: null");
     if (!known_dtype(dtype)) return set_error(MOPAR_E_DTYPE, "rotary: dtype must be f32 or bf16");
@@ -150,10 +104,10 @@ int rotary_apply_impl(const mopar_rotary_s* rot, int32_t dtype, int64_t tokens, 
     if (!pos) return bad("rotary: positions are null");
     if (int e = check_rows(x, "rotary: x", dtype, tokens, heads, d, false)) return e;
     if (int e = check_rows(y, "rotary: y", dtype, tokens, heads, d, true)) return e;
-    return hip_check(launch_rotary(rot->tab, dtype, tokens, heads, pos, 1, x, y, static_cast<hipStream_t>(stream)), "mopar_rotary_apply");
+    return hip_check(launch_rotary(rot->tab, dtype, tokens, heads, heads, pos, 1, x, y, static_cast<hipStream_t>(stream)), "mopar_rotary_apply");
 }
 
-int cache_append_impl(const mopar_cache* c, const mopar_rotary_s* rot, int64_t tokens, int32_t heads, const int32_t* pos,
+static int cache_append_impl(const mopar_cache* c, const mopar_rotary_s* rot, int64_t tokens, int32_t heads, const int32_t* pos,
                       const int32_t* seq, const int32_t* slot, const mopar_rows* q, const mopar_rows* q_out, const mopar_rows* k,
                       const mopar_rows* v, void* stream) {
     if (int e = check_cache(c)) return e;
@@ -175,7 +129,7 @@ int cache_append_impl(const mopar_cache* c, const mopar_rotary_s* rot, int64_t t
                      "mopar_cache_append");
 }
 
-int cache_keep_impl(const mopar_cache* c, int32_t layers, int64_t layer_stride, const int32_t* len, const int32_t* offsets,
+static int cache_keep_impl(const mopar_cache* c, int32_t layers, int64_t layer_stride, const int32_t* len, const int32_t* offsets,
                     int64_t entries, const int32_t* path, int32_t max_path, void* stream) {
     if (int e = check_cache(c)) return e;
     const int64_t epc = 16 / static_cast<int64_t>(dtype_size(c->dtype));
@@ -190,7 +144,7 @@ int cache_keep_impl(const mopar_cache* c, int32_t layers, int64_t layer_stride, 
                      "mopar_cache_keep");
 }
 
-int attention_prompt_impl(const mopar_attention* a, int64_t tokens, int32_t n_seq, const int32_t* offsets, int32_t max_len,
+static int attention_prompt_impl(const mopar_attention* a, int64_t tokens, int32_t n_seq, const int32_t* offsets, int32_t max_len,
                           const mopar_rows* q, const mopar_rows* k, const mopar_rows* v, const mopar_rows* out, void* stream) {
     if (int e = check_attention(a)) return e;
     if (tokens < 0 || tokens >= (int64_t(1) << 31) || n_seq < 0 || max_len < 0) return bad("attention: tokens, n_seq or max_len");
@@ -205,14 +159,14 @@ int attention_prompt_impl(const mopar_attention* a, int64_t tokens, int32_t n_se
                      "mopar_attention_prompt");
 }
 
-int attention_cache_ws_impl(const mopar_attention* a, const mopar_cache* c, int64_t tokens, int32_t max_q, int32_t max_len, size_t* bytes) {
+static int attention_cache_ws_impl(const mopar_attention* a, const mopar_cache* c, int64_t tokens, int32_t max_q, int32_t max_len, size_t* bytes) {
     if (!bytes) return bad("attention: null bytes");
     if (int e = check_cache_attention(a, c, tokens, max_q, max_len)) return e;
     *bytes = attention_cache_ws_bytes(*a, *c, tokens, max_q, max_len);
     return MOPAR_OK;
 }
 
-int attention_cache_impl(const mopar_attention* a, const mopar_cache* c, int64_t tokens, const int32_t* offsets, int32_t max_q,
+static int attention_cache_impl(const mopar_attention* a, const mopar_cache* c, int64_t tokens, const int32_t* offsets, int32_t max_q,
                          const int32_t* len, int32_t max_len, const uint64_t* mask, int32_t mask_words, const mopar_rows* q,
                          const mopar_rows* out, void* ws, size_t ws_bytes, void* stream) {
     if (int e = check_cache_attention(a, c, tokens, max_q, max_len)) return e;
@@ -231,3 +185,56 @@ int attention_cache_impl(const mopar_attention* a, const mopar_cache* c, int64_t
 }
 
 }  // namespace mopar
+
+using namespace mopar;
+
+extern "C" {
+
+int mopar_rotary_create(const mopar_rotary_desc* desc, mopar_rotary_t* out) {
+    return guarded("mopar_rotary_create", [&] { return rotary_create_impl(desc, out); });
+}
+
+void mopar_rotary_destroy(mopar_rotary_t rotary) { delete rotary; }
+
+int mopar_rotary_apply(mopar_rotary_t rotary, int32_t dtype, int64_t tokens, int32_t heads, const int32_t* pos_dev,
+                       const mopar_rows* x, const mopar_rows* y, void* stream) {
+    return guarded("mopar_rotary_apply", [&] { return rotary_apply_impl(rotary, dtype, tokens, heads, pos_dev, x, y, stream); });
+}
+
+int mopar_cache_append(const mopar_cache* cache, mopar_rotary_t rotary, int64_t tokens, int32_t heads, const int32_t* pos_dev,
+                       const int32_t* seq_dev, const int32_t* slot_dev, const mopar_rows* q, const mopar_rows* q_out,
+                       const mopar_rows* k, const mopar_rows* v, void* stream) {
+    return guarded("mopar_cache_append", [&] {
+        return cache_append_impl(cache, rotary, tokens, heads, pos_dev, seq_dev, slot_dev, q, q_out, k, v, stream);
+    });
+}
+
+int mopar_cache_keep(const mopar_cache* cache, int32_t layers, int64_t layer_stride, const int32_t* len_dev,
+                     const int32_t* path_offsets_dev, int64_t entries, const int32_t* path_dev, int32_t max_path, void* stream) {
+    return guarded("mopar_cache_keep", [&] {
+        return cache_keep_impl(cache, layers, layer_stride, len_dev, path_offsets_dev, entries, path_dev, max_path, stream);
+    });
+}
+
+int mopar_attention_prompt(const mopar_attention* a, int64_t tokens, int32_t n_seq, const int32_t* offsets_dev, int32_t max_len,
+                           const mopar_rows* q, const mopar_rows* k, const mopar_rows* v, const mopar_rows* out, void* stream) {
+    return guarded("mopar_attention_prompt",
+                   [&] { return attention_prompt_impl(a, tokens, n_seq, offsets_dev, max_len, q, k, v, out, stream); });
+}
+
+int mopar_attention_cache_workspace_bytes(const mopar_attention* a, const mopar_cache* cache, int64_t tokens, int32_t max_q,
+                                          int32_t max_len, size_t* bytes) {
+    return guarded("mopar_attention_cache_workspace_bytes",
+                   [&] { return attention_cache_ws_impl(a, cache, tokens, max_q, max_len, bytes); });
+}
+
+int mopar_attention_cache(const mopar_attention* a, const mopar_cache* cache, int64_t tokens, const int32_t* offsets_dev,
+                          int32_t max_q, const int32_t* len_dev, int32_t max_len, const uint64_t* mask_dev, int32_t mask_words,
+                          const mopar_rows* q, const mopar_rows* out, void* ws, size_t ws_bytes, void* stream) {
+    return guarded("mopar_attention_cache", [&] {
+        return attention_cache_impl(a, cache, tokens, offsets_dev, max_q, len_dev, max_len, mask_dev, mask_words, q, out, ws,
+                                    ws_bytes, stream);
+    });
+}
+
+}  // extern "C"

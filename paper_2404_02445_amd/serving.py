@@ -16,8 +16,6 @@ from . import _lib as L
 from ._lib import check, lib
 
 _DTYPE = {torch.float32: L.MOPAR_F32, torch.bfloat16: L.MOPAR_BF16}
-_LAYOUT = {"half": 0, "interleaved": 1}
-_SCALING = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
 def _need(ok, what):
@@ -73,11 +71,9 @@ def _ints(t, name, like, n, dtype=torch.int32):
 class Rotary:
     """Rotary positions (mopar_rotary_create): the angles of a descriptor, made once."""
 
-    def __init__(self, head_dim, rot_dim=None, layout="half", base=10000.0, scaling="none", factor=1.0, context=0.0,
-                 beta_slow=0.0, beta_fast=0.0, mscale=0.0):
-        _need(layout in _LAYOUT and scaling in _SCALING, f"layout of {list(_LAYOUT)} and scaling of {list(_SCALING)}")
-        d = L.RotaryDesc(_LAYOUT[layout], _SCALING[scaling], head_dim, head_dim if rot_dim is None else rot_dim, base, factor,
-                         context, beta_slow, beta_fast, mscale)
+    def __init__(self, head_dim, **kw):
+        """``kw``: rot_dim, layout, base, scaling, factor, context, beta_slow, beta_fast, mscale (mopar_rotary_desc)."""
+        d = L.rotary_desc(head_dim, **kw)
         h = ctypes.c_void_p()
         check(lib().mopar_rotary_create(ctypes.byref(d), ctypes.byref(h)))
         self.handle, self.head_dim = h, head_dim

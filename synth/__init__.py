@@ -209,6 +209,17 @@ class _Builder:
         return self.op(kind="attention", name=name, inputs=[qkv], out=out, heads=heads,
                        head_dim=f // heads, scale=1.0 / math.sqrt(f // heads), **kw)
 
+    def rotary(self, x, heads, head_dim, name, rotary=None, **kw):
+        """The first `heads` heads of every row turned to the token's position (rotary: rot_dim, layout, scaling ...)."""
+        out = self.tensor(self.shape(x))
+        return self.op(kind="rotary", name=name, inputs=[x], out=out, heads=heads, head_dim=head_dim, rotary=rotary or {}, **kw)
+
+    def causal_attention(self, qkv, heads, kv_heads, head_dim, name, **kw):
+        b, s, _ = self.shape(qkv)
+        out = self.tensor((b, s, heads * head_dim))
+        return self.op(kind="causal_attention", name=name, inputs=[qkv], out=out, heads=heads, kv_heads=kv_heads,
+                       head_dim=head_dim, scale=1.0 / math.sqrt(head_dim), **kw)
+
     def embed_bert(self, ids, vocab, max_pos, n_types, f, name, eps, std=0.02, **kw):
         b, s = self.shape(ids)
         self.store(name + ".tok", self.normal((vocab, f), std))
@@ -439,9 +450,38 @@ def skipnet_mini(batch=2, hw=16, k_rd=2, seed=1007, dtype=BF16):
     return bld.finish(y, n_slices=3, k_by_layer={rd_layer: k_rd})
 
 
-BUILDERS = {1: tiny_vgg, 2: resnet50, 3: vgg16, 4: bert_base, 5: lstm_lm, 6: inception_mini, 7: skipnet_mini}
+def decoder_mini(batch=2, seq=150, layers=2, hidden=128, heads=4, kv_heads=2, head_dim=64, ffn=256, vocab=300, k_rd=2,
+                 rotary=None, seed=1008, dtype=BF16):
+    """Small decoder language model: rotary positions, causal attention with grouped heads, post-LN blocks, and a
+    vocabulary projection; cut after every block."""
+    bld = _Builder("decoder_mini", dtype, batch, seed, cfg=8)
+    ids = bld.tensor((batch, seq), I32)
+    bld.new_layer("embed")
+    x = bld.embed(ids, vocab, hidden, "embed", -1.0, 1.0)
+    k_by_layer, cuts = {}, []
+    for li in range(layers):
+        nm = f"L{li + 1}"
+        bld.new_layer(nm)
+        qkv = bld.linear(x, (heads + 2 * kv_heads) * head_dim, "none", nm + ".qkv", "rand")
+        qkv = bld.rotary(qkv, heads + kv_heads, head_dim, nm + ".rot", rotary)
+        att = bld.causal_attention(qkv, heads, kv_heads, head_dim, nm + ".attn")
+        a = bld.linear(att, hidden, "none", nm + ".proj", "rand", res=x)
+        a = bld.layernorm(a, nm + ".ln1", 1e-12)
+        h = bld.linear(a, ffn, "gelu", nm + ".ffn1", "rand", rd=True)
+        h = bld.linear(h, hidden, "none", nm + ".ffn2", "rand", res=a, rd=True)
+        x = bld.layernorm(h, nm + ".ln2", 1e-12)
+        k_by_layer[bld.layer] = k_rd
+        cuts.append(bld.layer)
+    bld.new_layer("proj")
+    y = bld.linear(x, vocab, "none", "proj", "rand", rd=True)
+    k_by_layer[bld.layer] = k_rd
+    return bld.finish(y, n_slices=len(cuts) + 1, cuts_after=cuts, k_by_layer=k_by_layer)
+
+
+BUILDERS = {1: tiny_vgg, 2: resnet50, 3: vgg16, 4: bert_base, 5: lstm_lm, 6: inception_mini, 7: skipnet_mini,
+            8: decoder_mini}
 NAMES = {1: "tiny_vgg", 2: "resnet50", 3: "vgg16", 4: "bert_base", 5: "lstm_lm", 6: "inception_mini",
-         7: "skipnet_mini"}
+         7: "skipnet_mini", 8: "decoder_mini"}
 
 
 def build(cfg: int, **kw) -> Model:

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2404_02445_amd as P
-from serving_ref import (attend, cache_rows, check, pack_mask, page_table, rotate, rotate_tol, tree_mask)
+from tests.serving_ref import (attend, cache_rows, check, pack_mask, page_table, rotate, rotate_tol, tree_mask)
 
 pytestmark = pytest.mark.gpu
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
@@ -34,12 +34,12 @@ def test_rotary(dt, layout, tokens, heads, d, rot):
     x = rows[:, 1:heads + 1]
     pos = torch.randint(0, 5000, (tokens,), generator=g, dtype=torch.int32).cuda()
     y = torch.full((tokens, heads, d), 7.0, device="cuda", dtype=DT[dt])
-    P.mopar_rotary_apply(P.Rotary(d, rot, layout), x, y, pos)
+    P.mopar_rotary_apply(P.Rotary(d, rot_dim=rot, layout=layout), x, y, pos)
     ref, mag = rotate(x, pos, rot, layout)
     check(y, ref, rotate_tol(ref, mag, DT[dt]))
     assert torch.equal(y[..., rot:], x[..., rot:])
     before = rows.clone()
-    P.mopar_rotary_apply(P.Rotary(d, rot, layout), x, x, pos)          # in place, the rows around untouched
+    P.mopar_rotary_apply(P.Rotary(d, rot_dim=rot, layout=layout), x, x, pos)          # in place, the rows around untouched
     assert torch.equal(x, y)
     assert torch.equal(rows[:, 0], before[:, 0]) and torch.equal(rows[:, -1], before[:, -1])
 
@@ -71,7 +71,7 @@ def test_rotary_passes_nan_beside_what_turns():
     x = torch.zeros(2, 1, 64, device="cuda", dtype=torch.float32)
     x[:, :, 10:] = float("nan")
     y = torch.empty_like(x)
-    P.mopar_rotary_apply(P.Rotary(64, 10, "interleaved"), x, y, ints([3, 4]))
+    P.mopar_rotary_apply(P.Rotary(64, rot_dim=10, layout="interleaved"), x, y, ints([3, 4]))
     assert bool((y[:, :, :10] == 0).all()) and bool(y[:, :, 10:].isnan().all())
 
 
@@ -97,7 +97,7 @@ def test_append(dt, kv, heads, d, page, rot, layout):
     cache = P.PagedCache(kc, vc, table)
     turned = k
     if rot:
-        r = P.Rotary(d, rot, layout)
+        r = P.Rotary(d, rot_dim=rot, layout=layout)
         P.mopar_cache_append(cache, k, v, ints(seq), ints(slot), rotary=r, pos=pos, q=q, q_out=q_out)
         turned = torch.empty(t, kv, d, device="cuda", dtype=DT[dt])
         P.mopar_rotary_apply(r, k, turned, pos)

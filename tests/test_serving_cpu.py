@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import paper_2404_02445_amd as P
-from helpers import host_rule
+from tests.helpers import host_rule
 from paper_2404_02445_amd import _lib as L
 
 A = 0x10000          # an aligned address that no accepted call ever sees
