@@ -201,10 +201,14 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
                                 static_cast<unsigned>(uniform(static_cast<int>(v))));
 }
 
+// within rows of 16 lanes by DPP moves (partners 1 and 2 apart, the mirrored half row, the mirrored row), then the rows
 __device__ __forceinline__ int wave_sum(int v) {
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) v += __shfl_xor(v, i, 64);
-    return uniform(v);
+    v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, false);
+    return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) +
+           (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
 }
 
 // A sequence over the cache: its drafted rows, tokens before them and in all, and its work -- a unit is a tile of BM
@@ -735,10 +739,11 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         int first[AHEAD];                             // pages of the first stages
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) first[i] = PAGED && key0 < key1 ? *page_of(key0 + i * KT) : 0;
+        if (!PAGED) issue(0, 0, 0);
         // the queries are waited for here, or the compiler would do it, for every load in flight, in the loop
 #pragma unroll
         for (int i = 0; i < CH / 2; ++i) pin(qf[i]);
-        if (key0 < key1) {
+        if (PAGED && key0 < key1) {
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
                 look_at(first[i], key0 + i * KT);
@@ -801,6 +806,7 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             end();
         }
 
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // no load into LDS outlives the unit (the pages sent last)
         // what was left out, where it is seen (a weight is positive: the sum becomes infinite or NaN itself)
         if (marred) {
             for (int key = looked_at; key < wave_end; ++key) {
