@@ -217,9 +217,10 @@ void mopar_rotary_destroy(mopar_rotary_t rotary);
 
 /* y = x turned, for `heads` heads (the rotary's head_dim) of `tokens` rows, row t
  * at position pos_dev[t].  y may be x itself (same data and strides); any other
- * overlap is undefined.  tokens or heads 0: nothing to do.
+ * overlap is undefined.  heads is at most 65536; tokens or heads 0: nothing to do.
  * Errors: MOPAR_E_ARG, MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (head_dim off the
- * 16-byte granule, tokens * heads >= 2^31), MOPAR_E_HIP. */
+ * 16-byte granule, tokens * heads >= 2^31, work for more than 2^32 threads of at
+ * least one pair of dims each), MOPAR_E_HIP. */
 int mopar_rotary_apply(mopar_rotary_t rotary, int32_t dtype, int64_t tokens, int32_t heads, const int32_t* pos_dev,
                        const mopar_rows* x, const mopar_rows* y, void* stream);
 
@@ -227,7 +228,7 @@ int mopar_rotary_apply(mopar_rotary_t rotary, int32_t dtype, int64_t tokens, int
  * i mod page_tokens of page table_dev[s * table_stride + i / page_tokens]; page p
  * of head h is page_tokens rows of head_dim at
  * ((p * kv_heads + h) * page_tokens) * head_dim of k and of v (device, 16-byte
- * aligned, any size: offsets are 64-bit).  A sequence has slots for
+ * aligned, less than 2^46 elements: offsets are 64-bit).  A sequence has slots for
  * max_pages * page_tokens tokens; further ones do not exist. */
 typedef struct {
     int32_t dtype;
@@ -237,7 +238,7 @@ typedef struct {
     int64_t pages;              /* pages in k and in v, 1 .. 2^31 - 1  */
     void* k;
     void* v;
-    const int32_t* table_dev;
+    const int32_t* table_dev;   /* not read with n_seq 0 */
     int64_t table_stride;       /* entries between the rows of two sequences, >= max_pages */
     int32_t max_pages;          /* entries of a sequence's row, >= 1                       */
     int32_t n_seq;              /* rows of the table, >= 0                                 */
@@ -262,7 +263,7 @@ typedef struct {
     int32_t dtype;
     int32_t heads, kv_heads;    /* heads a multiple of kv_heads      */
     int32_t head_dim;           /* 32, 64, 96 or 128                 */
-    float scale;                /* > 0, finite; usually 1/sqrt(head_dim) */
+    float scale;                /* > 0, at most 2^127; usually 1/sqrt(head_dim) */
     int32_t reserved;
 } mopar_attention;
 
@@ -274,7 +275,8 @@ typedef struct {
  * max_len rows).  Rows of no sequence are neither read nor written, and what is not
  * visible to a row -- infinities and NaN included -- does not reach it.  out must
  * not overlap q, k or v.
- * Errors: MOPAR_E_ARG, MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (head_dim), MOPAR_E_HIP. */
+ * Errors: MOPAR_E_ARG, MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (head_dim; 2^30 tokens; 2^24
+ * tiles of 128 tokens, of the sequences and heads), MOPAR_E_HIP. */
 int mopar_attention_prompt(const mopar_attention* a, int64_t tokens, int32_t n_seq, const int32_t* offsets_dev,
                            int32_t max_len, const mopar_rows* q, const mopar_rows* k, const mopar_rows* v,
                            const mopar_rows* out, void* stream);
@@ -290,10 +292,13 @@ int mopar_attention_prompt(const mopar_attention* a, int64_t tokens, int32_t n_s
  * NULL: tokens j <= i (one new token, or a chain of them).  A row that sees nothing
  * gets zeros.  max_len >= 1 bounds len + drafted tokens; slots from max_len on are not
  * read.  `ws` holds mopar_attention_cache_workspace_bytes; its contents need not
- * survive between calls, and calls that overlap need one each.
+ * survive between calls, and calls that overlap need one each.  out must not overlap q;
+ * drafted rows past max_q are left as they are.
  * Errors: MOPAR_E_ARG (also a mask of fewer than ceil(max_q / 64) words),
  * MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (head_dim; heads / kv_heads * max_q of 2^20
- * and more; n_seq * kv_heads * max_len so large that their tiles reach 2^30),
+ * and more; n_seq * kv_heads * max_q so large that their tiles of 32 to 256 rows reach
+ * 2^22, or these times the tiles of 32 or 64 keys 2^30; max_len and the table's slots
+ * both above 2^30),
  * MOPAR_E_WORKSPACE, MOPAR_E_HIP. */
 int mopar_attention_cache_workspace_bytes(const mopar_attention* a, const mopar_cache* cache, int64_t tokens,
                                           int32_t max_q, int32_t max_len, size_t* bytes);
@@ -309,8 +314,10 @@ int mopar_attention_cache(const mopar_attention* a, const mopar_cache* cache, in
  * `entries`).  Drafted indices of a path ascend (as ancestors do in any order that puts
  * parents first); an index below its place i - lo, which no such path has, moves
  * nothing, nor does one from or to an absent page.  max_path bounds a path's length; entries past it are left.
+ * A page that a sequence stores into must be no other sequence's.
  * Afterwards the sequence has len_dev[s] + (hi - lo) tokens.
- * Errors: MOPAR_E_ARG, MOPAR_E_UNSUPPORTED, MOPAR_E_HIP. */
+ * Errors: MOPAR_E_ARG, MOPAR_E_UNSUPPORTED (2^24 and more blocks of up to
+ * 4 KB of a token, of the sequences and layers), MOPAR_E_HIP. */
 int mopar_cache_keep(const mopar_cache* cache, int32_t layers, int64_t layer_stride, const int32_t* len_dev,
                      const int32_t* path_offsets_dev, int64_t entries, const int32_t* path_dev, int32_t max_path,
                      void* stream);

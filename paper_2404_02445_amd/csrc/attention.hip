@@ -62,7 +62,7 @@ struct AttnParams {
     // cache
     const int32_t *table, *len;
     int64_t table_stride, pages;
-    int max_pages, shift, max_len;
+    int shift, max_len;              // max_len: at most the slots of the table, at most 2^30
     const uint64_t* mask;
     int mask_words;
     // over a cache: whether blocks take equal shares of all key stages (else one unit each), the least share,
@@ -221,7 +221,7 @@ template <int KT, int BM> __device__ __forceinline__ SeqShape seq_shape(const At
     SeqShape q;
     rows_of(p, s, q.start, q.rows);
     q.past = min(max(p.len[s], 0), p.max_len);
-    q.total = min(q.past + min(q.rows, p.max_len - q.past), p.max_pages << p.shift);
+    q.total = q.past + min(q.rows, p.max_len - q.past);
     q.nt = max(1, (q.total + KT - 1) / KT);
     q.units = (q.rows * p.group + BM - 1) / BM * p.kv_heads;
     return q;
@@ -969,7 +969,7 @@ CachePlan cache_plan(const mopar_attention& a, int n_seq, int max_q, int max_len
     // blocks that a CU holds at once, by LDS and two waves a SIMD
     const int stage = 2 * c.kt * (a.head_dim > 64 ? 128 : a.head_dim) * static_cast<int>(dtype_size(a.dtype));
     const int per_cu = std::min(256 / c.bm, 160 * 1024 / (ring_of(c.bm / 32, stage) * stage + c.bm / 32 * 1024));
-    const int64_t units = static_cast<int64_t>(n_seq) * a.kv_heads * c.row_tiles, nt = (max_len + c.kt - 1) / c.kt;
+    const int64_t units = static_cast<int64_t>(n_seq) * a.kv_heads * c.row_tiles, nt = (static_cast<int64_t>(max_len) + c.kt - 1) / c.kt;
     c.split = nt > 2 * kLeastStages;
     const int64_t blocks = c.split ? std::min<int64_t>(256 * per_cu, units * nt) : units;
     c.blocks = static_cast<int>(std::min<int64_t>(blocks, int64_t(1) << 30));
@@ -979,11 +979,11 @@ CachePlan cache_plan(const mopar_attention& a, int n_seq, int max_q, int max_len
 
 }  // namespace
 
-// stages of a call over a cache at most (they are counted in 32 bits)
+// A grid of a tile a block holds its threads, and stages are counted in 32 bits.
 bool attention_cache_fits(const mopar_attention& a, int n_seq, int max_q, int max_len) {
     const CachePlan c = cache_plan(a, n_seq, max_q, max_len);
-    const double stages = static_cast<double>(n_seq) * a.kv_heads * c.row_tiles * ((max_len + static_cast<double>(c.kt) - 1) / c.kt);
-    return stages < 1073741824.0;
+    const int64_t units = static_cast<int64_t>(n_seq) * a.kv_heads * c.row_tiles;          // (factors below 2^31, 2^16 and 2^15)
+    return units < 1 << 22 && units * ((static_cast<int64_t>(max_len) + c.kt - 1) / c.kt) < 1 << 30;
 }
 
 hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int n_seq, const int32_t* offsets, int max_len,
@@ -1001,16 +1001,13 @@ hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int
     p.v_hs = v->head_stride * es;
     p.offsets = offsets;
     p.n_seq = n_seq;
-    p.max_rows = max_len;
+    p.max_rows = static_cast<int>(std::min<int64_t>(max_len, tokens));
     p.tokens = tokens;
     p.heads = a.heads;
     p.kv_heads = a.kv_heads;
     p.group = a.heads / a.kv_heads;
     p.c = a.scale * 1.44269504088896341f;
-    // tiles of 128 rows: no more than the tokens fill and one more a sequence
-    const int64_t items = std::min<int64_t>(tokens / 128 + n_seq, static_cast<int64_t>(n_seq) * ((max_len + 127) / 128));
-    if (items * a.heads >= (int64_t(1) << 31)) return hipErrorInvalidValue;
-    const dim3 grid(static_cast<unsigned>(items * a.heads));
+    const dim3 grid(static_cast<unsigned>(prompt_tiles(tokens, n_seq, max_len) * a.heads));
     return by_type(a.dtype, a.head_dim, [&](auto t, auto d) {
         using T = decltype(t);
         launch_kernel((attention_kernel<T, d, 4, sizeof(T) == 2 ? 2 : 1, 2, false>), grid, dim3(256), 0, s, p);
@@ -1043,9 +1040,8 @@ hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c
     p.len = len;
     p.table_stride = c.table_stride;
     p.pages = c.pages;
-    p.max_pages = c.max_pages;
     p.shift = __builtin_ctz(static_cast<unsigned>(c.page_tokens));
-    p.max_len = max_len;
+    p.max_len = cache_limit(c, max_len);
     p.mask = mask;
     p.mask_words = mask_words;
     const CachePlan cp = cache_plan(a, c.n_seq, max_q, max_len);
@@ -1067,7 +1063,7 @@ hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c
             launch_kernel(join, dim3(grid.x, cp.bm / 16), dim3(256), 0, s, p);
             return hipGetLastError();
         };
-                auto of = [&](auto wr) {
+        auto of = [&](auto wr) {
             constexpr int WR = wr, SUBS = sizeof(T) == 2 && WR >= 4 ? 2 : 1, STAGE = 2 * 32 * SUBS * Geo<T, d>::RB;
             return go(attention_kernel<T, d, WR, SUBS, ring_of(WR, STAGE), true>, attention_join_kernel<T, d, WR * 32>, WR * 64);
         };

@@ -1,6 +1,7 @@
 // Internal declarations shared by the host code and the kernel launchers.
 #pragma once
 
+#include <algorithm>
 #include <cstdint>
 #include <exception>
 #include <string>
@@ -237,6 +238,19 @@ hipError_t launch_cache_keep(const mopar_cache& c, int layers, int64_t layer_str
 __attribute__((weak)) hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int n_seq, const int32_t* offsets, int max_len,
                                    const mopar_rows* q, const mopar_rows* k, const mopar_rows* v, const mopar_rows* out,
                                    hipStream_t s);
+// Its tiles of 128 rows: no more than the tokens fill and one more a sequence.
+inline int64_t prompt_tiles(int64_t tokens, int n_seq, int64_t max_len) {
+    return std::min(tokens / 128 + n_seq, n_seq * ((max_len + 127) / 128));
+}
+// threads of a grid at most
+constexpr int64_t kMaxThreads = int64_t(1) << 32;
+inline bool prompt_fits(int64_t tokens, int n_seq, int64_t max_len, int heads) {
+    return tokens < int64_t(1) << 30 && prompt_tiles(tokens, n_seq, max_len) < kMaxThreads / 256 / heads;
+}
+// Tokens of a sequence at most: max_len and the slots of the table.
+inline int cache_limit(const mopar_cache& c, int max_len) {
+    return static_cast<int>(std::min<int64_t>(max_len, static_cast<int64_t>(c.max_pages) * c.page_tokens));
+}
 // Attention over the paged cache; `ws` holds attention_cache_ws_bytes.
 bool attention_cache_fits(const mopar_attention& a, int n_seq, int max_q, int max_len);
 size_t attention_cache_ws_bytes(const mopar_attention& a, const mopar_cache& c, int64_t tokens, int max_q, int max_len);

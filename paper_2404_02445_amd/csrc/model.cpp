@@ -99,7 +99,7 @@ int rotary_table(const mopar_rotary_desc& d, RotaryTable* out) {
     if (d.head_dim < 2 || d.head_dim > 256) return set_error(MOPAR_E_ARG, "rotary: head_dim must be 2 to 256");
     if (d.rot_dim < 2 || d.rot_dim > d.head_dim || d.rot_dim % 2 != 0) return set_error(MOPAR_E_ARG, "rotary: rot_dim must be even, 2 to head_dim");
     if (!(d.base >= 1.0) || !std::isfinite(d.base)) return set_error(MOPAR_E_ARG, "rotary: base must be at least 1");
-    if (!(d.mscale >= 0.0) || !std::isfinite(d.mscale)) return set_error(MOPAR_E_ARG, "rotary: mscale must not be negative");
+    if (!(d.mscale >= 0.0) || !std::isfinite(static_cast<float>(d.mscale))) return set_error(MOPAR_E_ARG, "rotary: mscale must not be negative, nor past float32");
     const bool scaled = d.scaling != MOPAR_ROTARY_NONE;
     if (scaled && (!(d.factor >= 1.0) || !std::isfinite(d.factor))) return set_error(MOPAR_E_ARG, "rotary: factor must be at least 1");
     if (d.scaling == MOPAR_ROTARY_NTK && d.rot_dim <= 2) return set_error(MOPAR_E_ARG, "rotary: NTK scaling needs a rot_dim above 2");
@@ -471,9 +471,9 @@ static int validate_and_build(mopar_model_s& m) {
                     !shape_eq(y, {x.dims[0], x.dims[1], h * d}))
                     return set_error(MOPAR_E_SHAPE, nm + ": causal attention needs (B,S,(heads+2*kv_heads)*head_dim) -> (B,S,heads*head_dim)");
                 if (d % 32 != 0) return set_error(MOPAR_E_UNSUPPORTED, nm + ": head_dim must be 32, 64, 96 or 128");
-                if (!(op.scale > 0.0f) || !std::isfinite(op.scale)) return set_error(MOPAR_E_ARG, nm + ": scale must be positive and finite");
-                const int64_t tokens = x.dims[0] * x.dims[1];
-                if (tokens >= (int64_t(1) << 31) || (tokens / 32 + x.dims[0]) * h >= (int64_t(1) << 31) || x.dims[2] * es >= size_t(1) << 25)
+                if (!(op.scale > 0.0f) || !std::isfinite(op.scale * 1.5f)) return set_error(MOPAR_E_ARG, nm + ": scale must be positive and at most 2^127");
+                if (x.dims[0] >= int64_t(1) << 30 || !prompt_fits(x.dims[0] * x.dims[1], static_cast<int>(x.dims[0]), x.dims[1], op.heads) ||
+                    x.dims[2] * es >= size_t(1) << 25)
                     return set_error(MOPAR_E_UNSUPPORTED, nm + ": too many rows of heads, or rows of 32 MiB");
                 break;
             }

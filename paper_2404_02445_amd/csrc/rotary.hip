@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryParams p) {
         if (sq >= 0 && sq < p.n_seq && sl >= 0 && (sl >> p.shift) < p.max_pages) {
             const int page = p.table[sq * p.table_stride + (sl >> p.shift)];
             if (page >= 0 && page < p.pages)
-                place = page * p.kv_heads * head_bytes + static_cast<int64_t>(sl & ((1 << p.shift) - 1)) * (p.tab.d * ES);
+                place = static_cast<int64_t>(page) * p.kv_heads * head_bytes + static_cast<int64_t>(sl & ((1 << p.shift) - 1)) * (p.tab.d * ES);
         }
     }
     const int total = CACHE ? p.heads + 2 * p.kv_heads : p.heads;
@@ -221,7 +221,7 @@ hipError_t rotary_launch(RotaryParams& p, hipStream_t s) {
     while (groups < total && base * groups < 256 * 1024) groups = std::min<int64_t>(total, groups * 2);
     p.groups = static_cast<int>(groups);
     const int64_t blocks = (base * groups + 255) / 256;
-    if (blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
+    if (blocks >= kMaxThreads / 256) return hipErrorInvalidConfiguration;
     const dim3 grid(static_cast<unsigned>(blocks));
     if (mode == 0)
         launch_kernel((rotary_kernel<T, 0, CACHE>), grid, dim3(256), 0, s, p);
@@ -362,7 +362,6 @@ hipError_t launch_cache_keep(const mopar_cache& c, int layers, int64_t layer_str
     p.cols = 2 * c.kv_heads * p.row_bytes / 16;
     p.col_blocks = (p.cols + 255) / 256;
     const int64_t blocks = static_cast<int64_t>(p.col_blocks) * c.n_seq * layers;
-    if (blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
     launch_kernel(keep_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, p);
     return hipGetLastError();
 }

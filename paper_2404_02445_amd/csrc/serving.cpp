@@ -28,7 +28,7 @@ int check_rows(const mopar_rows* r, const char* name, int dtype, int64_t tokens,
         return bad(nm + ": strides must be multiples of 16 bytes and not negative");
     const int64_t lim = int64_t(1) << 31;
     if (r->token_stride >= lim / (64 * es)) return set_error(MOPAR_E_UNSUPPORTED, nm + ": 64 token strides reach 2 GiB");
-    if (r->head_stride >= (int64_t(1) << 46)) return bad(nm + ": head stride");
+    if (r->head_stride >= (int64_t(1) << 44)) return bad(nm + ": head stride");      // (65536 of them: 2^62 bytes)
     if (out) {
         const bool tokens_outside = (tokens <= 1 || r->token_stride >= (heads - 1) * r->head_stride + d) &&
                                     (heads <= 1 || r->head_stride >= d);
@@ -51,8 +51,10 @@ int check_cache(const mopar_cache* c) {
     if (c->n_seq < 0) return bad("cache: n_seq");
     if (c->max_pages < 1 || c->table_stride < c->max_pages) return bad("cache: table_stride must cover max_pages, which is at least 1");
     if (static_cast<int64_t>(c->max_pages) * c->page_tokens >= (int64_t(1) << 31)) return bad("cache: 2^31 slots a sequence");
+    if (c->pages > (int64_t(1) << 46) / (static_cast<int64_t>(c->kv_heads) * c->page_tokens * c->head_dim))
+        return bad("cache: 2^46 elements and more");
     if (!aligned(c->k) || !aligned(c->v)) return bad("cache: k and v must be 16-byte aligned device pointers");
-    if (!c->table_dev) return bad("cache: table is null");
+    if (c->n_seq > 0 && !c->table_dev) return bad("cache: table is null");
     return MOPAR_OK;
 }
 
@@ -63,7 +65,7 @@ int check_attention(const mopar_attention* a) {
         return bad("attention: heads must be a multiple of kv_heads");
     if (a->head_dim != 32 && a->head_dim != 64 && a->head_dim != 96 && a->head_dim != 128)
         return set_error(MOPAR_E_UNSUPPORTED, "attention: head_dim must be 32, 64, 96 or 128");
-    if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return bad("attention: scale must be positive and finite");
+    if (!(a->scale > 0.0f) || !std::isfinite(a->scale * 1.5f)) return bad("attention: scale must be positive and at most 2^127");
     return MOPAR_OK;
 }
 
@@ -75,9 +77,16 @@ int check_cache_attention(const mopar_attention* a, const mopar_cache* c, int64_
     if (tokens < 0 || tokens >= (int64_t(1) << 31) || max_q < 0 || max_len < 1) return bad("attention: tokens, max_q or max_len");
     if (static_cast<int64_t>(max_q) * (a->heads / a->kv_heads) >= (int64_t(1) << 20))
         return set_error(MOPAR_E_UNSUPPORTED, "attention: 2^20 query rows a key head and more");
+    if (cache_limit(*c, max_len) > 1 << 30) return set_error(MOPAR_E_UNSUPPORTED, "attention: more than 2^30 slots a sequence");
     if (!attention_cache_fits(*a, c->n_seq, max_q, max_len))
-        return set_error(MOPAR_E_UNSUPPORTED, "attention: sequences, key heads and max_len make 2^30 stages and more");
+        return set_error(MOPAR_E_UNSUPPORTED, "attention: sequences, key heads, max_q and max_len make 2^22 tiles or 2^30 stages and more");
     return MOPAR_OK;
+}
+
+// ... of a launch that may need more threads than a grid has
+int launched(hipError_t e, const char* who) {
+    if (e == hipErrorInvalidConfiguration) return set_error(MOPAR_E_UNSUPPORTED, std::string(who) + ": more than 2^32 threads");
+    return hip_check(e, who);
 }
 
 }  // namespace
@@ -98,13 +107,13 @@ static int rotary_apply_impl(const mopar_rotary_s* rot, int32_t dtype, int64_t t
     if (!known_dtype(dtype)) return set_error(MOPAR_E_DTYPE, "rotary: dtype must be f32 or bf16");
     const int d = rot->tab.d;
     if (d * dtype_size(dtype) % 16 != 0) return set_error(MOPAR_E_UNSUPPORTED, "rotary: head_dim must be a multiple of 16 bytes");
-    if (tokens < 0 || heads < 0) return bad("rotary: tokens or heads");
+    if (tokens < 0 || heads < 0 || heads > 65536) return bad("rotary: tokens or heads");
     if (tokens == 0 || heads == 0) return MOPAR_OK;
     if (tokens >= (int64_t(1) << 31) / heads) return set_error(MOPAR_E_UNSUPPORTED, "rotary: 2^31 heads of tokens and more");
     if (!pos) return bad("rotary: positions are null");
     if (int e = check_rows(x, "rotary: x", dtype, tokens, heads, d, false)) return e;
     if (int e = check_rows(y, "rotary: y", dtype, tokens, heads, d, true)) return e;
-    return hip_check(launch_rotary(rot->tab, dtype, tokens, heads, heads, pos, 1, x, y, static_cast<hipStream_t>(stream)), "mopar_rotary_apply");
+    return launched(launch_rotary(rot->tab, dtype, tokens, heads, heads, pos, 1, x, y, static_cast<hipStream_t>(stream)), "mopar_rotary_apply");
 }
 
 static int cache_append_impl(const mopar_cache* c, const mopar_rotary_s* rot, int64_t tokens, int32_t heads, const int32_t* pos,
@@ -124,9 +133,9 @@ static int cache_append_impl(const mopar_cache* c, const mopar_rotary_s* rot, in
     }
     if (int e = check_rows(k, "append: k", c->dtype, tokens, c->kv_heads, c->head_dim, false)) return e;
     if (int e = check_rows(v, "append: v", c->dtype, tokens, c->kv_heads, c->head_dim, false)) return e;
-    return hip_check(launch_cache_append(*c, rot ? &rot->tab : nullptr, tokens, heads, pos, seq, slot, q, q_out, k, v,
-                                         static_cast<hipStream_t>(stream)),
-                     "mopar_cache_append");
+    return launched(launch_cache_append(*c, rot ? &rot->tab : nullptr, tokens, heads, pos, seq, slot, q, q_out, k, v,
+                                        static_cast<hipStream_t>(stream)),
+                    "mopar_cache_append");
 }
 
 static int cache_keep_impl(const mopar_cache* c, int32_t layers, int64_t layer_stride, const int32_t* len, const int32_t* offsets,
@@ -139,7 +148,7 @@ static int cache_keep_impl(const mopar_cache* c, int32_t layers, int64_t layer_s
     if (c->n_seq == 0 || layers == 0 || entries == 0 || max_path == 0) return MOPAR_OK;
     if (!len || !offsets || !path) return bad("keep: lengths, offsets or path are null");
     const int64_t blocks = (static_cast<int64_t>(2) * c->kv_heads * c->head_dim / epc + 255) / 256;
-    if (blocks * c->n_seq >= (int64_t(1) << 31) / layers) return set_error(MOPAR_E_UNSUPPORTED, "keep: too many sequences and layers");
+    if (blocks * c->n_seq >= kMaxThreads / 256 / layers) return set_error(MOPAR_E_UNSUPPORTED, "keep: too many sequences and layers");
     return hip_check(launch_cache_keep(*c, layers, layer_stride, len, offsets, entries, path, max_path, static_cast<hipStream_t>(stream)),
                      "mopar_cache_keep");
 }
@@ -149,7 +158,8 @@ static int attention_prompt_impl(const mopar_attention* a, int64_t tokens, int32
     if (int e = check_attention(a)) return e;
     if (tokens < 0 || tokens >= (int64_t(1) << 31) || n_seq < 0 || max_len < 0) return bad("attention: tokens, n_seq or max_len");
     if (tokens == 0 || n_seq == 0 || max_len == 0) return MOPAR_OK;
-    if ((tokens / 32 + n_seq) * a->heads >= (int64_t(1) << 31)) return set_error(MOPAR_E_UNSUPPORTED, "attention: too many rows of heads");
+    if (!prompt_fits(tokens, n_seq, max_len, a->heads))
+        return set_error(MOPAR_E_UNSUPPORTED, "attention: 2^30 tokens, or 2^24 tiles of 128 tokens of a sequence and head, and more");
     if (!offsets) return bad("attention: offsets are null");
     if (int e = check_rows(q, "attention: q", a->dtype, tokens, a->heads, a->head_dim, false)) return e;
     if (int e = check_rows(k, "attention: k", a->dtype, tokens, a->kv_heads, a->head_dim, false)) return e;

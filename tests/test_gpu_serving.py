@@ -423,6 +423,55 @@ def test_pools_past_32_bit_offsets():
     assert torch.equal(kc[pages - 1, :, 200], k[699]) and torch.equal(vc[pages - 1, :, 200], v[699])
 
 
+def test_more_pages_of_heads_than_32_bits_count():
+    g = gen(11)
+    kv, d, pages = 65536, 8, 32770                           # 34 GB a pool, of pages of one token
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("80 GB of memory")
+    kc, vc = (torch.empty(pages, kv, 1, d, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    cache = P.PagedCache(kc, vc, ints([[5, pages - 1, 16385, pages - 2]]))
+    k, v = randn(g, 4, kv, d), randn(g, 4, kv, d)
+    P.mopar_cache_append(cache, k, v, ints([0] * 4), ints([0, 1, 2, 3]))
+    for i, page in enumerate((5, pages - 1, 16385, pages - 2)):
+        assert torch.equal(kc[page, :, 0], k[i]) and torch.equal(vc[page, :, 0], v[i])
+    P.mopar_cache_keep(cache, ints([0]), ints([0, 2]), ints([1, 3]), 2)
+    assert torch.equal(kc[5, :, 0], k[1]) and torch.equal(vc[pages - 1, :, 0], v[3])
+    del cache, kc, vc
+    torch.cuda.empty_cache()
+
+
+def test_append_without_sequences_turns_queries():
+    g = gen(12)
+    pool = randn(g, 4, 2, 16, 64)
+    before, q, k = pool.clone(), randn(g, 3, 4, 64), randn(g, 3, 2, 64)
+    out, want = torch.empty_like(q), torch.empty_like(q)
+    cache = P.PagedCache(pool, pool.clone(), torch.empty(0, 2, device="cuda", dtype=torch.int32))
+    rot, pos = P.Rotary(64), ints([4, 5, 6])
+    P.mopar_cache_append(cache, k, k, ints([0, 0, -1]), ints([0, 1, 2]), rotary=rot, pos=pos, q=q, q_out=out)
+    P.mopar_rotary_apply(rot, q, want, pos)
+    assert torch.equal(out, want) and torch.equal(pool, before)
+
+
+@pytest.mark.parametrize("dt,lens,new", [("bf16", [500, 7], [1, 9]), ("f32", [500, 2 ** 31 - 1], [3, 1]), ("bf16", [2 ** 31 - 1, 3], [64, 64])])
+def test_a_limit_past_every_slot(dt, lens, new):
+    """max_len 2^31 - 1 and lengths to match: a sequence ends with its table's slots."""
+    g = gen(13)
+    heads, kv, d, page, slots = 4, 2, 64, 16, 640
+    table = torch.randperm(2 * slots // page, generator=g, dtype=torch.int32).view(2, -1).cuda()
+    kc, vc = (randn(g, 2 * slots // page, kv, page, d, dt=dt) for _ in range(2))
+    cache, t, top = P.PagedCache(kc, vc, table), sum(new), max(new)
+    q = randn(g, t, heads, d, dt=dt)
+    out = torch.empty_like(q)
+    most = 2 ** 31 - 1
+    P.mopar_attention_cache(q, out, cache, ints([0, new[0], t]), top, ints(lens), most, ws=P.alloc_attention_workspace(q, cache, top, most))
+    for s, (lo, n) in enumerate(zip((0, new[0]), new)):
+        total = min(lens[s] + n, slots)
+        seen = torch.arange(total)[None] <= min(lens[s], slots) + torch.arange(n)[:, None]
+        k, v = (cache_rows(x.cpu(), table.cpu(), s, total) for x in (kc, vc))
+        ref, tol = attend(q[lo:lo + n], k, v, seen, d ** -0.5)
+        check(out[lo:lo + n], ref, tol, f"sequence {s}")
+
+
 def test_streams_and_graphs():
     """Every call on a stream of its own, captured, and replayed over changed inputs with eager work between."""
     g = gen(9)

@@ -216,6 +216,34 @@ def test_cache_attention_refusals():
     assert ws_bytes(max_len=1) == (0, 0)
 
 
+def test_sizes_that_no_grid_or_offset_holds():
+    """Sizes at which an index, a byte offset or a grid would not fit are refused, and the last that fit are not."""
+    E, U = L.MOPAR_E_ARG, L.MOPAR_E_UNSUPPORTED
+    assert apply_status(heads=65537) == E and apply_status(x=rows(A, 1024, 1 << 44)) == E
+    # one pair of dims a thread: 2^30 rows of 31 units
+    assert apply_status(rot=rotary(head_dim=32, rot_dim=2), tokens=1 << 30, heads=1) == U
+    with pytest.raises(P.MoparError):
+        rotary(mscale=1e39)
+    big = cache(kv_heads=65536, page_tokens=4096, head_dim=256, pages=1 << 11)
+    assert append_status(big, k=rows(None)) == E and b"elements" in P.lib().mopar_last_error()
+    assert prompt_status(attention(scale=3e38)) == E
+    assert prompt_status(tokens=1 << 30) == U
+    assert prompt_status(attention(heads=64), n_seq=1 << 18, tokens=1 << 20) == U
+    wide = cache(page_tokens=4096, max_pages=1 << 18, table_stride=1 << 18)
+    wider = cache(page_tokens=4096, max_pages=(1 << 18) + 1, table_stride=(1 << 18) + 1)
+    assert ws_bytes(c=wide, max_len=2 ** 31 - 1)[0] == 0 and ws_bytes(c=wider, max_len=1 << 30)[0] == 0
+    assert ws_bytes(c=wider, max_len=(1 << 30) + 1)[0] == U
+    assert ws_bytes(max_len=2 ** 31 - 1)[0] == 0
+    assert ws_bytes(c=cache(n_seq=(1 << 21) - 1), max_len=1)[0] == 0 and ws_bytes(c=cache(n_seq=1 << 21), max_len=1)[0] == U
+    assert keep_status(layers=1 << 12, stride=1 << 20, c=cache(n_seq=1 << 12)) == U
+
+
+def test_a_cache_of_no_sequences_needs_no_table():
+    none = cache(n_seq=0, table_dev=None)
+    assert keep_status(none) == 0 and cache_status(c=none) == 0
+    assert append_status(none, tokens=0) == 0
+
+
 def test_binding_refuses_mismatched_tensors():
     bf = torch.bfloat16
     k = torch.zeros(4, 2, 16, 64, dtype=bf)
