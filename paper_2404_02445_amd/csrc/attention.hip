@@ -67,7 +67,8 @@ struct AttnParams {
     int mask_words;
     // over a cache: whether blocks take equal shares of all key stages (else one unit each), the least share,
     // partial sums [2 blocks][rows of a tile][head_dim] and their statistics, row tiles of a (sequence, key head)
-    int split, least;
+    // over prompts: log2 of the query heads of a tile
+    int split, least, side;
     float *part, *stat;
     CutUnit* cuts;                   // a block's: the unit that it ends and did not begin (parts 0: none)
     int row_tiles;
@@ -271,20 +272,20 @@ template <int KT, int BM> __device__ __forceinline__ bool take_share(const AttnP
     }
 }
 
-// The item-th tile of BM rows: within each 64 sequences, the tiles furthest along their sequence -- the causal
+// The item-th tile of 2^sh tokens: within each 64 sequences, the tiles furthest along their sequence -- the causal
 // ones with most keys -- first, so that the long ones start early and the short ones fill the end.
-template <int BM> __device__ __forceinline__ bool pick_tile(const AttnParams& p, int item, int lane, int& s, int& tile) {
+__device__ __forceinline__ bool pick_tile(const AttnParams& p, int sh, int item, int lane, int& s, int& tile) {
     for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
         int64_t start;
         int rows = 0;
         if (s0 + lane < p.n_seq) rows_of(p, s0 + lane, start, rows);
-        const int nt = (rows + BM - 1) / BM, all = wave_sum(nt);
+        const int nt = (rows + (1 << sh) - 1) >> sh, all = wave_sum(nt);
         if (item >= all) {
             item -= all;
             continue;
         }
         // the level of the item: at least `above` tiles lie higher, sum of (nt - level) over the taller sequences
-        int lo = 0, hi = (p.max_rows + BM - 1) / BM, above = 0;      // tiles at or past lo: > item; at or past hi: <= item
+        int lo = 0, hi = (p.max_rows + (1 << sh) - 1) >> sh, above = 0;      // tiles at or past lo: > item; at or past hi: <= item
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2, n = wave_sum(max(nt - mid, 0));
             if (n > item) lo = mid; else hi = mid, above = n;
@@ -353,7 +354,7 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
     }
     for (;;) {
         int64_t start;
-        int rows, kvh, head = 0, tile, past = 0, total, key0 = 0, key1, slot = 0, took = 0;
+        int rows, kvh, head = 0, tile, row0, wave0, past = 0, total, key0 = 0, key1, slot = 0, took = 0;
         bool whole = true;                            // no other block has keys of these rows
         if constexpr (PAGED) {
             start = sq.start;
@@ -363,6 +364,8 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             const int row_tiles = sq.units / p.kv_heads, unit = (g - base) / sq.nt, t0 = g - base - unit * sq.nt;
             kvh = unit / row_tiles;
             tile = unit - kvh * row_tiles;
+            row0 = tile * BM;
+            wave0 = row0 + wave * 32;
             took = min(sq.nt - t0, gend - g);
             key0 = t0 * KT;
             key1 = min(total, key0 + took * KT);
@@ -371,28 +374,31 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             if (t0 > 0 && t0 + took == sq.nt && threadIdx.x == 0) {
                 const int first = (g - t0) / per;
                 args_again()->cuts[blockIdx.x] =
-                    CutUnit{static_cast<int>(blockIdx.x) - first + 1, first, min(BM, rows * p.group - tile * BM), tile * BM, kvh, 0, start};
+                    CutUnit{static_cast<int>(blockIdx.x) - first + 1, first, min(BM, rows * p.group - row0), row0, kvh, 0, start};
             }
         } else {
-            // key heads fastest: the XCDs take blocks round-robin, so the query heads of a key head meet in one L2
-            const int hi = blockIdx.x % p.heads, gi = hi / p.kv_heads;
+            // a tile is 2^side heads of a key head by BM >> side tokens, a wave 32 tokens of one head.  Key heads fastest: the
+            // XCDs take blocks round-robin, so the query heads of a key head meet in one L2
+            const int sets = p.heads >> p.side, hi = blockIdx.x % sets, gi = hi / p.kv_heads;
             kvh = hi - gi * p.kv_heads;
-            head = kvh * p.group + gi;
-            if (!pick_tile<BM>(p, blockIdx.x / p.heads, lane, s, tile)) return;
+            head = kvh * p.group + (gi << p.side) + (wave & ((1 << p.side) - 1));
+            constexpr int kShift = __builtin_ctz(BM);
+            if (!pick_tile(p, kShift - p.side, blockIdx.x / sets, lane, s, tile)) return;
             s = uniform(s);
             tile = uniform(tile);
             rows_of(p, s, start, rows);
             start = uniform(start);
             rows = uniform(rows);
             total = rows;
-            key1 = min(total, (tile + 1) * BM);
+            row0 = tile << (kShift - p.side);
+            wave0 = row0 + (wave >> p.side) * 32;
+            key1 = min(total, row0 + (BM >> p.side));
         }
         const int group = PAGED ? p.group : 1;
         const int nrow = rows * group;                // query rows: tokens, times the heads of a group over a cache
-        const int row0 = tile * BM;
 
         // --- this wave's rows: row lr of its 32 (past the last: that one again, never stored) ------------
-        const int row = min(row0 + wave * 32 + lr, nrow - 1);
+        const int row = min(wave0 + lr, nrow - 1);
         const int qtok = PAGED ? row / group : row;   // the row's token within the sequence
         const int qhead = PAGED ? kvh * group + (row - qtok * group) : head;
         u32x4 qf[CH / 2];
@@ -732,7 +738,6 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
 
         // --- the keys ----------------------------------------------------------------------------------
         // Of this wave's rows: the keys that all of them see, and the end of those that any sees.
-        const int wave0 = row0 + wave * 32;
         const int all_see = PAGED ? past : wave0 + 1;
         const int wave_end = PAGED ? (wave0 < nrow ? key1 : key0) : min(key1, wave0 + 32);
         int k0 = key0, at = 0;                        // the stage at hand and its place
@@ -836,7 +841,7 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         // --- results -----------------------------------------------------------------------------------
         l += other_half(l);
         const ArgsPtr ar = args_again();
-        if (row0 + wave * 32 + lr < nrow) {
+        if (wave0 + lr < nrow) {
             if (whole) {
                 const float inv = l != 0.0f ? 1.0f / l : 0.0f;
                 unsigned char* dst = ar->out + (start + qtok) * ar->o_ts + qhead * ar->o_hs;
@@ -1007,7 +1012,8 @@ hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int
     p.kv_heads = a.kv_heads;
     p.group = a.heads / a.kv_heads;
     p.c = a.scale * 1.44269504088896341f;
-    const dim3 grid(static_cast<unsigned>(prompt_tiles(tokens, n_seq, max_len) * a.heads));
+    p.side = p.group % 4 == 0 ? 2 : p.group % 2 == 0 ? 1 : 0;
+    const dim3 grid(static_cast<unsigned>(prompt_tiles(tokens, n_seq, max_len, 128 >> p.side) * (a.heads >> p.side)));
     return by_type(a.dtype, a.head_dim, [&](auto t, auto d) {
         using T = decltype(t);
         launch_kernel((attention_kernel<T, d, 4, sizeof(T) == 2 ? 2 : 1, 2, false>), grid, dim3(256), 0, s, p);

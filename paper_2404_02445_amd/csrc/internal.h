@@ -238,14 +238,14 @@ hipError_t launch_cache_keep(const mopar_cache& c, int layers, int64_t layer_str
 __attribute__((weak)) hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int n_seq, const int32_t* offsets, int max_len,
                                    const mopar_rows* q, const mopar_rows* k, const mopar_rows* v, const mopar_rows* out,
                                    hipStream_t s);
-// Its tiles of 128 rows: no more than the tokens fill and one more a sequence.
-inline int64_t prompt_tiles(int64_t tokens, int n_seq, int64_t max_len) {
-    return std::min(tokens / 128 + n_seq, n_seq * ((max_len + 127) / 128));
+// Its tiles of so many tokens of a sequence: no more than the tokens fill and one more a sequence.
+inline int64_t prompt_tiles(int64_t tokens, int n_seq, int64_t max_len, int size) {
+    return std::min(tokens / size + n_seq, n_seq * ((max_len + size - 1) / size));
 }
 // threads of a grid at most
 constexpr int64_t kMaxThreads = int64_t(1) << 32;
 inline bool prompt_fits(int64_t tokens, int n_seq, int64_t max_len, int heads) {
-    return tokens < int64_t(1) << 30 && prompt_tiles(tokens, n_seq, max_len) < kMaxThreads / 256 / heads;
+    return tokens < int64_t(1) << 30 && prompt_tiles(tokens, n_seq, max_len, 128) < kMaxThreads / 256 / heads;
 }
 // Tokens of a sequence at most: max_len and the slots of the table.
 inline int cache_limit(const mopar_cache& c, int max_len) {
