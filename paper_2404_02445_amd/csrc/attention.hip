@@ -894,42 +894,46 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p)
     typedef float fv __attribute__((ext_vector_type(PER)));
     auto at = [&](int k) { return static_cast<int64_t>(2 * (u.first + k) + (k == 0)) * BM; };
     if (u.parts == 0) return;
-    for (int rr = blockIdx.y * 4 + (threadIdx.x >> 6); rr < u.rows; rr += gridDim.y * 4) {
-        float top = kNoMax, sum = 0.0f;
-        for (int k0 = 0; k0 < u.parts; k0 += 64)
-            top = fmaxf(top, k0 + lane < u.parts ? p.stat[2 * (at(k0 + lane) + rr)] : kNoMax);
+    // `many` loads in flight: 16, or four where there are no more parts (a tree's tile of a sequence)
+    auto join = [&](auto many) __attribute__((always_inline)) {
+        for (int rr = blockIdx.y * 4 + (threadIdx.x >> 6); rr < u.rows; rr += gridDim.y * 4) {
+            float top = kNoMax, sum = 0.0f;
+            for (int k0 = 0; k0 < u.parts; k0 += 64)
+                top = fmaxf(top, k0 + lane < u.parts ? p.stat[2 * (at(k0 + lane) + rr)] : kNoMax);
 #pragma unroll
-        for (int i = 1; i < 64; i *= 2) top = fmaxf(top, __shfl_xor(top, i, 64));
-        float acc[PER] = {};
-        for (int k0 = 0; k0 < u.parts; k0 += 64) {
-            float f = 0.0f;                           // this lane's part: its weight
-            if (k0 + lane < u.parts) {
-                f = __builtin_amdgcn_exp2f(p.stat[2 * (at(k0 + lane) + rr)] - top);
-                sum += p.stat[2 * (at(k0 + lane) + rr) + 1] * f;
-            }
-            const int n = min(64, u.parts - k0);
-            for (int k = 0; k < n; k += 16) {
-                fv v[16];
+            for (int i = 1; i < 64; i *= 2) top = fmaxf(top, __shfl_xor(top, i, 64));
+            float acc[PER] = {};
+            for (int k0 = 0; k0 < u.parts; k0 += 64) {
+                float f = 0.0f;                           // this lane's part: its weight
+                if (k0 + lane < u.parts) {
+                    f = __builtin_amdgcn_exp2f(p.stat[2 * (at(k0 + lane) + rr)] - top);
+                    sum += p.stat[2 * (at(k0 + lane) + rr) + 1] * f;
+                }
+                const int n = min(64, u.parts - k0);
+                for (int k = 0; k < n; k += many) {
+                    fv v[many];
 #pragma unroll
-                for (int i = 0; i < 16; ++i)           // (past the last part: that one again, with weight 0)
-                    if (lane < LANES) v[i] = *reinterpret_cast<const fv*>(p.part + (at(min(k0 + k + i, u.parts - 1)) + rr) * D + lane * PER);
+                    for (int i = 0; i < many; ++i)           // (past the last part: that one again, with weight 0)
+                        if (lane < LANES) v[i] = *reinterpret_cast<const fv*>(p.part + (at(min(k0 + k + i, u.parts - 1)) + rr) * D + lane * PER);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float w = __shfl(f, min(k + i, 63), 64);
+                    for (int i = 0; i < many; ++i) {
+                        const float w = __shfl(f, min(k + i, 63), 64);
 #pragma unroll
-                    for (int e = 0; e < PER; ++e) acc[e] += k + i < n ? v[i][e] * w : 0.0f;
+                        for (int e = 0; e < PER; ++e) acc[e] += k + i < n ? v[i][e] * w : 0.0f;
+                    }
                 }
             }
+#pragma unroll
+            for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i, 64);
+            const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+            const int row = u.row0 + rr, tok = row / p.group, h = u.kvh * p.group + (row - tok * p.group);
+            T* dst = reinterpret_cast<T*>(p.out + (u.start + tok) * p.o_ts + h * p.o_hs);
+            if (lane < LANES)
+#pragma unroll
+                for (int e = 0; e < PER; ++e) dst[lane * PER + e] = static_cast<T>(acc[e] * inv);
         }
-#pragma unroll
-        for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i, 64);
-        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-        const int row = u.row0 + rr, tok = row / p.group, h = u.kvh * p.group + (row - tok * p.group);
-        T* dst = reinterpret_cast<T*>(p.out + (u.start + tok) * p.o_ts + h * p.o_hs);
-        if (lane < LANES)
-#pragma unroll
-            for (int e = 0; e < PER; ++e) dst[lane * PER + e] = static_cast<T>(acc[e] * inv);
-    }
+    };
+    if (u.parts <= 4) join(std::integral_constant<int, 4>{}); else join(std::integral_constant<int, 16>{});
 }
 
 void set_rows(AttnParams& p, int es, const mopar_rows* q, const mopar_rows* out) {
@@ -1066,7 +1070,7 @@ hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c
             launch_kernel(kernel, grid, dim3(threads), 0, s, p);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess || !cp.split) return e;
-            launch_kernel(join, dim3(grid.x, cp.bm / 16), dim3(256), 0, s, p);
+            launch_kernel(join, dim3(grid.x, cp.bm / 8), dim3(256), 0, s, p);
             return hipGetLastError();
         };
         auto of = [&](auto wr) {
