@@ -273,13 +273,14 @@ template <int KT, int BM> __device__ __forceinline__ bool take_share(const AttnP
 }
 
 // The item-th tile of 2^sh tokens: within each 64 sequences, the tiles furthest along their sequence -- the causal
-// ones with most keys -- first, so that the long ones start early and the short ones fill the end.
-__device__ __forceinline__ bool pick_tile(const AttnParams& p, int sh, int item, int lane, int& s, int& tile) {
+// ones with most keys -- first, so that the long ones start early and the short ones fill the end.  With its
+// sequence's rows.
+__device__ __forceinline__ bool pick_tile(const AttnParams& p, int sh, int item, int lane, int& tile, int64_t& start, int& rows) {
     for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
-        int64_t start;
-        int rows = 0;
-        if (s0 + lane < p.n_seq) rows_of(p, s0 + lane, start, rows);
-        const int nt = (rows + (1 << sh) - 1) >> sh, all = wave_sum(nt);
+        int64_t first = 0;
+        int n = 0;
+        if (s0 + lane < p.n_seq) rows_of(p, s0 + lane, first, n);
+        const int nt = (n + (1 << sh) - 1) >> sh, all = wave_sum(nt);
         if (item >= all) {
             item -= all;
             continue;
@@ -287,15 +288,18 @@ __device__ __forceinline__ bool pick_tile(const AttnParams& p, int sh, int item,
         // the level of the item: at least `above` tiles lie higher, sum of (nt - level) over the taller sequences
         int lo = 0, hi = (p.max_rows + (1 << sh) - 1) >> sh, above = 0;      // tiles at or past lo: > item; at or past hi: <= item
         while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2, n = wave_sum(max(nt - mid, 0));
-            if (n > item) lo = mid; else hi = mid, above = n;
+            const int mid = (lo + hi) / 2, higher = wave_sum(max(nt - mid, 0));
+            if (higher > item) lo = mid; else hi = mid, above = higher;
         }
         const uint64_t have = __ballot(nt > lo);
         const int rank = item - above;
         const uint64_t below = have & ((uint64_t(1) << lane) - 1);
         const uint64_t hit = __ballot(((have >> lane) & 1) && __popcll(below) == rank);
-        s = __builtin_amdgcn_readfirstlane(s0 + static_cast<int>(__builtin_ctzll(hit)));
-        tile = __builtin_amdgcn_readfirstlane(lo);
+        const int at = uniform(static_cast<int>(__builtin_ctzll(hit)));
+        tile = uniform(lo);
+        start = static_cast<int64_t>(static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(first >> 32), at))) << 32 |
+                                     static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(first), at)));
+        rows = __builtin_amdgcn_readlane(n, at);
         return true;
     }
     return false;
@@ -383,12 +387,7 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             kvh = hi - gi * p.kv_heads;
             head = kvh * p.group + (gi << p.side) + (wave & ((1 << p.side) - 1));
             constexpr int kShift = __builtin_ctz(BM);
-            if (!pick_tile(p, kShift - p.side, blockIdx.x / sets, lane, s, tile)) return;
-            s = uniform(s);
-            tile = uniform(tile);
-            rows_of(p, s, start, rows);
-            start = uniform(start);
-            rows = uniform(rows);
+            if (!pick_tile(p, kShift - p.side, blockIdx.x / sets, lane, tile, start, rows)) return;
             total = rows;
             row0 = tile << (kShift - p.side);
             wave0 = row0 + (wave >> p.side) * 32;

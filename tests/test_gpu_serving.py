@@ -205,6 +205,17 @@ def test_prompt_heads(dt, heads, kv):
     check_prompt(prompt(q, k, v, lens), q, k, v, lens)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv,d", [(4, 2, 64), (8, 2, 128), (12, 2, 32), (24, 3, 96)])
+def test_prompt_groups_of_two_and_four_heads(dt, heads, kv, d):
+    """Tiles of two or four heads of a key head, and lengths round their 64 and 32 tokens."""
+    g = gen(heads + d)
+    lens = [33, 0, 129, 1, 64, 31, 96]
+    t = sum(lens) + 2
+    q, k, v = randn(g, t, heads, d, dt=dt), randn(g, t, kv, d, dt=dt), randn(g, t, kv, d, dt=dt)
+    check_prompt(prompt(q, k, v, lens), q, k, v, lens)
+
+
 def test_prompt_long():
     g = gen(5)
     n = 4500
@@ -256,6 +267,21 @@ def test_prompt_hidden_values_do_not_reach_a_row(dt):
     rest[2:, 63] = 0
     assert bool(torch.isfinite(rest).all())
     check_prompt(torch.cat([out[140:190], out[190:]]), q[140:], k[140:], v[140:], [50])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_prompt_hidden_values_in_grouped_heads(dt):
+    """Infinities and NaN reach the same dims of the same rows whether a key head is shared or given once a head."""
+    g = gen(10)
+    q, k, v = randn(g, 150, 4, 64, dt=dt), randn(g, 150, 1, 64, dt=dt), randn(g, 150, 1, 64, dt=dt)
+    v[33, 0, 3], v[70, 0, 5], v[149, 0, 1] = float("inf"), float("nan"), float("-inf")
+    k[95, 0, 7] = float("nan")
+    k4, v4 = k.expand(150, 4, 64).contiguous(), v.expand(150, 4, 64).contiguous()
+    for n in (2, 4):
+        out, each = prompt(q[:, :n], k, v, [150]), prompt(q[:, :n], k4[:, :n], v4[:, :n], [150])
+        for kind in (torch.isnan, torch.isposinf, torch.isneginf):
+            assert torch.equal(kind(out), kind(each))
+        assert bool(torch.isfinite(out[:33]).all()) and bool((out[33:95, :, 3] == float("inf")).all())
 
 
 def test_prompt_offsets_out_of_bounds_are_cut():
