@@ -65,10 +65,10 @@ struct AttnParams {
     int shift, max_len;              // max_len: at most the slots of the table, at most 2^30
     const uint64_t* mask;
     int mask_words;
-    // over a cache: whether blocks take equal shares of all key stages (else one unit each), the least share,
+    // over a cache: whether blocks take equal shares of all key stages (else one unit each),
     // partial sums [2 blocks][rows of a tile][head_dim] and their statistics, row tiles of a (sequence, key head)
     // over prompts: log2 of the query heads of a tile
-    int split, least, side;
+    int split, side;
     float *part, *stat;
     CutUnit* cuts;                   // a block's: the unit that it ends and did not begin (parts 0: none)
     int row_tiles;
@@ -249,7 +249,7 @@ template <int KT, int BM> __device__ __forceinline__ bool take_share(const AttnP
     const int head = stages(lane);                     // the first 64 sequences are looked up once
     int all = wave_sum(head);
     for (int s0 = 64; s0 < p.n_seq; s0 += 64) all += wave_sum(stages(s0 + lane));
-    sh.per = max(p.least, static_cast<int>((all + gridDim.x - 1) / gridDim.x));
+    sh.per = static_cast<int>((all + gridDim.x - 1) / gridDim.x);
     if (static_cast<int64_t>(blockIdx.x) * sh.per >= all) return false;
     sh.g = blockIdx.x * sh.per;
     sh.gend = min(all, sh.g + sh.per);
@@ -962,25 +962,32 @@ struct CachePlan {
     int bm, kt, row_tiles, split, blocks;
     int64_t slots_bytes;
 };
-constexpr int kLeastStages = 2;
-// stages in the ring of a block of 64 to 256 rows: as many as 64 KB hold (128 KB of 256 rows), two to four
-constexpr int ring_of(int wr, int stage_bytes) {
-    const int room = (wr == 8 ? 128 : 64) * 1024 / stage_bytes;
-    return wr == 1 ? 2 : room >= 4 ? 4 : 2;
-}
+// Stages in a block's ring: two, and four in 64-row blocks where they fill 64 KB (head dims of 256 bytes).  16 sequences of
+// 4.5k tokens, 32 heads of 128 on 8, bf16: 16 drafted tokens 97 -> 92 us with four (of 64 dims: 53 -> 54), 48 (256-row
+// blocks) 142 us with either.
+constexpr int ring_of(int wr, int stage_bytes) { return wr == 2 && stage_bytes == 16384 ? 4 : 2; }
 CachePlan cache_plan(const mopar_attention& a, int n_seq, int max_q, int max_len) {
     CachePlan c{};
     const int64_t rows = static_cast<int64_t>(max_q) * (a.heads / a.kv_heads);
-    c.bm = rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-    c.kt = a.dtype == MOPAR_BF16 && c.bm >= 128 ? 64 : 32;
+    // Tiles hold a key head's query rows where 256 do, so that its keys are read once; small ones where few rows leave
+    // most of a tile idle.  The same sequences: single tokens 122 us in tiles of 32 rows and 131 of 64; 16 drafted tokens
+    // (64 rows) 92 us in 64 and 94 in 128; 32 (128 rows) 154 us in 64, 115 in 128, 110 in 256, so there are none of 128.
+    c.bm = rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
+    // 64 keys a stage in the large tiles in bf16: 32 of them cost 6 % (two tiles' scores for one rescale); float32 has not
+    // the registers
+    c.kt = a.dtype == MOPAR_BF16 && c.bm == 256 ? 64 : 32;
     c.row_tiles = static_cast<int>((rows + c.bm - 1) / c.bm);
-    // blocks that a CU holds at once, by LDS and two waves a SIMD
+    // blocks that the card holds at once, by LDS and two waves a SIMD
     const int stage = 2 * c.kt * (a.head_dim > 64 ? 128 : a.head_dim) * static_cast<int>(dtype_size(a.dtype));
-    const int per_cu = std::min(256 / c.bm, 160 * 1024 / (ring_of(c.bm / 32, stage) * stage + c.bm / 32 * 1024));
+    const int64_t slots = 256 * std::min(256 / c.bm, 160 * 1024 / (ring_of(c.bm / 32, stage) * stage + c.bm / 32 * 1024));
     const int64_t units = static_cast<int64_t>(n_seq) * a.kv_heads * c.row_tiles, nt = (static_cast<int64_t>(max_len) + c.kt - 1) / c.kt;
-    c.split = nt > 2 * kLeastStages;
-    const int64_t blocks = c.split ? std::min<int64_t>(256 * per_cu, units * nt) : units;
-    c.blocks = static_cast<int>(std::min<int64_t>(blocks, int64_t(1) << 30));
+    // Equal shares, with partial sums and a second launch to join them, where they save more stages on the longest path
+    // than the join costs: about 9 of bf16 (1 to 2 us each), 4 of float32 (3 us).  64 single tokens over 600: 42 us in
+    // shares, 34 with a unit a block; 8 over 200: 14 and 13, over 400: 16 and 20; a float32 one over 100: 16 and 16,
+    // over 200: 16 and 25; 16 drafts of 20 to 48 over 200 to 800: 47 and 34.
+    const int64_t saved = nt * ((units + slots - 1) / slots) - (nt * units + slots - 1) / slots;
+    c.split = saved > (a.dtype == MOPAR_BF16 ? 9 : 4);
+    c.blocks = static_cast<int>(std::min<int64_t>(c.split ? std::min(slots, units * nt) : units, int64_t(1) << 30));
     c.slots_bytes = c.split ? c.blocks * (int64_t(2) * c.bm * (a.head_dim + 2) * 4 + static_cast<int64_t>(sizeof(CutUnit))) : 0;
     return c;
 }
@@ -1056,7 +1063,6 @@ hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c
     const CachePlan cp = cache_plan(a, c.n_seq, max_q, max_len);
     p.row_tiles = cp.row_tiles;
     p.split = cp.split;
-    p.least = kLeastStages;
     p.part = static_cast<float*>(ws);
     if (cp.split) {
         p.stat = p.part + int64_t(2) * cp.blocks * cp.bm * a.head_dim;
@@ -1073,12 +1079,11 @@ hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c
             return hipGetLastError();
         };
         auto of = [&](auto wr) {
-            constexpr int WR = wr, SUBS = sizeof(T) == 2 && WR >= 4 ? 2 : 1, STAGE = 2 * 32 * SUBS * Geo<T, d>::RB;
+            constexpr int WR = wr, SUBS = sizeof(T) == 2 && WR == 8 ? 2 : 1, STAGE = 2 * 32 * SUBS * Geo<T, d>::RB;
             return go(attention_kernel<T, d, WR, SUBS, ring_of(WR, STAGE), true>, attention_join_kernel<T, d, WR * 32>, WR * 64);
         };
         if (cp.bm == 32) return of(std::integral_constant<int, 1>{});
         if (cp.bm == 64) return of(std::integral_constant<int, 2>{});
-        if (cp.bm == 128) return of(std::integral_constant<int, 4>{});
         return of(std::integral_constant<int, 8>{});
     });
 }

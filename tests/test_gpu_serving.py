@@ -381,6 +381,13 @@ def test_cache_split_over_a_long_axis(dt, d):
     over_cache(g, dt, 4, 2, d, 16, [3000, 3, 513], [9, 20, 12], lambda n: tree_mask(n, g)[0])
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [[1, 1, 0, 1, 1], [16, 3, 0, 9, 1], [40, 2, 0, 64, 17]])
+def test_short_sequences_under_a_far_limit(dt, new):
+    """A limit that lets the blocks share the work, on sequences that fill a few of the shares."""
+    over_cache(gen(14), dt, 8, 2, 64, 16, [70, 0, 33, 1, 300], new, lambda n: tree_mask(n, gen(n))[0] if n else causal(0), spare=3, max_len=200000)
+
+
 def test_absent_pages_are_not_visible():
     for bad in (-1, 10 ** 9):
         over_cache(gen(5), "bf16", 4, 2, 64, 16, [300, 40], [3, 2], None, absent=(0, 4, bad))
