@@ -8,9 +8,30 @@
 // -- the k index of an MFMA may run over the keys in any order that both operands share, so P never leaves the
 // registers.  V^T fragments come from row-major V in LDS by transposing reads (bf16) or element reads (float32).
 //
-// Keys and values stream to LDS with 16-byte direct loads, two stages (K, K, V, V); a row of LDS is the head's dims, a power
-// of two of 16-byte chunks, chunk c of row r at place c ^ f(r) (swizzle()), which keeps both the fragment reads
-// of K (32 rows, one chunk) and those of V (four rows, 64 bytes) off each other's banks.
+// Keys and values stream through a ring of stages in LDS (all K, then all V) by 16-byte direct loads; a row of LDS is the
+// head's dims, a power of two of 16-byte chunks, chunk c of row r at place c ^ f(r) (swizzle()), which keeps both the
+// fragment reads of K (32 rows, one chunk) and those of V (four rows, 64 bytes) off each other's banks.
+//
+// Softmax.  Weights are 2^(s c - m), c = scale log2(e), with m at most 8 below the row's running maximum (they stay under
+// 2^8, far from overflow in float32 and in bf16's exponent), so the accumulators are rescaled only where a maximum rises by
+// more.  Sums are taken in float32 before the weights are rounded to bf16 for the second product: that rounding (2^-8
+// relative, at most) is the one that the matrix instruction's operand needs.
+//
+// Stages that every row of a block sees whole run without masks, their tiles together and LDS reads ahead of the MFMAs
+// (`full`, bf16); the others -- the causal edge, the drafts' own keys, the last keys, absent pages -- run tile by tile with
+// a mask (`tile32`).  float32 has its MFMAs at a tenth of bf16's rate and runs on tile32 alone.
+//
+// Measured, with what bounds it (32 heads of 128 on 8 key heads in bf16; copies reach 5.0 TB/s here, large bf16 products 1450
+// TFLOP/s):
+//   8192 causal tokens: 510 to 550 us, 1000 to 1080 TFLOP/s.  Matrix units busy half of the time, vector units 57 %: two
+//     waves a SIMD (the registers of 32 rows x 128 dims) hide each other's softmax only in part.  Deeper LDS prefetch,
+//     32-key stages (584 us) and products issued a stage ahead of the softmax (593 us) did not help.
+//   16 prompts of 20 to 1100 tokens: 139 us; 48 us of copying and 80 us of products that blocks of the same length, started
+//     together, do not overlap.
+//   64 single tokens over 100 to 4096 cached ones: 121 us, 4.5 TB/s: memory.
+//   16 trees of 20 to 48 over 1000 to 8000: 115 to 122 us, 2.9 TB/s and 390 TFLOP/s at once; 17 us of it the join.
+//   One float32 token over 16400, 12 heads of 64: 38 us, 2.6 TB/s: a wave's float32 products for 32 rows of which one counts
+//     (12 us) behind its loads, and the join (7 us).
 #include <algorithm>
 #include <type_traits>
 
@@ -65,10 +86,10 @@ struct AttnParams {
     int shift, max_len;              // max_len: at most the slots of the table, at most 2^30
     const uint64_t* mask;
     int mask_words;
-    // over a cache: whether blocks take equal shares of all key stages (else one unit each),
-    // partial sums [2 blocks][rows of a tile][head_dim] and their statistics, row tiles of a (sequence, key head)
-    // over prompts: log2 of the query heads of a tile
-    int split, side;
+    int side;                        // over prompts: log2 of the query heads of a tile
+    // over a cache: whether blocks take equal shares of all key stages (else one unit each), partial sums
+    // [2 blocks][rows of a tile][head_dim] and their statistics, row tiles of a (sequence, key head)
+    int split;
     float *part, *stat;
     CutUnit* cuts;                   // a block's: the unit that it ends and did not begin (parts 0: none)
     int row_tiles;
@@ -1022,6 +1043,9 @@ hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int
     p.kv_heads = a.kv_heads;
     p.group = a.heads / a.kv_heads;
     p.c = a.scale * 1.44269504088896341f;
+    // As many heads of a key head to a tile as its four waves take: the causal edge then meets every wave alike, and the
+    // heads share their keys' loads.  16 prompts of 20 to 1100 tokens, 4 heads a key head: 151 -> 141 us (against one head
+    // by 128 tokens), of 20 to 400 38 -> 31 us, one of 8192 the same.
     p.side = p.group % 4 == 0 ? 2 : p.group % 2 == 0 ? 1 : 0;
     const dim3 grid(static_cast<unsigned>(prompt_tiles(tokens, n_seq, max_len, 128 >> p.side) * (a.heads >> p.side)));
     return by_type(a.dtype, a.head_dim, [&](auto t, auto d) {

@@ -1,6 +1,9 @@
 // Rotary positions and the paged cache's writes (gfx950): turning the heads of packed token rows, the
 // same on the way into the cache, and moving the accepted tokens of a drafted tree.  All three read and
-// write each byte once and are bound by HBM, or by a launch when there are few tokens.
+// write each byte once and are bound by HBM, or by a launch when there are few tokens.  Measured (a copy reaches 5.0 TB/s
+// here): 16384 tokens of 40 heads of 128 in bf16 turned in 73 us, 4.6 TB/s; 22k tokens of 32 + 8 + 8 heads turned and
+// stored in 119 us, 4.55 TB/s; eight tokens in 5 us, a launch and two loads in a row; 4 kept tokens in 5 us, 32 sequences'
+// in 16 layers (22 MB) in 11 us: five loads, each of which waits for the one before (offset, path, page, row).
 //
 // Rotation.  Pair j of a token at position p turns by p w_j.  The host keeps w_j / 2 pi as a 64-bit
 // fraction of a turn, so p times it, wrapped to 64 bits, is the angle modulo a turn: exact range
@@ -215,7 +218,8 @@ hipError_t rotary_launch(RotaryParams& p, hipStream_t s) {
         p.units = rot / 2 + (d - rot);
     }
     const int total = CACHE ? p.heads + 2 * p.kv_heads : p.heads;
-    // threads that share a token's heads: eight heads a thread, fewer while the threads would not fill the card
+    // Threads that share a token's heads: eight heads a thread, so that an angle serves eight (22k tokens stored: 119 us,
+    // 147 with a head a thread), fewer while the threads would not fill the card (eight tokens: 7.4 us with eight, 5.0)
     const int64_t base = p.tokens * p.units;
     int64_t groups = (total + 7) / 8;
     while (groups < total && base * groups < 256 * 1024) groups = std::min<int64_t>(total, groups * 2);
