@@ -292,8 +292,9 @@ int mopar_attention_prompt(const mopar_attention* a, int64_t tokens, int32_t n_s
  * NULL: tokens j <= i (one new token, or a chain of them).  A row that sees nothing
  * gets zeros.  max_len >= 1 bounds len + drafted tokens; slots from max_len on are not
  * read.  `ws` holds mopar_attention_cache_workspace_bytes; its contents need not
- * survive between calls, and calls that overlap need one each.  out must not overlap q;
- * drafted rows past max_q are left as they are.
+ * survive between calls, and calls that overlap need one each.  The size does not fall
+ * as n_seq, tokens, max_q or max_len grow, so the largest call's workspace serves the
+ * smaller ones.  out must not overlap q; drafted rows past max_q are left as they are.
  * Errors: MOPAR_E_ARG (also a mask of fewer than ceil(max_q / 64) words),
  * MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (head_dim; heads / kv_heads * max_q of 2^20
  * and more; n_seq * kv_heads * max_q so large that their tiles of 32 to 256 rows reach

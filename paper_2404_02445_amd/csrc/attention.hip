@@ -981,19 +981,21 @@ template <typename F> hipError_t by_type(int dtype, int d, F&& go) {
 // whether the blocks take equal shares of the stages.
 struct CachePlan {
     int bm, kt, row_tiles, split, blocks;
-    int64_t slots_bytes;
+    int64_t shared_bytes;              // the workspace of equal shares
 };
 // Stages in a block's ring: two, and four in 64-row blocks where they fill 64 KB (head dims of 256 bytes).  16 sequences of
 // 4.5k tokens, 32 heads of 128 on 8, bf16: 16 drafted tokens 97 -> 92 us with four (of 64 dims: 53 -> 54), 48 (256-row
 // blocks) 142 us with either.
 constexpr int ring_of(int wr, int stage_bytes) { return wr == 2 && stage_bytes == 16384 ? 4 : 2; }
-CachePlan cache_plan(const mopar_attention& a, int n_seq, int max_q, int max_len) {
+// Tiles hold a key head's query rows where 256 do, so that its keys are read once; small ones where few rows leave most of
+// a tile idle.  The same sequences: single tokens 122 us in tiles of 32 rows and 131 of 64; 16 drafted tokens (64 rows) 92 us
+// in 64 and 94 in 128; 32 (128 rows) 154 us in 64, 115 in 128, 110 in 256, so there are none of 128.
+int tile_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 256; }
+// Stages that equal shares must save to be taken: see cache_plan.
+int join_stages(const mopar_attention& a) { return a.dtype == MOPAR_BF16 ? 9 : 4; }
+CachePlan plan_of(const mopar_attention& a, int n_seq, int64_t rows, int max_len) {
     CachePlan c{};
-    const int64_t rows = static_cast<int64_t>(max_q) * (a.heads / a.kv_heads);
-    // Tiles hold a key head's query rows where 256 do, so that its keys are read once; small ones where few rows leave
-    // most of a tile idle.  The same sequences: single tokens 122 us in tiles of 32 rows and 131 of 64; 16 drafted tokens
-    // (64 rows) 92 us in 64 and 94 in 128; 32 (128 rows) 154 us in 64, 115 in 128, 110 in 256, so there are none of 128.
-    c.bm = rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
+    c.bm = tile_rows(rows);
     // 64 keys a stage in the large tiles in bf16: 32 of them cost 6 % (two tiles' scores for one rescale); float32 has not
     // the registers
     c.kt = a.dtype == MOPAR_BF16 && c.bm == 256 ? 64 : 32;
@@ -1007,11 +1009,13 @@ CachePlan cache_plan(const mopar_attention& a, int n_seq, int max_q, int max_len
     // shares, 34 with a unit a block; 8 over 200: 14 and 13, over 400: 16 and 20; a float32 one over 100: 16 and 16,
     // over 200: 16 and 25; 16 drafts of 20 to 48 over 200 to 800: 47 and 34.
     const int64_t saved = nt * ((units + slots - 1) / slots) - (nt * units + slots - 1) / slots;
-    c.split = saved > (a.dtype == MOPAR_BF16 ? 9 : 4);
+    c.split = saved > join_stages(a);
     c.blocks = static_cast<int>(std::min<int64_t>(c.split ? std::min(slots, units * nt) : units, int64_t(1) << 30));
-    c.slots_bytes = c.split ? c.blocks * (int64_t(2) * c.bm * (a.head_dim + 2) * 4 + static_cast<int64_t>(sizeof(CutUnit))) : 0;
+    c.shared_bytes = std::min(slots, units * nt) * (int64_t(2) * c.bm * (a.head_dim + 2) * 4 + static_cast<int64_t>(sizeof(CutUnit)));
     return c;
 }
+int64_t query_rows(const mopar_attention& a, int max_q) { return static_cast<int64_t>(max_q) * (a.heads / a.kv_heads); }
+CachePlan cache_plan(const mopar_attention& a, int n_seq, int max_q, int max_len) { return plan_of(a, n_seq, query_rows(a, max_q), max_len); }
 
 }  // namespace
 
@@ -1055,8 +1059,14 @@ hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int
     });
 }
 
+// What this call or one of fewer sequences, drafted tokens or keys may take (a smaller call may share where this one does
+// not): none where there are no more stages than a join costs.
 size_t attention_cache_ws_bytes(const mopar_attention& a, const mopar_cache& c, int64_t, int max_q, int max_len) {
-    return static_cast<size_t>(cache_plan(a, c.n_seq, max_q, max_len).slots_bytes);
+    if ((static_cast<int64_t>(max_len) + 31) / 32 <= join_stages(a)) return 0;
+    const int64_t rows = query_rows(a, max_q);
+    int64_t most = plan_of(a, c.n_seq, rows, max_len).shared_bytes;
+    for (int64_t r : {32, 64}) most = std::max(most, plan_of(a, c.n_seq, std::min(rows, r), max_len).shared_bytes);
+    return static_cast<size_t>(most);
 }
 
 hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c, int64_t tokens, const int32_t* offsets,

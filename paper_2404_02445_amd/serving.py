@@ -182,7 +182,7 @@ def mopar_attention_cache_workspace_bytes(q, cache, max_q, max_len):
 
 
 def alloc_attention_workspace(q, cache, max_q, max_len):
-    """A workspace for mopar_attention_cache calls with as many rows, max_q and max_len as these."""
+    """A workspace for mopar_attention_cache calls with as many rows, max_q and max_len as these, or fewer."""
     n = mopar_attention_cache_workspace_bytes(q, cache, max_q, max_len)
     return torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
 

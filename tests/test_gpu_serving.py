@@ -388,6 +388,27 @@ def test_short_sequences_under_a_far_limit(dt, new):
     over_cache(gen(14), dt, 8, 2, 64, 16, [70, 0, 33, 1, 300], new, lambda n: tree_mask(n, gen(n))[0] if n else causal(0), spare=3, max_len=200000)
 
 
+def test_one_workspace_for_every_size():
+    """The largest call's workspace, full of NaN, under calls of fewer sequences and drafted tokens that share where it does not."""
+    g = gen(15)
+    d, page, n = 64, 16, 700
+    table = torch.randperm(40 * 44, generator=g, dtype=torch.int32).view(40, 44).cuda()
+    kc, vc = (randn(g, 40 * 44, 8, page, d) for _ in range(2))
+    q = randn(g, 40 * 64, 8, d)
+    ws = P.alloc_attention_workspace(q, P.PagedCache(kc, vc, table), 64, n)
+    for seqs, new in ((40, 64), (40, 1), (3, 1), (1, 64), (1, 9)):
+        cache, t = P.PagedCache(kc, vc, table[:seqs]), seqs * new
+        off, ln = ints([i * new for i in range(seqs + 1)]), ints([n - new] * seqs)
+        out = torch.empty(t, 8, d, device="cuda", dtype=torch.bfloat16)
+        ws.fill_(0xFF)
+        P.mopar_attention_cache(q[:t], out, cache, off, new, ln, n, ws=ws)
+        s = seqs - 1
+        k, v = (cache_rows(x.cpu(), table.cpu(), s, n) for x in (kc, vc))
+        seen = torch.arange(n)[None] <= n - new + torch.arange(new)[:, None]
+        ref, tol = attend(q[s * new:t], k, v, seen, d ** -0.5)
+        check(out[s * new:], ref, tol, f"{seqs} sequences, {new} tokens")
+
+
 def test_absent_pages_are_not_visible():
     for bad in (-1, 10 ** 9):
         over_cache(gen(5), "bf16", 4, 2, 64, 16, [300, 40], [3, 2], None, absent=(0, 4, bad))

@@ -244,6 +244,22 @@ def test_a_cache_of_no_sequences_needs_no_table():
     assert append_status(none, tokens=0) == 0
 
 
+@pytest.mark.parametrize("dtype,dims", [(L.MOPAR_BF16, (32, 64, 96, 128)), (L.MOPAR_F32, (32, 64, 96, 128))])
+def test_a_workspace_holds_smaller_calls(dtype, dims):
+    """The size does not fall as sequences, drafted tokens or the limit grow."""
+    steps = dict(n_seq=(1, 3, 40, 700, 20000), max_q=(1, 5, 8, 9, 16, 17, 64, 65, 300), max_len=(1, 33, 129, 160, 289, 321, 700, 5000, 100000))
+    for d in dims:
+        def need(n_seq, max_q, max_len):
+            st, n = ws_bytes(attention(dtype=dtype, head_dim=d), cache(dtype=dtype, head_dim=d, n_seq=n_seq), 10, max_q, max_len)
+            return n if st == 0 else None
+        size = {(i, j, k): need(a, b, c) for i, a in enumerate(steps["n_seq"]) for j, b in enumerate(steps["max_q"])
+                for k, c in enumerate(steps["max_len"])}
+        for (i, j, k), n in size.items():
+            for up in ((i + 1, j, k), (i, j + 1, k), (i, j, k + 1)):
+                if size.get(up) is not None:
+                    assert n <= size[up], (d, (i, j, k), up)
+
+
 def test_binding_refuses_mismatched_tensors():
     bf = torch.bfloat16
     k = torch.zeros(4, 2, 16, 64, dtype=bf)
