@@ -981,6 +981,7 @@ template <typename F> hipError_t by_type(int dtype, int d, F&& go) {
 // whether the blocks take equal shares of the stages.
 struct CachePlan {
     int bm, kt, row_tiles, split, blocks;
+    int64_t units, nt;                 // (sequence, key head, row tile) triples at most, stages of each at most
     int64_t shared_bytes;              // the workspace of equal shares
 };
 // Stages in a block's ring: two, and four in 64-row blocks where they fill 64 KB (head dims of 256 bytes).  16 sequences of
@@ -991,19 +992,27 @@ constexpr int ring_of(int wr, int stage_bytes) { return wr == 2 && stage_bytes =
 // a tile idle.  The same sequences: single tokens 122 us in tiles of 32 rows and 131 of 64; 16 drafted tokens (64 rows) 92 us
 // in 64 and 94 in 128; 32 (128 rows) 154 us in 64, 115 in 128, 110 in 256, so there are none of 128.
 int tile_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 256; }
-// Stages that equal shares must save to be taken: see cache_plan.
+// Stages that equal shares must save to be taken: see plan_of.
 int join_stages(const mopar_attention& a) { return a.dtype == MOPAR_BF16 ? 9 : 4; }
-CachePlan plan_of(const mopar_attention& a, int n_seq, int64_t rows, int max_len) {
+// Its tiles alone: n_seq below 2^31, at most 2^16 key heads and 2^15 row tiles, so the units fit 64 bits.
+CachePlan tiles_of(const mopar_attention& a, int n_seq, int64_t rows, int max_len) {
     CachePlan c{};
     c.bm = tile_rows(rows);
     // 64 keys a stage in the large tiles in bf16: 32 of them cost 6 % (two tiles' scores for one rescale); float32 has not
     // the registers
     c.kt = a.dtype == MOPAR_BF16 && c.bm == 256 ? 64 : 32;
     c.row_tiles = static_cast<int>((rows + c.bm - 1) / c.bm);
+    c.units = static_cast<int64_t>(n_seq) * a.kv_heads * c.row_tiles;
+    c.nt = (static_cast<int64_t>(max_len) + c.kt - 1) / c.kt;
+    return c;
+}
+// The whole plan, of tiles that attention_cache_fits has let pass.
+CachePlan plan_of(const mopar_attention& a, int n_seq, int64_t rows, int max_len) {
+    CachePlan c = tiles_of(a, n_seq, rows, max_len);
     // blocks that the card holds at once, by LDS and two waves a SIMD
     const int stage = 2 * c.kt * (a.head_dim > 64 ? 128 : a.head_dim) * static_cast<int>(dtype_size(a.dtype));
     const int64_t slots = 256 * std::min(256 / c.bm, 160 * 1024 / (ring_of(c.bm / 32, stage) * stage + c.bm / 32 * 1024));
-    const int64_t units = static_cast<int64_t>(n_seq) * a.kv_heads * c.row_tiles, nt = (static_cast<int64_t>(max_len) + c.kt - 1) / c.kt;
+    const int64_t units = c.units, nt = c.nt;
     // Equal shares, with partial sums and a second launch to join them, where they save more stages on the longest path
     // than the join costs: about 9 of bf16 (1 to 2 us each), 4 of float32 (3 us).  64 single tokens over 600: 42 us in
     // shares, 34 with a unit a block; 8 over 200: 14 and 13, over 400: 16 and 20; a float32 one over 100: 16 and 16,
@@ -1015,15 +1024,13 @@ CachePlan plan_of(const mopar_attention& a, int n_seq, int64_t rows, int max_len
     return c;
 }
 int64_t query_rows(const mopar_attention& a, int max_q) { return static_cast<int64_t>(max_q) * (a.heads / a.kv_heads); }
-CachePlan cache_plan(const mopar_attention& a, int n_seq, int max_q, int max_len) { return plan_of(a, n_seq, query_rows(a, max_q), max_len); }
 
 }  // namespace
 
 // A grid of a tile a block holds its threads, and stages are counted in 32 bits.
 bool attention_cache_fits(const mopar_attention& a, int n_seq, int max_q, int max_len) {
-    const CachePlan c = cache_plan(a, n_seq, max_q, max_len);
-    const int64_t units = static_cast<int64_t>(n_seq) * a.kv_heads * c.row_tiles;          // (factors below 2^31, 2^16 and 2^15)
-    return units < 1 << 22 && units * ((static_cast<int64_t>(max_len) + c.kt - 1) / c.kt) < 1 << 30;
+    const CachePlan c = tiles_of(a, n_seq, query_rows(a, max_q), max_len);
+    return c.units < 1 << 22 && c.units * c.nt < 1 << 30;
 }
 
 hipError_t launch_attention_prompt(const mopar_attention& a, int64_t tokens, int n_seq, const int32_t* offsets, int max_len,
@@ -1094,7 +1101,7 @@ hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c
     p.max_len = cache_limit(c, max_len);
     p.mask = mask;
     p.mask_words = mask_words;
-    const CachePlan cp = cache_plan(a, c.n_seq, max_q, max_len);
+    const CachePlan cp = plan_of(a, c.n_seq, query_rows(a, max_q), max_len);
     p.row_tiles = cp.row_tiles;
     p.split = cp.split;
     p.part = static_cast<float*>(ws);
