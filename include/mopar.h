@@ -317,8 +317,10 @@ int mopar_attention_cache(const mopar_attention* a, const mopar_cache* cache, in
  * nothing, nor does one from or to an absent page.  max_path bounds a path's length; entries past it are left.
  * A page that a sequence stores into must be no other sequence's.
  * Afterwards the sequence has len_dev[s] + (hi - lo) tokens.
- * Errors: MOPAR_E_ARG, MOPAR_E_UNSUPPORTED (2^24 and more blocks of up to
- * 4 KB of a token, of the sequences and layers), MOPAR_E_HIP. */
+ * layer_stride is read with two layers and more.
+ * Errors: MOPAR_E_ARG (also layers that span 2^58 elements and more),
+ * MOPAR_E_UNSUPPORTED (2^24 and more blocks of up to 4 KB of a token, of the sequences
+ * and layers), MOPAR_E_HIP. */
 int mopar_cache_keep(const mopar_cache* cache, int32_t layers, int64_t layer_stride, const int32_t* len_dev,
                      const int32_t* path_offsets_dev, int64_t entries, const int32_t* path_dev, int32_t max_path,
                      void* stream);

@@ -348,7 +348,7 @@ hipError_t launch_cache_keep(const mopar_cache& c, int layers, int64_t layer_str
     KeepParams p{};
     p.k = static_cast<unsigned char*>(c.k);
     p.v = static_cast<unsigned char*>(c.v);
-    p.layer_bytes = layer_stride * es;
+    p.layer_bytes = layers > 1 ? layer_stride * es : 0;
     p.pages = c.pages;
     p.table_stride = c.table_stride;
     p.entries = entries;

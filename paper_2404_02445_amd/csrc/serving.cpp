@@ -145,6 +145,7 @@ static int cache_keep_impl(const mopar_cache* c, int32_t layers, int64_t layer_s
     if (layers < 0 || entries < 0 || max_path < 0) return bad("keep: layers, entries or max_path");
     if (layers > 1 && (layer_stride % epc != 0 || layer_stride < c->pages * c->kv_heads * c->page_tokens * c->head_dim))
         return bad("keep: layer_stride must cover a layer's pages and be a multiple of 16 bytes");
+    if (layers > 1 && layer_stride > (int64_t(1) << 58) / layers) return bad("keep: 2^58 elements of layers and more");   // (2^60 bytes)
     if (c->n_seq == 0 || layers == 0 || entries == 0 || max_path == 0) return MOPAR_OK;
     if (!len || !offsets || !path) return bad("keep: lengths, offsets or path are null");
     const int64_t blocks = (static_cast<int64_t>(2) * c->kv_heads * c->head_dim / epc + 255) / 256;

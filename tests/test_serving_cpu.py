@@ -238,6 +238,14 @@ def test_sizes_that_no_grid_or_offset_holds():
     assert keep_status(layers=1 << 12, stride=1 << 20, c=cache(n_seq=1 << 12)) == U
 
 
+def test_layers_whose_offsets_no_word_holds():
+    """Byte offsets of the layers stay within 2^60; the stride of a single layer is not read."""
+    far = 1 << 61
+    assert keep_status(layers=2, stride=far) == L.MOPAR_E_ARG and b"2^58 elements" in P.lib().mopar_last_error()
+    assert keep_status(layers=2, stride=1 << 57, ln=None) == L.MOPAR_E_ARG and b"null" in P.lib().mopar_last_error()
+    assert keep_status(layers=1, stride=far, ln=None) == L.MOPAR_E_ARG and b"null" in P.lib().mopar_last_error()
+
+
 def test_a_cache_of_no_sequences_needs_no_table():
     none = cache(n_seq=0, table_dev=None)
     assert keep_status(none) == 0 and cache_status(c=none) == 0
