@@ -86,8 +86,10 @@ def rotary_desc(head_dim, rot_dim=None, layout="half", base=10000.0, scaling="no
     """A mopar_rotary_desc; layout and scaling by name (ValueError for an unknown one)."""
     if layout not in ROTARY_LAYOUT or scaling not in ROTARY_SCALING:
         raise ValueError(f"layout of {list(ROTARY_LAYOUT)} and scaling of {list(ROTARY_SCALING)}")
-    return RotaryDesc(ROTARY_LAYOUT[layout], ROTARY_SCALING[scaling], head_dim, head_dim if rot_dim is None else rot_dim, base,
-                      factor, context, beta_slow, beta_fast, mscale)
+    rot_dim = head_dim if rot_dim is None else rot_dim
+    if not (-2 ** 31 <= head_dim < 2 ** 31 and -2 ** 31 <= rot_dim < 2 ** 31):      # (ctypes would drop the bits past 32)
+        raise ValueError(f"head_dim {head_dim} and rot_dim {rot_dim} must fit 32 bits")
+    return RotaryDesc(ROTARY_LAYOUT[layout], ROTARY_SCALING[scaling], head_dim, rot_dim, base, factor, context, beta_slow, beta_fast, mscale)
 
 
 class Cache(ctypes.Structure):

@@ -23,6 +23,13 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+def _size(n, name):
+    """n as the C int that it becomes (ctypes would drop the bits past 32)."""
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name}: {n} does not fit 32 bits")
+    return n
+
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)    # (torch's own handle lookup without a Stream object)
 
 
@@ -101,6 +108,8 @@ class PagedCache:
         self.layers = k.shape[0] if k.dim() == 5 else 1
         self.layer_stride = k.stride(0) if k.dim() == 5 else 0
         pages, heads, page, d = layer.shape
+        for n, name in ((heads, "kv_heads"), (page, "page_tokens"), (d, "head_dim"), (table.shape[0], "sequences"), (table.shape[1], "max_pages")):
+            _size(n, name)
         self.raw = L.Cache(_dtype(k), heads, d, page, pages, k.data_ptr(), v.data_ptr(), table.data_ptr(),
                            max(table.stride(0), table.shape[1]), table.shape[1], table.shape[0])
 
@@ -121,7 +130,7 @@ def mopar_rotary_apply(rotary, x, y, pos, stream=None):
     t, heads, d = x.shape
     _need(d == rotary.head_dim, "x: head_dim is not the rotary's")
     p = _ints(pos, "pos", x, t)
-    _call(lib().mopar_rotary_apply, x.device, stream, rotary.handle, _dtype(x), t, heads, p, rx, ry)
+    _call(lib().mopar_rotary_apply, x.device, stream, rotary.handle, _dtype(x), t, _size(heads, "heads"), p, rx, ry)
     return y
 
 
@@ -137,7 +146,7 @@ def mopar_cache_append(cache, k, v, seq, slot, rotary=None, pos=None, q=None, q_
         _need(pos is not None, "pos: needed with a rotary")
         _need((q is None) == (q_out is None), "q and q_out come together")
         if q is not None:
-            heads = q.shape[1]
+            heads = _size(q.shape[1], "heads")
             rq, ro = _rows(q, "q", cache.k, (t, heads, c.head_dim)), _rows(q_out, "q_out", cache.k, (t, heads, c.head_dim))
     else:
         _need(pos is None and q is None and q_out is None, "pos, q and q_out go with a rotary")
@@ -152,12 +161,13 @@ def mopar_cache_keep(cache, lens, path_offsets, path, max_path, stream=None):
     c = cache.raw
     ln, po = _ints(lens, "lens", cache.k, c.n_seq), _ints(path_offsets, "path_offsets", cache.k, c.n_seq + 1)
     pa = _ints(path, "path", cache.k, path.numel())
-    _call(lib().mopar_cache_keep, cache.k.device, stream, c, cache.layers, cache.layer_stride, ln, po, path.numel(), pa, max_path)
+    _call(lib().mopar_cache_keep, cache.k.device, stream, c, cache.layers, cache.layer_stride, ln, po, path.numel(), pa,
+          _size(max_path, "max_path"))
 
 
 def _attention(q, kv_heads, scale):
     d = q.shape[2]
-    return L.Attention(_dtype(q), q.shape[1], kv_heads, d, d ** -0.5 if scale is None else scale, 0)
+    return L.Attention(_dtype(q), _size(q.shape[1], "heads"), _size(kv_heads, "kv_heads"), _size(d, "head_dim"), d ** -0.5 if scale is None else scale, 0)
 
 
 def mopar_attention_prompt(q, k, v, out, offsets, max_len, scale=None, stream=None):
@@ -169,7 +179,8 @@ def mopar_attention_prompt(q, k, v, out, offsets, max_len, scale=None, stream=No
     off = _ints(offsets, "offsets", q, offsets.numel())
     _need(offsets.numel() >= 1, "offsets: one more than sequences")
     a = _attention(q, k.shape[1], scale)
-    _call(lib().mopar_attention_prompt, q.device, stream, a, t, offsets.numel() - 1, off, max_len, rq, rk, rv, ro)
+    _call(lib().mopar_attention_prompt, q.device, stream, a, t, _size(offsets.numel() - 1, "sequences"), off, _size(max_len, "max_len"),
+          rq, rk, rv, ro)
     return out
 
 
@@ -177,7 +188,8 @@ def mopar_attention_cache_workspace_bytes(q, cache, max_q, max_len):
     c = _single(cache).raw
     n = ctypes.c_size_t()
     a = _attention(q, c.kv_heads, None)
-    check(lib().mopar_attention_cache_workspace_bytes(ctypes.byref(a), ctypes.byref(c), q.shape[0], max_q, max_len, ctypes.byref(n)))
+    check(lib().mopar_attention_cache_workspace_bytes(ctypes.byref(a), ctypes.byref(c), q.shape[0], _size(max_q, "max_q"),
+                                                        _size(max_len, "max_len"), ctypes.byref(n)))
     return n.value
 
 
@@ -202,6 +214,6 @@ def mopar_attention_cache(q, out, cache, offsets, max_q, lens, max_len, mask=Non
     a = _attention(q, c.kv_heads, scale)
     if ws is not None:
         _need(ws.device == q.device and ws.is_contiguous(), "ws: a contiguous tensor on the same device")
-    _call(lib().mopar_attention_cache, q.device, stream, a, c, q.shape[0], off, max_q, ln, max_len, mk, words, rq, ro,
-          None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes)
+    _call(lib().mopar_attention_cache, q.device, stream, a, c, q.shape[0], off, _size(max_q, "max_q"), ln, _size(max_len, "max_len"),
+          mk, _size(words, "words"), rq, ro, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes)
     return out

@@ -294,3 +294,20 @@ def test_binding_refuses_mismatched_tensors():
     for f in bad:
         with pytest.raises(ValueError):
             f()
+
+
+def test_binding_refuses_sizes_past_32_bits():
+    """They are not answered as what their lower 32 bits say."""
+    bf, past = torch.bfloat16, 1 << 32
+    k = torch.zeros(4, 2, 16, 64, dtype=bf)
+    c = P.PagedCache(k, k.clone(), torch.zeros(2, 2, dtype=torch.int32))
+    x = torch.zeros(3, 2, 64, dtype=bf)
+    i3, i2 = torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    for what, f in [("max_len", lambda n: P.mopar_attention_prompt(x, x, x, x, i2, n)),
+                    ("max_len", lambda n: P.mopar_attention_cache(x, x, c, i3, 1, i2, n)), ("max_q", lambda n: P.mopar_attention_cache(x, x, c, i3, n, i2, 8)),
+                    ("max_len", lambda n: P.mopar_attention_cache_workspace_bytes(x, c, 1, n)),
+                    ("max_q", lambda n: P.alloc_attention_workspace(x, c, n, 8)), ("max_path", lambda n: P.mopar_cache_keep(c, i2, i3, i3, n)),
+                    ("rot_dim", lambda n: P.Rotary(64, rot_dim=n)), ("head_dim", lambda n: P.Rotary(n, rot_dim=32))]:
+        for n in (past + 32, 1 << 31, -past):
+            with pytest.raises(ValueError, match=what):
+                f(n)
