@@ -154,7 +154,13 @@ int mopar_plan_slices(const mopar_layer_profile* layers, int32_t n, const mopar_
  *            weighted sums and rotations are float32, rounded once when
  *            stored; with bf16 the softmax weights are rounded to bf16 before
  *            they meet the values (they are at most 2^8, and their sum is
- *            taken in float32 before the rounding).
+ *            taken in float32 before the rounding).  Weighted sums are taken
+ *            before the division by the weights' sum: values of 2^100 and more
+ *            may overflow to infinity.
+ * Infinities An attention row is not reached by what it does not see, infinities
+ * and NaN.   and NaN included.  An infinity or NaN among the values that it sees
+ *            reaches it whatever its weight, however small (infinities of both
+ *            signs give NaN); a NaN among its scores makes it NaN.
  * Rows.      A tensor of packed tokens is a mopar_rows: element (token t,
  *            head h, dim i) at data + t * token_stride + h * head_stride + i,
  *            strides in elements, so heads may sit inside wider fused rows or
@@ -272,8 +278,7 @@ typedef struct {
  * non-decreasing offsets, the first 0 or more, the last at most `tokens`), and row i
  * of a sequence is the softmax(scale q_i . k_j) weighted sum of v_j over its rows
  * j <= i.  max_len bounds the length of a sequence (a longer one is cut to its first
- * max_len rows).  Rows of no sequence are neither read nor written, and what is not
- * visible to a row -- infinities and NaN included -- does not reach it.  out must
+ * max_len rows).  Rows of no sequence are neither read nor written.  out must
  * not overlap q, k or v.
  * Errors: MOPAR_E_ARG, MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (head_dim; 2^30 tokens; 2^24
  * tiles of 128 tokens, of the sequences and heads), MOPAR_E_HIP. */

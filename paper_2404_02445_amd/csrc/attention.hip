@@ -638,7 +638,7 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
                     }
                 });
                 // Where a row does not see every key, an infinity or NaN among the values must not meet its zero weight:
-                // it is left out here and added where it is seen at the end.
+                // it is left out here and put back where it is seen at the end.
                 if (cut) {
                     unsigned bad = 0;
 #pragma unroll
@@ -811,10 +811,11 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
                     begin();
                     full(std::integral_constant<int, 0>{});
                     end();
-                    if (k0 >= full_end) break;
-                    begin();
-                    full(std::integral_constant<int, 1>{});
-                    end();
+                    if (k0 < full_end) {
+                        begin();
+                        full(std::integral_constant<int, 1>{});
+                        end();
+                    }
                 }
             } else {
                 while (k0 < full_end && k0 + KT <= bad_from) {
@@ -832,39 +833,21 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         }
 
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // no load into LDS outlives the unit (the pages sent last)
-        // what was left out, where it is seen (a weight is positive: the sum becomes infinite or NaN itself)
-        if (marred) {
-            for (int key = looked_at; key < wave_end; ++key) {
-                const unsigned char* vrow;
-                if constexpr (PAGED) {
-                    const unsigned page = pages[key >> p.shift];
-                    if (page >= static_cast<unsigned>(p.pages)) continue;
-                    vrow = vbase + page_at(page, key);
-                } else {
-                    vrow = vbase + key * p.v_ts;
-                }
-                if (!(visible(key) & 1)) continue;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const unsigned* src = reinterpret_cast<const unsigned*>(vrow + (d * 32 + 8 * i + 4 * lh) * ES);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const unsigned w = ES == 2 ? (e & 1 ? src[e / 2] & 0xffff0000u : src[e / 2] << 16) : src[e];
-                            if (not_finite<4>(w)) o[d][4 * i + e] += __uint_as_float(w);
-                        }
-                    }
-            }
-        }
 
         // --- results -----------------------------------------------------------------------------------
         l += other_half(l);
         const ArgsPtr ar = args_again();
+        const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+        unsigned char* const dst = ar->out + (start + qtok) * ar->o_ts + qhead * ar->o_hs;
+        const int64_t to = static_cast<int64_t>(slot) * BM + wave * 32 + lr;
+        bool off = false;                             // a result is infinite or NaN, its row's sum is not
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) off |= not_finite<4>(__float_as_uint(o[d][i])) != 0;
+        off = __any(off && !not_finite<4>(__float_as_uint(l)));
         if (wave0 + lr < nrow) {
             if (whole) {
-                const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-                unsigned char* dst = ar->out + (start + qtok) * ar->o_ts + qhead * ar->o_hs;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -877,7 +860,6 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
                             *reinterpret_cast<f32x4*>(dst + dim * 4) = v;
                     }
             } else {
-                const int64_t to = static_cast<int64_t>(slot) * BM + wave * 32 + lr;
                 if (lh == 0) {
                     ar->stat[2 * to] = m;
                     ar->stat[2 * to + 1] = l;
@@ -888,6 +870,63 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
                     for (int i = 0; i < 4; ++i)
                         *reinterpret_cast<f32x4*>(ar->part + to * D + d * 32 + 8 * i + 4 * lh) =
                             f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+            }
+        }
+        // An infinity or NaN among the values reaches every row that sees it, whatever its weight.  The products lose that
+        // where a weight has become 0 (and makes NaN of an infinity) and where values were left out, so the visible values
+        // that are not finite are added up alone, and where there are any their sum is the result.
+        if (marred || off) {
+            int ln = lane;                            // (nothing of this is worked out before the loops: registers)
+            pin(ln);
+#pragma unroll 1
+            for (int d = 0; d < DT; ++d) {
+                float sum[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
+                bool all_nan = false;
+#pragma unroll 1
+                for (int k = off ? key0 : looked_at; k < wave_end && !all_nan; k += 64) {
+                    auto value = [&](int key) __attribute__((always_inline)) -> const u32x4* {      // its 32 dims; null on an absent page
+                        if constexpr (PAGED) {
+                            const unsigned page = pages[key >> p.shift];
+                            return page < static_cast<unsigned>(p.pages) ? reinterpret_cast<const u32x4*>(vbase + page_at(page, key) + d * 32 * ES) : nullptr;
+                        } else {
+                            return reinterpret_cast<const u32x4*>(vbase + key * p.v_ts + d * 32 * ES);
+                        }
+                    };
+                    bool has = false;                 // a lane looks at a key
+                    if (k + ln < wave_end) {
+                        const u32x4* v = value(k + ln);
+                        for (int i = 0; v && i < 2 * ES; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) has |= not_finite<ES>(v[i][e]) != 0;
+                    }
+                    for (uint64_t keys = __ballot(has); keys && !all_nan; keys &= keys - 1) {
+                        const int key = k + static_cast<int>(__builtin_ctzll(keys));
+                        const unsigned char* v = reinterpret_cast<const unsigned char*>(value(key));
+                        all_nan = true;
+                        const bool sees = visible(key) & 1;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int dim = 8 * (i / 4) + 4 * (ln >> 5) + i % 4;
+                            const unsigned w = ES == 2 ? static_cast<unsigned>(*reinterpret_cast<const uint16_t*>(v + dim * 2)) << 16
+                                                       : *reinterpret_cast<const unsigned*>(v + dim * ES);
+                            if (sees && not_finite<4>(w)) sum[i] += __uint_as_float(w);
+                            all_nan &= sum[i] != sum[i];
+                        }
+                        all_nan = __all(all_nan);
+                    }
+                }
+                if (wave0 + lr < nrow)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        if (sum[i] == 0.0f) continue;
+                        const int dim = d * 32 + 8 * (i / 4) + 4 * (ln >> 5) + i % 4;
+                        if (whole)
+                            reinterpret_cast<typename std::conditional<ES == 2, __bf16, float>::type*>(dst)[dim] = sum[i] * inv;
+                        else
+                            ar->part[to * D + dim] = sum[i];
+                    }
             }
         }
         if constexpr (!PAGED) {
@@ -939,7 +978,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p)
                     for (int i = 0; i < many; ++i) {
                         const float w = __shfl(f, min(k + i, 63), 64);
 #pragma unroll
-                        for (int e = 0; e < PER; ++e) acc[e] += k + i < n ? v[i][e] * w : 0.0f;
+                        for (int e = 0; e < PER; ++e)        // (a part's infinity or NaN counts whatever its weight)
+                            acc[e] += k + i < n ? not_finite<4>(__float_as_uint(v[i][e])) ? v[i][e] : v[i][e] * w : 0.0f;
                     }
                 }
             }

@@ -459,6 +459,57 @@ def test_hidden_drafts_do_not_reach_a_row(dt):
         assert bool(torch.isfinite(o).all())
 
 
+def tiny_weights(g, n, heads, kv, d, dt, at, peak):
+    """Queries, keys and values of which key `peak` outweighs all others by e^300, so that their weights are 0 in float32;
+    infinities and a NaN among the values at `at`, `at` + 1 and `at` + 2."""
+    q = torch.ones(n, heads, d, device="cuda", dtype=DT[dt])
+    k, v = randn(g, n, kv, d, dt="f32") * 0.1, randn(g, n, kv, d, dt=dt)
+    k[peak] += 300.0 / d ** 0.5
+    v[at, 0, 3], v[at + 1, 0, 4], v[at + 2, 0, 5] = float("inf"), float("-inf"), float("nan")
+    v[at, 0, 6], v[at + 1, 0, 6] = float("inf"), float("-inf")
+    return q, k.to(DT[dt]), v
+
+
+def check_tiny_weights(out, q, k, v, seen):
+    """Results of finite values against the plain form with zeros for the others, whose error is bounded by that of each
+    weighted value (the sum of |p v|); where a row sees values that are not finite, their sum."""
+    off = ~torch.isfinite(v)
+    ref, tol = attend(q, k, torch.where(off, torch.zeros_like(v), v), seen, q.shape[2] ** -0.5)
+    heads = q.shape[1] // v.shape[1]
+    for j, h, i in torch.nonzero(off.cpu()).tolist():
+        for row in torch.nonzero(seen[:, j])[:, 0].tolist():
+            for x in range(h * heads, (h + 1) * heads):
+                ref[row, x, i] += v[j, h, i].item()
+    assert not bool(torch.isfinite(ref).all())
+    check(out, ref, tol)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("at,peak", [(5, 150), (5, 9), (100, 20), (250, 290), (290, 200)])
+def test_prompt_infinities_of_tiny_weight(dt, at, peak):
+    """In whole and partly hidden tiles, before and after the peak: they reach the rows that see them."""
+    q, k, v = tiny_weights(gen(20), 300, 4, 1, 64, dt, at, peak)
+    check_tiny_weights(prompt(q, k, v, [300]), q, k, v, causal(300))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("new,heads", [(1, 2), (20, 2), (40, 8)])
+@pytest.mark.parametrize("n,at,peak", [(60, 5, 55), (300, 5, 150), (300, 290, 100), (4000, 5, 3990), (4000, 3000, 3), (4000, 3990, 2000)])
+def test_cache_infinities_of_tiny_weight(dt, new, heads, n, at, peak):
+    """The same over a cache: tiles of every size, a unit by one block and shared by many."""
+    page, d = 16, 64
+    g = gen(21)
+    q, k, v = tiny_weights(g, n, heads, 1, d, dt, at, peak)
+    table, pages = page_table([n], page, g)
+    kc, vc = (torch.full((pages, 1, page, d), float("nan"), device="cuda", dtype=DT[dt]) for _ in range(2))
+    cache = P.PagedCache(kc, vc, table.cuda())
+    P.mopar_cache_append(cache, k, v, ints([0] * n), torch.arange(n, dtype=torch.int32, device="cuda"))
+    out = torch.empty(new, heads, d, device="cuda", dtype=DT[dt])
+    P.mopar_attention_cache(q[:new], out, cache, ints([0, new]), new, ints([n - new]), n, ws=P.alloc_attention_workspace(q[:new], cache, new, n))
+    seen = torch.arange(n)[None] <= n - new + torch.arange(new)[:, None]
+    check_tiny_weights(out, q[:new], k, v, seen)
+
+
 def test_pools_past_32_bit_offsets():
     g = gen(8)
     kv, page, d, n = 8, 256, 128, 700
