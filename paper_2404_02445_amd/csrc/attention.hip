@@ -48,7 +48,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
-typedef const __attribute__((address_space(1))) void* gptr_t;
 
 // what absent keys and values are read from
 __device__ __attribute__((aligned(16))) const unsigned int kZeros[4] = {0u, 0u, 0u, 0u};
@@ -56,12 +55,37 @@ __device__ __attribute__((aligned(16))) const unsigned int kZeros[4] = {0u, 0u, 
 constexpr int kRsrcWord3 = 0x00020000;       // raw buffer, 32-bit data format
 constexpr unsigned kOOB = 0x80000000u;       // a lane offset past every resource: reads zeros
 
-// One 16-byte chunk per lane from base + voff into place `lane` of the 1 KB block at dst; zeros where voff is kOOB.
-__device__ __forceinline__ void load_lds(const unsigned char* base, lds_ptr_t dst, unsigned voff) {
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), static_cast<short>(0),
-                                                                      0x7fffffff, kRsrcWord3);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, voff, 0, 0, 0);
+// Direct loads into LDS, to the byte address dst (the same in every lane), in inline asm so that the compiler does not take
+// every later read of LDS for a reader of theirs (it would wait for all loads in flight).  They have no result in registers.
+// What they write is read after begin(): a count of the loads in flight and a barrier, which the compiler moves no access
+// of memory across.  m0, which they write, is in no other use (the compiler warns that it is a reserved register).
+// Wait states: one after a write of m0, five after a lane's value went into a scalar register.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ u32x4 resource(const unsigned char* base) {
+    const uint64_t a = reinterpret_cast<uint64_t>(base);
+    return u32x4{static_cast<unsigned>(a), static_cast<unsigned>(a >> 32) & 0xffffu, 0x7fffffffu, kRsrcWord3};
 }
+// Two 16-byte chunks per lane, from k + kofs and v + vofs into place `lane` of the 1 KB blocks at kdst and vdst; zeros where an
+// offset is kOOB.
+__device__ __forceinline__ void load_lds(const unsigned char* k, unsigned kdst, unsigned kofs, const unsigned char* v, unsigned vdst, unsigned vofs) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds\n\t"
+                 "s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, 0 offen lds"
+                 ::"s"(kdst), "v"(kofs), "s"(resource(k)), "s"(vdst), "v"(vofs), "s"(resource(v))
+                 : "memory", "m0");
+}
+// ... from the lane's own addresses
+__device__ __forceinline__ void load_lds(const unsigned char* k, unsigned kdst, const unsigned char* v, unsigned vdst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off\n\t"
+                 "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, off"
+                 ::"s"(kdst), "v"(k), "s"(vdst), "v"(v)
+                 : "memory", "m0");
+}
+// One word per lane from its own address into word `lane` of dst.
+__device__ __forceinline__ void load_lds(const int32_t* src, unsigned dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
+}
+#pragma clang diagnostic pop
 
 constexpr float kNoMax = -3.40282347e38f;    // running maximum of a row that has seen no key
 
@@ -121,10 +145,9 @@ template <int RS> __host__ __device__ constexpr int swizzle(int r) {
     return (r >> 2) & 3;
 }
 
-// LDS fragment reads, in inline asm so that the compiler does not take them for readers of the direct loads in flight
-// (it would wait for all of those first).  The plain forms wait within the asm.  The `start` forms return at once: a
-// value may be touched only after an lds_wait and its pin -- nothing guards it against a spill or a copy in between, so
-// they are for the one loop whose registers all fit.
+// LDS fragment reads.  Those of the masked tiles wait within their asm; of the whole stages the compiler knows each (lds_get16,
+// lds_get_tr), and waits for it where its value is used.  A read whose wait stands elsewhere would leave its registers to the
+// allocator before they are written, so there are none.
 template <int N, int OFF> __device__ __forceinline__ void lds_read16(u32x4 (&v)[N], const unsigned (&a)[N]) {
     static_assert(OFF >= 0 && OFF < 65536 && N >= 2 && N <= 4, "ds offset");
     if constexpr (N == 4)
@@ -167,22 +190,11 @@ __device__ __forceinline__ unsigned lds_read_word(unsigned a) {
     asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(a) : "memory");
     return v;
 }
-template <int OFF> __device__ __forceinline__ u32x4 lds_start16(unsigned addr) {
-    static_assert(OFF >= 0 && OFF < 65536, "ds offset");
-    u32x4 v;
-    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
-    return v;
+template <int OFF> __device__ __forceinline__ u32x4 lds_get16(unsigned addr) {
+    return *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(addr + OFF);
 }
-template <int OFF> __device__ __forceinline__ u32x2 lds_start_tr(unsigned addr) {
-    static_assert(OFF >= 0 && OFF < 65536, "ds offset");
-    u32x2 v;
-    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
-    return v;
-}
-// until at most N of this wave's LDS reads are still in flight (they complete in order)
-template <int N = 0> __device__ __forceinline__ void lds_wait() {
-    static_assert(N >= 0 && N <= 15, "lgkmcnt range");
-    asm volatile("s_waitcnt lgkmcnt(%0)" ::"n"(N) : "memory");
+template <int OFF> __device__ __forceinline__ bf16x4 lds_get_tr(unsigned addr) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(uintptr_t)(addr + OFF));
 }
 template <typename V> __device__ __forceinline__ void pin(V& v) { asm volatile("" : "+v"(v)); }
 
@@ -346,6 +358,7 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
     constexpr int RING = 2 * NS * TILE;              // then, over a cache, each wave's pages of four stages
     __shared__ __attribute__((aligned(1024))) unsigned char lds[RING + (PAGED ? WR * 1024 : 0)];
     static_assert(AHEAD <= 3, "places for the pages");
+    const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_ptr_t)lds));
 
     const int lane = threadIdx.x & 63, wave = OWN ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lr = lane & 31, lh = lane >> 5;
@@ -452,32 +465,31 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         };
         auto send_pages = [&](int k0) __attribute__((always_inline)) {
             if constexpr (PAGED)
-                __builtin_amdgcn_global_load_lds((gptr_t)page_of(k0), (lds_ptr_t)(lds + RING + wave * 1024 + (k0 / KT & 3) * 256), 4, 0, 0);
+                load_lds(page_of(k0), lds0 + RING + wave * 1024 + (k0 / KT & 3) * 256);
         };
         auto sent_pages = [&](int k0) __attribute__((always_inline)) -> int {
             if constexpr (!PAGED) return 0;
-            return lds_read_word(static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_ptr_t)lds)) + RING + wave * 1024 + (k0 / KT & 3) * 256 + lane * 4);
+            return lds_read_word(lds0 + RING + wave * 1024 + (k0 / KT & 3) * 256 + lane * 4);
         };
         auto look_at = [&](int pgs, int k0) __attribute__((always_inline)) {
             if constexpr (PAGED)
                 if (__any(static_cast<unsigned>(pgs) >= static_cast<unsigned>(p.pages))) bad_from = min(bad_from, k0);
         };
         auto issue = [&](int k0, int at, int pgs) __attribute__((always_inline)) {
-            unsigned char __attribute__((address_space(3)))* const place = (unsigned char __attribute__((address_space(3)))*)(lds_ptr_t)lds + at * TILE;
+            const unsigned place = lds0 + at * TILE;
             if (PAGED && small) {
                 for (int j = 0; j < LPW; ++j) {
                     const int b = wave * LPW + j;
                     if (NBLK % WR != 0 && b >= NBLK) break;
                     const int rrow = b * RPB + lrow, ch = (lane % RS) ^ swizzle<RS>(rrow), key = k0 + rrow;
-                    const unsigned page = (key < key1) & (ch < CH) ? pages[key >> p.shift] : ~0u;
+                    const unsigned page = key < key1 && ch < CH ? pages[key >> p.shift] : ~0u;
                     const unsigned char *ks = reinterpret_cast<const unsigned char*>(kZeros), *vs = ks;
                     if (page < static_cast<unsigned>(p.pages)) {
                         const int64_t off = page_at(page, key) + ch * 16;
                         ks = kbase + off;
                         vs = vbase + off;
                     }
-                    __builtin_amdgcn_global_load_lds((gptr_t)ks, (lds_ptr_t)(place + b * 1024), 16, 0, 0);
-                    __builtin_amdgcn_global_load_lds((gptr_t)vs, (lds_ptr_t)(place + NS * TILE + b * 1024), 16, 0, 0);
+                    load_lds(ks, place + b * 1024, vs, place + NS * TILE + b * 1024);
                 }
                 return;
             }
@@ -494,17 +506,16 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
                 const int b = wave * LPW + j;
                 if (NBLK % WR != 0 && b >= NBLK) continue;
                 const int rrow = b * RPB + lrow, ch = (lane % RS) ^ swizzle<RS>(rrow);
-                const lds_ptr_t kd = (lds_ptr_t)(place + b * 1024), vd = (lds_ptr_t)(place + NS * TILE + b * 1024);
+                const unsigned kd = place + b * 1024, vd = place + NS * TILE + b * 1024;
                 if constexpr (PAGED) {
                     const int64_t off = static_cast<int64_t>(__builtin_amdgcn_readlane(lo, b)) |
                                         static_cast<int64_t>(__builtin_amdgcn_readlane(hi, b)) << 32;
                     const unsigned vo = CH == RS || ch < CH ? static_cast<unsigned>(lrow * (D * ES) + ch * 16) : kOOB;
-                    load_lds(kbase + off, kd, vo);
-                    load_lds(vbase + off, vd, vo);
+                    load_lds(kbase + off, kd, vo, vbase + off, vd, vo);
                 } else {
                     const bool in = (k0 + rrow < key1) & (ch < CH);
-                    load_lds(kbase + k0 * p.k_ts, kd, in ? static_cast<unsigned>(rrow * static_cast<int>(p.k_ts)) + ch * 16 : kOOB);
-                    load_lds(vbase + k0 * p.v_ts, vd, in ? static_cast<unsigned>(rrow * static_cast<int>(p.v_ts)) + ch * 16 : kOOB);
+                    load_lds(kbase + k0 * p.k_ts, kd, in ? static_cast<unsigned>(rrow * static_cast<int>(p.k_ts)) + ch * 16 : kOOB,
+                             vbase + k0 * p.v_ts, vd, in ? static_cast<unsigned>(rrow * static_cast<int>(p.v_ts)) + ch * 16 : kOOB);
                 }
             }
         };
@@ -516,7 +527,6 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-        const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_ptr_t)lds));
         // K fragment: row lr, chunk 2 st + lh;  V fragment (bf16): row 4 lh + (lane % 16) / 4 of eight, dims 16 ((lane / 16) % 2)
         // + 4 (lane % 4) of 32; (float32): row 4 lh, dim lr of 32
         const unsigned ka = lds0 + static_cast<unsigned>(lr * RB + ((lh ^ swizzle<RS>(lr)) << 4));
@@ -689,33 +699,28 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             auto read_k = [&](auto gr) __attribute__((always_inline)) {
                 static_for<KG>([&](auto e) __attribute__((always_inline)) {
                     constexpr int st = (gr * KG + e) % (CH / 2), sub = (gr * KG + e) / (CH / 2), half = gr % 2;
-                    kf[half][e] = lds_start16<B0 + sub * 32 * RB>(PAGED ? kd ^ (st << 5) : kr[PAGED ? 0 : st]);
+                    kf[half][e] = lds_get16<B0 + sub * 32 * RB>(PAGED ? kd ^ (st << 5) : kr[PAGED ? 0 : st]);
                 });
             };
             read_k(std::integral_constant<int, 0>{});
             static_for<NKG>([&](auto gr) __attribute__((always_inline)) {
                 constexpr int half = gr % 2;
-                if constexpr (gr + 1 < NKG) {
-                    read_k(std::integral_constant<int, gr + 1>{});
-                    lds_wait<KG>();
-                } else {
-                    lds_wait();
-                }
+                if constexpr (gr + 1 < NKG) read_k(std::integral_constant<int, gr + 1>{});
+                __builtin_amdgcn_sched_barrier(0);    // (the next group's reads before this one's products)
                 static_for<KG>([&](auto e) __attribute__((always_inline)) {
                     constexpr int st = (gr * KG + e) % (CH / 2), sub = (gr * KG + e) / (CH / 2);
-                    pin(kf[half][e]);
                     sc[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[half][e]), __builtin_bit_cast(bf16x8, qf[st]),
                                                                       sc[sub], 0, 0, 0);
                 });
             });
             // the first values on their way under the softmax
             constexpr int NVG = 2 * SUBS;
-            u32x2 vf[2][2 * DT];
+            bf16x4 vf[2][2 * DT];
             auto read_v = [&](auto gr) __attribute__((always_inline)) {
                 static_for<DT>([&](auto d) __attribute__((always_inline)) {
                     constexpr int half = gr % 2, off = B0 + gr * 16 * RB;
-                    vf[half][2 * d] = lds_start_tr<off>(PAGED ? vd ^ (d << 6) : vr[PAGED ? 0 : 2 * d]);
-                    vf[half][2 * d + 1] = lds_start_tr<off + 8 * RB>(PAGED ? vd ^ ((d << 6) | (swizzle<RS>(8) << 4)) : vr[PAGED ? 0 : 2 * d + 1]);
+                    vf[half][2 * d] = lds_get_tr<off>(PAGED ? vd ^ (d << 6) : vr[PAGED ? 0 : 2 * d]);
+                    vf[half][2 * d + 1] = lds_get_tr<off + 8 * RB>(PAGED ? vd ^ ((d << 6) | (swizzle<RS>(8) << 4)) : vr[PAGED ? 0 : 2 * d + 1]);
                 });
             };
             read_v(std::integral_constant<int, 0>{});
@@ -737,21 +742,15 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
             l += sum[0] + sum[1];
             static_for<NVG>([&](auto gr) __attribute__((always_inline)) {
                 constexpr int half = gr % 2;
-                if constexpr (gr + 1 < NVG) {
-                    read_v(std::integral_constant<int, gr + 1>{});
-                    lds_wait<2 * DT>();
-                } else {
-                    lds_wait();
-                }
+                if constexpr (gr + 1 < NVG) read_v(std::integral_constant<int, gr + 1>{});
+                __builtin_amdgcn_sched_barrier(0);
                 bf16x8 pf;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) pf[i] = static_cast<__bf16>(sc[gr / 2][8 * (gr % 2) + i]);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    pin(vf[half][2 * d]);
-                    pin(vf[half][2 * d + 1]);
-                    const u32x4 w = {vf[half][2 * d][0], vf[half][2 * d][1], vf[half][2 * d + 1][0], vf[half][2 * d + 1][1]};
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf, o[d], 0, 0, 0);
+                    const bf16x8 w = __builtin_shufflevector(vf[half][2 * d], vf[half][2 * d + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, pf, o[d], 0, 0, 0);
                 }
             });
         };
@@ -788,9 +787,9 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         // the stage at hand has arrived once only the loads of the AHEAD - 1 after it (or later ones) are on their way
         auto begin = [&]() __attribute__((always_inline)) {
             if (AHEAD > 1 && k0 + (AHEAD - 1) * KT < key1)
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NBLK % WR == 0 ? (AHEAD - 1) * (2 * LPW + PAGED) : 0) : "memory");
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NBLK % WR == 0 ? (AHEAD - 1) * (2 * LPW + PAGED) : 0) : "memory");
             else
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             if constexpr (!OWN) {
                 __builtin_amdgcn_s_barrier();         // for every wave, and none works on the stage before any more
                 asm volatile("" ::: "memory");
