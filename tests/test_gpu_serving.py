@@ -388,6 +388,48 @@ def test_short_sequences_under_a_far_limit(dt, new):
     over_cache(gen(14), dt, 8, 2, 64, 16, [70, 0, 33, 1, 300], new, lambda n: tree_mask(n, gen(n))[0] if n else causal(0), spare=3, max_len=200000)
 
 
+def shares(dt, d, heads, kv, seqs, top, limit):
+    """Blocks that share a call's key stages, keys of a stage, rows of a tile: the rule, its workspace checked against the library's."""
+    def plan(rows):
+        bm = 32 if rows <= 32 else 64 if rows <= 64 else 256
+        es = 2 if dt == "bf16" else 4
+        kt = 64 if es == 2 and bm == 256 else 32
+        stage = 2 * kt * (128 if d > 64 else d) * es
+        ring = 4 if bm == 64 and stage == 16384 else 2
+        slots = 256 * min(256 // bm, 160 * 1024 // (ring * stage + bm // 32 * 1024))
+        units, nt = seqs * kv * -(-rows // bm), -(-limit // kt)
+        blocks = min(slots, units * nt)
+        saved = nt * -(-units // slots) - -(-nt * units // slots)
+        return blocks * (2 * bm * (d + 2) * 4 + 32), blocks if saved > (9 if es == 2 else 4) else 0, kt, bm
+    rows = top * heads // kv
+    pool = torch.empty(1, kv, 16, d, dtype=DT[dt])
+    cache = P.PagedCache(pool, pool, torch.zeros(seqs, 1, dtype=torch.int32))
+    need = P.mopar_attention_cache_workspace_bytes(torch.empty(1, heads, d, dtype=DT[dt]), cache, top, limit)
+    assert need == max(plan(r)[0] for r in (rows, min(rows, 32), min(rows, 64)))
+    return plan(rows)[1:]
+
+
+@pytest.mark.parametrize("dt,d,page", [("bf16", 128, 16), ("bf16", 64, 1), ("bf16", 96, 64), ("bf16", 32, 8), ("f32", 64, 16), ("f32", 128, 32),
+                                       ("f32", 96, 1), ("f32", 32, 128)])
+@pytest.mark.parametrize("seqs,top,tile", [(40, 1, 32), (40, 16, 64), (24, 40, 256)])
+def test_shares_of_several_units(dt, d, page, seqs, top, tile):
+    """Ragged sequences of which a block's share holds many stages: whole units, the end of one and the start of the next."""
+    g = gen(seqs + d + page)
+    kv = 8 if tile == 32 else 4
+    heads = 4 * kv
+    lens = [int(x) for x in torch.randint(1, 1500, (seqs,), generator=g)]
+    new = [int(x) for x in torch.randint(1, top + 1, (seqs,), generator=g)]
+    lens[0], lens[3], lens[4], lens[5], new[0], new[7] = 1500, 0, 1, 31, top, 0
+    limit = 1500 + top
+    blocks, kt, bm = shares(dt, d, heads, kv, seqs, top, limit)
+    nt = [-(-(a + b) // kt) for a, b in zip(lens, new)]
+    units = [kv * -(-n * 4 // bm) for n in new]
+    per = -(-sum(a * b for a, b in zip(nt, units)) // blocks)
+    assert bm == tile and blocks > 0 and per > 2 and per > 2 * min(n for n, u in zip(nt, units) if u)
+    over_cache(g, dt, heads, kv, d, page, lens, new, (lambda n: tree_mask(n, g)[0] if n else causal(0)) if top > 1 else None, spare=2,
+               absent=(0, 700 // page, -1), max_len=limit)
+
+
 def test_one_workspace_for_every_size():
     """The largest call's workspace, full of NaN, under calls of fewer sequences and drafted tokens that share where it does not."""
     g = gen(15)
