@@ -224,7 +224,7 @@ struct RotaryTable {
 int rotary_table(const mopar_rotary_desc& d, RotaryTable* out);
 // Rows of `heads` heads, the first `turned` of them turned and the others copied; row t at position pos[t]
 // (pos null: t mod period).  (Weak, as launch_attention_prompt: host-only programs link the model code without
-// the decoding kernels, which only a forward of a model with such operators calls.)
+// the decoding kernels; mopar_model_create then refuses models with these operators.)
 __attribute__((weak)) hipError_t launch_rotary(const RotaryTable& tab, int dtype, int64_t tokens, int heads, int turned,
                                                const int32_t* pos, int period, const mopar_rows* x, const mopar_rows* y,
                                                hipStream_t s);

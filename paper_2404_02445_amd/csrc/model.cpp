@@ -455,6 +455,7 @@ static int validate_and_build(mopar_model_s& m) {
             }
             case MOPAR_OP_ROTARY: {
                 const int64_t d = op.rotary.head_dim;
+                if (!launch_rotary) return set_error(MOPAR_E_UNSUPPORTED, nm + ": linked without the decoding kernels");
                 inf.rotary = std::make_shared<RotaryTable>();
                 if (int e = rotary_table(op.rotary, inf.rotary.get())) return e;
                 if (x.rank != 3 || !shape_eq(y, {x.dims[0], x.dims[1], x.dims[2]}) || x.dims[2] % d != 0 || op.heads < 1 ||
@@ -467,6 +468,7 @@ static int validate_and_build(mopar_model_s& m) {
             }
             case MOPAR_OP_CAUSAL_ATTENTION: {
                 const int64_t h = op.heads, kv = op.kv_heads, d = op.head_dim;
+                if (!launch_attention_prompt) return set_error(MOPAR_E_UNSUPPORTED, nm + ": linked without the decoding kernels");
                 if (x.rank != 3 || h < 1 || kv < 1 || h > 65536 || h % kv != 0 || d < 1 || d > 128 || x.dims[2] != (h + 2 * kv) * d ||
                     !shape_eq(y, {x.dims[0], x.dims[1], h * d}))
                     return set_error(MOPAR_E_SHAPE, nm + ": causal attention needs (B,S,(heads+2*kv_heads)*head_dim) -> (B,S,heads*head_dim)");
