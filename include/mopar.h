@@ -50,6 +50,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#define MOPAR_VERSION "0.2"
+
 #ifdef __cplusplus
 extern "C" {
 #endif
@@ -654,7 +656,9 @@ int mopar_model_measure(mopar_model_t model, int32_t k_max, int32_t reps, const 
 /* Description of the last error on this thread ("" when none). */
 const char* mopar_last_error(void);
 
-/* Library version string. */
+/* Library version string: "mopar-mi355x ", MOPAR_VERSION, " (gfx950)".  The version changes with the
+ * layout of any struct above (0.2: mopar_op has the fields of causal attention and
+ * rotary positions), so a caller compares it with the one that it was compiled against. */
 const char* mopar_version(void);
 
 #ifdef __cplusplus

@@ -161,6 +161,6 @@ int mopar_model_measure(mopar_model_t model, int32_t k_max, int32_t reps, const 
 
 const char* mopar_last_error(void) { return g_error.c_str(); }
 
-const char* mopar_version(void) { return "mopar-mi355x 0.1 (gfx950)"; }
+const char* mopar_version(void) { return "mopar-mi355x " MOPAR_VERSION " (gfx950)"; }
 
 }  // extern "C"

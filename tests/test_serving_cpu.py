@@ -2,6 +2,8 @@
 rotary's angles."""
 import ctypes
 import math
+import os
+import re
 from fractions import Fraction
 
 import numpy as np
@@ -311,3 +313,11 @@ def test_binding_refuses_sizes_past_32_bits():
         for n in (past + 32, 1 << 31, -past):
             with pytest.raises(ValueError, match=what):
                 f(n)
+
+
+def test_the_version_tells_the_layout_of_the_structs():
+    """mopar_op of version 0.1 had no rotary descriptor and ended at w5."""
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "mopar.h")) as f:
+        version = re.search(r'#define MOPAR_VERSION "([0-9.]+)"', f.read())[1]
+    assert P.lib().mopar_version().decode() == f"mopar-mi355x {version} (gfx950)"
+    assert version != "0.1" and ctypes.sizeof(L.Op) == L.Op.w5.offset + 8 + 8 + ctypes.sizeof(L.RotaryDesc)
