@@ -104,6 +104,7 @@ class PagedCache:
               "k and v: a layer's pages must be contiguous")
         _need(table.dim() == 2 and table.dtype == torch.int32 and table.device == k.device and
               (table.stride(1) == 1 or table.shape[1] == 1), "table: int32 [sequences, max_pages] on the pools' device")
+        _need(table.shape[0] <= 1 or table.stride(0) >= table.shape[1], "table: the rows of two sequences overlap")
         self.k, self.v, self.table = k, v, table
         self.layers = k.shape[0] if k.dim() == 5 else 1
         self.layer_stride = k.stride(0) if k.dim() == 5 else 0

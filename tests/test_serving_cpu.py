@@ -321,3 +321,16 @@ def test_the_version_tells_the_layout_of_the_structs():
         version = re.search(r'#define MOPAR_VERSION "([0-9.]+)"', f.read())[1]
     assert P.lib().mopar_version().decode() == f"mopar-mi355x {version} (gfx950)"
     assert version != "0.1" and ctypes.sizeof(L.Op) == L.Op.w5.offset + 8 + 8 + ctypes.sizeof(L.RotaryDesc)
+
+
+def test_binding_refuses_tables_whose_rows_overlap():
+    """A table of one row expanded over the sequences has no row behind the first: it is not read as if it had."""
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    row = torch.zeros(1, 3, dtype=torch.int32)
+    for table in (row.expand(5, 3), row[:, :1].expand(5, 1), torch.zeros(9, dtype=torch.int32).as_strided((3, 3), (2, 1))):
+        with pytest.raises(ValueError, match="table"):
+            P.PagedCache(k, k.clone(), table)
+    wide = torch.zeros(4, 8, dtype=torch.int32)
+    assert P.PagedCache(k, k.clone(), wide[:, 2:5]).raw.table_stride == 8
+    assert P.PagedCache(k, k.clone(), row.expand(1, 3)).raw.table_stride == 3
+    assert P.PagedCache(k, k.clone(), wide[:, :1]).raw.table_stride == 8
