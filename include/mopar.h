@@ -149,7 +149,7 @@ int mopar_plan_slices(const mopar_layer_profile* layers, int32_t n, const mopar_
  * accepted ones.  (Inside a model, MOPAR_OP_ROTARY and
  * MOPAR_OP_CAUSAL_ATTENTION run the first and the third over whole sequences.)
  * The conventions of this header hold: nothing is allocated, nothing
- * synchronises, every call is one to three kernel launches on `stream`, fit
+ * synchronises, every call is one or two kernel launches on `stream`, fit
  * for capture into a graph, and bitwise reproducible.
  *
  * Types.     MOPAR_F32 and MOPAR_BF16.  Dot products, softmax statistics,
@@ -195,7 +195,8 @@ typedef struct {
  *           positions: g = clamp((context w / 2 pi - slow) / (fast - slow))
  * m is mscale; 0 stands for 1, with YARN for 0.1 ln(f) + 1 (arXiv 2309.00071).
  * Angles are taken modulo a full turn in 64-bit fixed point, so a far position
- * costs no accuracy (error below 2^-32 turns for any int32 position). */
+ * costs no accuracy: for any int32 position the reduced angle is off by at most
+ * 2^-31 turns, and at most 2^-28 after its rounding to float32. */
 typedef enum { MOPAR_ROTARY_HALF = 0, MOPAR_ROTARY_INTERLEAVED = 1 } mopar_rotary_layout;
 typedef enum {
     MOPAR_ROTARY_NONE = 0,
@@ -257,8 +258,8 @@ typedef struct {
  * `heads` query heads of q go to q_out turned the same (q_out may be q).  Without
  * one (NULL), pos_dev, q and q_out are not read and keys are stored as they are.
  * A row with seq or slot out of range, or on an absent page, is not stored (padding
- * rows carry seq -1; their queries turn all the same).  Two rows for one slot: one
- * of them is stored, which is not defined.
+ * rows carry seq -1; their queries turn all the same).  Two rows for one slot: its
+ * contents are undefined (parts of both).
  * heads 0: no queries (q and q_out may be NULL).
  * Errors: as mopar_rotary_apply. */
 int mopar_cache_append(const mopar_cache* cache, mopar_rotary_t rotary, int64_t tokens, int32_t heads,

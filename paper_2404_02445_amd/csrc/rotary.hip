@@ -2,14 +2,15 @@
 // same on the way into the cache, and moving the accepted tokens of a drafted tree.  All three read and
 // write each byte once and are bound by HBM, or by a launch when there are few tokens.  Measured (a copy reaches 5.0 TB/s
 // here): 16384 tokens of 40 heads of 128 in bf16 turned in 73 us, 4.6 TB/s; 22k tokens of 32 + 8 + 8 heads turned and
-// stored in 119 us, 4.55 TB/s; eight tokens in 5 us, a launch and two loads in a row; 4 kept tokens in 5 us, 32 sequences'
-// in 16 layers (22 MB) in 11 us: five loads, each of which waits for the one before (offset, path, page, row).
+// stored in 119 us, 4.55 TB/s; eight tokens in 5 us, a launch and two loads in a row; up to five kept
+// tokens of four sequences in 5 us, up to eight of 32 in 16 layers (22 MB) in 11 us: a path's entries one after the other (see keep_kernel).
 //
 // Rotation.  Pair j of a token at position p turns by p w_j.  The host keeps w_j / 2 pi as a 64-bit
-// fraction of a turn, so p times it, wrapped to 64 bits, is the angle modulo a turn: exact range
-// reduction by one integer product, with an error below 2^-33 turns for any int32 position.  The top 32
-// bits give the quadrant and an angle of at most pi/4, whose sine and cosine are their Taylor
-// polynomials (degree 9 and 10: the next terms are below 2e-9).
+// fraction of a turn, so p times it, wrapped to 64 bits, is the angle modulo a turn: range reduction by one
+// integer product, off by the fraction's error (2^-64 turns) times p: 2^-33 turns for any int32 position.  Its top 32
+// bits (the others: below 2^-32 turns) give the quadrant and an angle of at most pi/4, 2^29 units of 2^-32 turns, which
+// float32 rounds by at most 16: 2^-28 turns.  Its sine and cosine are their Taylor polynomials (degree 9 and 10: the
+// next terms are below 2e-9).
 #include <algorithm>
 
 #include "internal.h"
@@ -238,9 +239,12 @@ hipError_t rotary_launch(RotaryParams& p, hipStream_t s) {
 
 // ---------------------------------------------------------------------------
 // The accepted path of a drafted tree: a thread carries one 16-byte column of the rows of one sequence, layer
-// and pool, and moves its path entries in order, eight loads before eight stores.  Entry i lands in slot i
+// and pool, and moves its path entries in order, up to eight rows before they are stored.  Entry i lands in slot i
 // after the sequence and comes from slot path[i] >= i: a slot is never written before an entry that
 // comes from it has been read, whatever the path holds.
+// What bounds it is not the bytes: the tests of an entry, its source page and its destination page are branches, and each of
+// those words is waited for before the next load, with the row that the entry before has sent for.  Eight entries are up to
+// 32 loads in a row.
 // ---------------------------------------------------------------------------
 struct KeepParams {
     unsigned char *k, *v;
