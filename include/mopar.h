@@ -162,7 +162,8 @@ int mopar_plan_slices(const mopar_layer_profile* layers, int32_t n, const mopar_
  * Infinities An attention row is not reached by what it does not see, infinities
  * and NaN.   and NaN included.  An infinity or NaN among the values that it sees
  *            reaches it whatever its weight, however small (infinities of both
- *            signs give NaN); a NaN among its scores makes it NaN.
+ *            signs give NaN); a score of NaN or +infinity makes it NaN.  A score
+ *            of -infinity has no weight: a row with no other gets zeros.
  * Rows.      A tensor of packed tokens is a mopar_rows: element (token t,
  *            head h, dim i) at data + t * token_stride + h * head_stride + i,
  *            strides in elements, so heads may sit inside wider fused rows or

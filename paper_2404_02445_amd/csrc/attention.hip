@@ -59,7 +59,7 @@ constexpr unsigned kOOB = 0x80000000u;       // a lane offset past every resourc
 // every later read of LDS for a reader of theirs (it would wait for all loads in flight).  They have no result in registers.
 // What they write is read after begin(): a count of the loads in flight and a barrier, which the compiler moves no access
 // of memory across.  m0, which they write, is in no other use (the compiler warns that it is a reserved register).
-// Wait states: one after a write of m0, five after a lane's value went into a scalar register.
+// Wait states: one after a write of m0, five after a vector instruction (a readlane) wrote a scalar register of a resource.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ u32x4 resource(const unsigned char* base) {
@@ -69,21 +69,21 @@ __device__ __forceinline__ u32x4 resource(const unsigned char* base) {
 // Two 16-byte chunks per lane, from k + kofs and v + vofs into place `lane` of the 1 KB blocks at kdst and vdst; zeros where an
 // offset is kOOB.
 __device__ __forceinline__ void load_lds(const unsigned char* k, unsigned kdst, unsigned kofs, const unsigned char* v, unsigned vdst, unsigned vofs) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds\n\t"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds\n\t"
                  "s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, 0 offen lds"
                  ::"s"(kdst), "v"(kofs), "s"(resource(k)), "s"(vdst), "v"(vofs), "s"(resource(v))
                  : "memory", "m0");
 }
 // ... from the lane's own addresses
 __device__ __forceinline__ void load_lds(const unsigned char* k, unsigned kdst, const unsigned char* v, unsigned vdst) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off\n\t"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\t"
                  "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, off"
                  ::"s"(kdst), "v"(k), "s"(vdst), "v"(v)
                  : "memory", "m0");
 }
 // One word per lane from its own address into word `lane` of dst.
 __device__ __forceinline__ void load_lds(const int32_t* src, unsigned dst) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
 }
 #pragma clang diagnostic pop
 
@@ -839,12 +839,12 @@ __global__ __launch_bounds__(WR * 64, 2) void attention_kernel(const AttnParams 
         const float inv = l != 0.0f ? 1.0f / l : 0.0f;
         unsigned char* const dst = ar->out + (start + qtok) * ar->o_ts + qhead * ar->o_hs;
         const int64_t to = static_cast<int64_t>(slot) * BM + wave * 32 + lr;
-        bool off = false;                             // a result is infinite or NaN, its row's sum is not
+        float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};     // 0 where the results are finite, else NaN
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) off |= not_finite<4>(__float_as_uint(o[d][i])) != 0;
-        off = __any(off && !not_finite<4>(__float_as_uint(l)));
+            for (int i = 0; i < 16; ++i) zero[i & 3] = __builtin_fmaf(o[d][i], 0.0f, zero[i & 3]);
+        const bool off = __any((zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.0f && l * 0.0f == 0.0f);   // results off, their sum is not
         if (wave0 + lr < nrow) {
             if (whole) {
 #pragma unroll
@@ -964,7 +964,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p)
             for (int k0 = 0; k0 < u.parts; k0 += 64) {
                 float f = 0.0f;                           // this lane's part: its weight
                 if (k0 + lane < u.parts) {
-                    f = __builtin_amdgcn_exp2f(p.stat[2 * (at(k0 + lane) + rr)] - top);
+                    // (not 0: a part's infinity counts whatever its weight)
+                    f = fmaxf(__builtin_amdgcn_exp2f(p.stat[2 * (at(k0 + lane) + rr)] - top), 0x1p-126f);
                     sum += p.stat[2 * (at(k0 + lane) + rr) + 1] * f;
                 }
                 const int n = min(64, u.parts - k0);
@@ -977,8 +978,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p)
                     for (int i = 0; i < many; ++i) {
                         const float w = __shfl(f, min(k + i, 63), 64);
 #pragma unroll
-                        for (int e = 0; e < PER; ++e)        // (a part's infinity or NaN counts whatever its weight)
-                            acc[e] += k + i < n ? not_finite<4>(__float_as_uint(v[i][e])) ? v[i][e] : v[i][e] * w : 0.0f;
+                        for (int e = 0; e < PER; ++e) acc[e] += k + i < n ? v[i][e] * w : 0.0f;
                     }
                 }
             }

@@ -552,6 +552,29 @@ def test_cache_infinities_of_tiny_weight(dt, new, heads, n, at, peak):
     check_tiny_weights(out, q[:new], k, v, seen)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 20])
+@pytest.mark.parametrize("n,at", [(60, 7), (4000, 7), (4000, 2500)])
+def test_cache_infinite_scores(dt, new, n, at):
+    """A score of +infinity or NaN makes NaN of its row, also where it is in one of many parts; one of -infinity has no weight."""
+    page, d = 16, 64
+    g = gen(22)
+    table, pages = page_table([n], page, g)
+    kc, vc = (randn(g, pages, 3, page, d, dt=dt) for _ in range(2))
+    q = torch.ones(new, 6, d, device="cuda", dtype=DT[dt])
+    p = int(table[0, at // page])
+    kc[p, 0, at % page, 5], kc[p, 1, at % page, 5], kc[p, 2, at % page, 5] = float("inf"), float("nan"), float("-inf")
+    cache = P.PagedCache(kc, vc, table.cuda())
+    out = torch.empty(new, 6, d, device="cuda", dtype=DT[dt])
+    P.mopar_attention_cache(q, out, cache, ints([0, new]), new, ints([n - new]), n, ws=P.alloc_attention_workspace(q, cache, new, n))
+    assert bool(out[:, :4].isnan().all())
+    k, v = (cache_rows(x.cpu(), table, 0, n)[:, 2:] for x in (kc, vc))
+    seen = torch.arange(n)[None] <= n - new + torch.arange(new)[:, None]
+    seen[:, at], k[at] = False, 0
+    ref, tol = attend(q[:, 4:], k, v, seen, d ** -0.5)
+    check(out[:, 4:], ref, tol)
+
+
 def test_pools_past_32_bit_offsets():
     g = gen(8)
     kv, page, d, n = 8, 256, 128, 700
