@@ -462,7 +462,9 @@ static int validate_and_build(mopar_model_s& m) {
                     op.heads > x.dims[2] / d)
                     return set_error(MOPAR_E_SHAPE, nm + ": rotary needs (B,S,n*head_dim) -> the same, 1 <= heads <= n");
                 if (d % epc != 0) return set_error(MOPAR_E_UNSUPPORTED, nm + ": head_dim must be a multiple of " + std::to_string(epc));
-                if (x.dims[1] >= (int64_t(1) << 31) || numel(x) / d >= (int64_t(1) << 31) || x.dims[2] * es >= size_t(1) << 25)
+                const int64_t lim = int64_t(1) << 31;      // (each product of factors that the ones before hold small)
+                if (x.dims[2] >= (int64_t(1) << 25) / static_cast<int64_t>(es) || x.dims[0] >= lim || x.dims[1] >= lim ||
+                    x.dims[0] * x.dims[1] >= lim || x.dims[0] * x.dims[1] * (x.dims[2] / d) >= lim)
                     return set_error(MOPAR_E_UNSUPPORTED, nm + ": 2^31 heads of tokens or rows of 32 MiB");
                 break;
             }
@@ -474,8 +476,10 @@ static int validate_and_build(mopar_model_s& m) {
                     return set_error(MOPAR_E_SHAPE, nm + ": causal attention needs (B,S,(heads+2*kv_heads)*head_dim) -> (B,S,heads*head_dim)");
                 if (d % 32 != 0) return set_error(MOPAR_E_UNSUPPORTED, nm + ": head_dim must be 32, 64, 96 or 128");
                 if (!(op.scale > 0.0f) || !std::isfinite(op.scale * 1.5f)) return set_error(MOPAR_E_ARG, nm + ": scale must be positive and at most 2^127");
-                if (x.dims[0] >= int64_t(1) << 30 || !prompt_fits(x.dims[0] * x.dims[1], static_cast<int>(x.dims[0]), x.dims[1], op.heads) ||
-                    x.dims[2] * es >= size_t(1) << 25)
+                const int64_t lim = int64_t(1) << 30;
+                if (x.dims[2] >= (int64_t(1) << 25) / static_cast<int64_t>(es) || x.dims[0] >= lim || x.dims[1] >= lim ||
+                    !prompt_fits(x.dims[0] * x.dims[1], static_cast<int>(x.dims[0]), x.dims[1], op.heads) ||
+                    x.dims[1] + 1 > (int64_t(1) << 61) / (x.dims[0] * x.dims[1] * h * d))      // (the profile's operations)
                     return set_error(MOPAR_E_UNSUPPORTED, nm + ": too many rows of heads, or rows of 32 MiB");
                 break;
             }

@@ -36,6 +36,33 @@ static mopar_cache cache_of(int32_t n_seq, int32_t kv_heads, int32_t head_dim, i
     return c;
 }
 
+// A model of one operator over b sequences of n rows of f elements.
+static int create(mopar_op op, int32_t dtype, int64_t b, int64_t n, int64_t f_in, int64_t f_out) {
+    mopar_tensor_desc t[2] = {{dtype, 3, {b, n, f_in, 0}}, {dtype, 3, {b, n, f_out, 0}}};
+    op.in0 = 0;
+    op.in1 = -1;
+    op.out = 1;
+    mopar_model_desc d{};
+    d.dtype = dtype;
+    d.n_tensors = 2;
+    d.tensors = t;
+    d.n_ops = 1;
+    d.ops = &op;
+    d.n_layers = 1;
+    d.input = 0;
+    d.output = 1;
+    static unsigned char weights[16];
+    mopar_model_t m = nullptr;
+    const int rc = mopar_model_create(&d, weights, sizeof weights, &m);
+    CHECK((rc == MOPAR_OK) == (m != nullptr));
+    if (m) {
+        mopar_layer_profile p;
+        CHECK(mopar_model_profile(m, &p) == MOPAR_OK);
+    }
+    mopar_model_destroy(m);
+    return rc;
+}
+
 int main() {
     const int32_t most = 2147483647;
     const mopar_rows rows{A, 1 << 20, 128};
@@ -56,6 +83,34 @@ int main() {
                                 CHECK(mopar_attention_cache(&a, &c, most, nullptr, max_q, nullptr, max_len, nullptr, 0, &rows, &rows, A, n,
                                                             nullptr) == (rc != MOPAR_OK ? rc : n_seq && max_q ? MOPAR_E_ARG : MOPAR_OK));
                             }
+    // the two operators in a model, of sizes whose products pass 64 bits
+    mopar_op rot_op{}, att_op{};
+    rot_op.kind = MOPAR_OP_ROTARY;
+    rot_op.heads = 1;
+    rot_op.rotary.head_dim = rot_op.rotary.rot_dim = 64;
+    rot_op.rotary.base = 10000;
+    att_op.kind = MOPAR_OP_CAUSAL_ATTENTION;
+    att_op.heads = att_op.kv_heads = 1;
+    att_op.head_dim = 64;
+    att_op.scale = 0.125f;
+    const int64_t sizes[] = {1, 7, 1 << 20, (int64_t(1) << 30) - 1, int64_t(1) << 31, int64_t(1) << 33, int64_t(1) << 47, int64_t(1) << 62};
+    for (int32_t dtype : {MOPAR_F32, MOPAR_BF16})
+        for (int64_t b : sizes)
+            for (int64_t n : sizes) {
+                const bool small = b <= 7 && n <= 7, large = b > 1 << 20 && n > 1 << 20;
+                const int r = create(rot_op, dtype, b, n, 64, 64), a = create(att_op, dtype, b, n, 192, 64);
+                CHECK(r == MOPAR_OK || r == MOPAR_E_UNSUPPORTED);
+                CHECK(a == MOPAR_OK || a == MOPAR_E_UNSUPPORTED);
+                if (small) CHECK(r == MOPAR_OK && a == MOPAR_OK);
+                if (large) CHECK(r == MOPAR_E_UNSUPPORTED && a == MOPAR_E_UNSUPPORTED);
+                CHECK(create(rot_op, dtype, b, n, int64_t(1) << 62, int64_t(1) << 62) == MOPAR_E_UNSUPPORTED);
+            }
+    for (int64_t h : {1, 65536, 2147483647}) {
+        att_op.heads = att_op.kv_heads = static_cast<int32_t>(h);
+        CHECK(create(att_op, MOPAR_F32, 1, 4, 3 * h * 64, h * 64) != MOPAR_OK || h == 1 || h == 65536);
+        rot_op.heads = static_cast<int32_t>(h);
+        create(rot_op, MOPAR_F32, 1, 4, h * 64, h * 64);
+    }
     // random sizes, small and near the ends of their types
     std::mt19937_64 rng(11);
     auto pick32 = [&]() -> int32_t {
