@@ -23,15 +23,27 @@
 //
 // Measured, with what bounds it (32 heads of 128 on 8 key heads in bf16; copies reach 5.0 TB/s here, large bf16 products 1450
 // TFLOP/s):
-//   8192 causal tokens: 510 to 550 us, 1000 to 1080 TFLOP/s.  Matrix units busy half of the time, vector units 57 %: two
-//     waves a SIMD (the registers of 32 rows x 128 dims) hide each other's softmax only in part.  Deeper LDS prefetch,
-//     32-key stages (584 us) and products issued a stage ahead of the softmax (593 us) did not help.
-//   16 prompts of 20 to 1100 tokens: 139 us; 48 us of copying and 80 us of products that blocks of the same length, started
-//     together, do not overlap.
-//   64 single tokens over 100 to 4096 cached ones: 121 us, 4.5 TB/s: memory.
-//   16 trees of 20 to 48 over 1000 to 8000: 115 to 122 us, 2.9 TB/s and 390 TFLOP/s at once; 17 us of it the join.
-//   One float32 token over 16400, 12 heads of 64: 38 us, 2.6 TB/s: a wave's float32 products for 32 rows of which one counts
-//     (12 us) behind its loads, and the join (7 us).
+//   8192 causal tokens: 530 to 560 us on different cards, 980 to 1040 TFLOP/s.  Matrix units busy 51 % of the time, vector
+//     instructions active 46 %: two waves a SIMD (the registers of 32 rows x 128 dims) hide each other's softmax only in part.
+//     Deeper LDS prefetch, 32-key stages and products issued a stage ahead of the softmax did not help.
+//   16 prompts of 20 to 1100 tokens: 138 to 145 us.  Their bytes are 48 us of copying, their products 80 us at the rate above;
+//     the rest is the edges of tiles and, in each short tile, the time to its first keys.
+//   64 single tokens over 100 to 4096 cached ones: 122 to 126 us, 4.3 to 4.4 TB/s: memory.
+//   16 trees of 20 to 48 over 1000 to 8000: 118 us, 17 us of it the join.  Neither memory (2.9 TB/s) nor the matrix units (19 %
+//     busy): waves wait half of their time, one block a CU with a barrier a stage, of whose eight waves three to six have rows.
+//   One float32 token over 16400, 12 heads of 64: 38 to 40 us, 2.6 TB/s: a wave's float32 products for 32 rows of which one
+//     counts (12 us) behind its loads, and the join (7 us).
+// What costs more than its work:
+//   Pages whose rows of a key head do not fill 1 KB of LDS (fewer than 4 tokens of 128 bf16 dims, 16 of 32): every stage is
+//     masked and looks its pages up key by key.  64 single tokens over 2000: 107 us in pages of 4 or 16, 232 in pages of 1 or 2.
+//   max_len far past the sequences: it alone decides whether blocks share.  64 single tokens over 200: 16 us with a max_len of
+//     201, 21 with 4096.
+//   Thousands of short sequences: each block looks all of them up, 64 at a time.  Prompts of 32 tokens: 512 in 99 us, 4096 in
+//     1270; single tokens over 60: 37 and 274.
+//   Many new tokens without a mask over a cache: each row meets all the new keys, masked.  2048 over nothing 145 us, where as
+//     a prompt they take 52.
+// Scalar registers do not suffice over a cache: 8 to 70 are kept in lanes of vector registers, and some forms have a few bytes of
+// scratch for that; no vector register is spilled.
 #include <algorithm>
 #include <type_traits>
 
