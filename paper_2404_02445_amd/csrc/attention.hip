@@ -42,7 +42,7 @@
 //     1270; single tokens over 60: 37 and 274.
 //   Many new tokens without a mask over a cache: each row meets all the new keys, masked.  2048 over nothing 145 us, where as
 //     a prompt they take 52.
-// Scalar registers do not suffice over a cache: 8 to 70 are kept in lanes of vector registers, and some forms have a few bytes of
+// Scalar registers do not suffice over a cache: 15 to 67 are kept in lanes of vector registers, and some forms have a few bytes of
 // scratch for that; no vector register is spilled.
 #include <algorithm>
 #include <type_traits>
