@@ -3,8 +3,9 @@
 Row tensors are [tokens, heads, head_dim] views whose last dimension is contiguous (slices of fused
 rows included); pools are [pages, kv_heads, page_tokens, head_dim], or with a leading [layers].  Device
 integers are contiguous int32 tensors.  Every call runs on ``stream``, by default the current stream
-of the tensors' device.  Sizes that the library cannot see (one tensor against another) are checked here
-and raise ``ValueError``; the library's own refusals raise ``MoparError``.
+of the tensors' device; on another stream than the one that allocated them, tensors (the workspace among
+them) are the caller's to keep until the work is done.  Sizes that the library cannot see (one tensor
+against another) are checked here and raise ``ValueError``; the library's own refusals raise ``MoparError``.
 """
 from __future__ import annotations
 
