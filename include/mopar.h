@@ -343,6 +343,96 @@ int mopar_cache_keep(const mopar_cache* cache, int32_t layers, int64_t layer_str
                      void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Decoder steps in 8 bits                                                   */
+/* ------------------------------------------------------------------------ */
+
+/* What a decoder does between its attention calls, on rows of tokens: the residual
+ * stream's norm, products with weights in 8 bits, and what the logits say.  Forward
+ * only, as the rest of the library.  dtype is MOPAR_F32 or MOPAR_BF16 throughout;
+ * sums, statistics and scales are float32 or wider. */
+
+/* Rows of contiguous elements, row t at data + t * stride elements.  data needs only
+ * its elements' alignment and stride none (16-byte rows are read fastest).  Rows
+ * that are read may overlap (stride 0: one row for all); rows that are written may
+ * not. */
+typedef struct {
+    void* data;
+    int64_t stride;
+} mopar_matrix;
+
+/* Rows in 8 bits: element i of row t stands for q[t * stride + i] * scale[t].  q is
+ * 16-byte aligned and stride a multiple of 16, less than 2^23; the bytes of a row
+ * up to the next multiple of 16 must be the caller's too (they are read and do not
+ * count; nothing writes them). */
+typedef struct {
+    int8_t* q;
+    int64_t stride;
+    float* scale;               /* 4-byte aligned */
+} mopar_rows8;
+
+/* Root mean square norm of the residual stream.  h = x, or x + residual rounded to
+ * dtype and stored in `total` (residual and total may be NULL, total only with
+ * residual);  r = 1 / sqrt(mean(h^2) + eps);
+ *   out  = h r weight, rounded once (NULL: not stored)
+ *   out8 = h r weight in 8 bits, not rounded before (NULL: not stored): with p = h weight
+ *          and a = max |p| of the row, q = 127 p / a rounded to the nearest integer, halves
+ *          to even, as 64-bit arithmetic gives it, and scale = a r / 127.  A row of zeros has
+ *          scale 0; one with an infinity or NaN has zeros and scale NaN.
+ * The sum of squares is taken in float32, so rows whose squares pass its range are off.
+ * `width` 1 .. 2^24 elements a row, weight [width] in dtype.  total may be x or residual, out may be x
+ * or residual when total is NULL or another (same data and stride); any other
+ * overlap is undefined.  tokens 0: nothing to do.
+ * Errors: MOPAR_E_ARG (also neither out nor out8), MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (2^31 tokens,
+ * 2^46 elements between the first and the last row), MOPAR_E_HIP. */
+int mopar_rms_norm(int32_t dtype, int64_t tokens, int32_t width, const mopar_matrix* x, const mopar_matrix* residual,
+                   const mopar_matrix* total, const void* weight, float eps, const mopar_matrix* out,
+                   const mopar_rows8* out8, void* stream);
+
+typedef enum { MOPAR_GATE_NONE = 0, MOPAR_GATE_SILU = 1, MOPAR_GATE_GELU = 2 } mopar_gate;
+
+/* Rows in 8 bits: p = x (MOPAR_GATE_NONE; gate NULL), silu(gate) x = gate x / (1 + e^-gate),
+ * or gelu(gate) x = gate (1 + erf(gate / sqrt 2)) / 2 x, not rounded before; q and scale = a / 127
+ * as for mopar_rms_norm, as 64-bit arithmetic gives them where the gate's activation stays in
+ * float32's normal range.  Also how weights [n_out][width] are made: a row of theirs is
+ * a channel.  Errors: as mopar_rms_norm. */
+int mopar_quantize_rows(int32_t dtype, int64_t tokens, int32_t width, const mopar_matrix* x, const mopar_matrix* gate,
+                        int32_t act, const mopar_rows8* out8, void* stream);
+
+/* out[t][n] = (sum_i x.q[t][i] w.q[n][i]) x.scale[t] w.scale[n] + bias[n], for x of `tokens` and w of n_out
+ * rows of `width` (1 .. 131071: the sum is exact in 32 bits) values of 8 bits, -128 .. 127; out and bias
+ * (NULL: none) in dtype, rounded once.  Sums are exact in any order, so how a product is cut never shows
+ * in its bits.  `ws` holds mopar_linear8_workspace_bytes, which does not fall as tokens, n_out or width grow;
+ * NULL: long sums with few results are not shared out, which is right and slower.  Its contents need not
+ * survive between calls, and calls that overlap need one each.  out must overlap nothing
+ * that is read.  tokens or n_out 0: nothing to do.
+ * Errors: MOPAR_E_ARG, MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (2^31 rows, width, strides, 2^46 elements from
+ * the first to the last row of out, 2^23 tiles of 64 by 64 results), MOPAR_E_WORKSPACE, MOPAR_E_HIP. */
+int mopar_linear8_workspace_bytes(int64_t tokens, int64_t n_out, int32_t width, size_t* bytes);
+int mopar_linear8(int32_t dtype, int64_t tokens, int64_t n_out, int32_t width, const mopar_rows8* x, const mopar_rows8* w,
+                  const void* bias, const mopar_matrix* out, void* ws, size_t ws_bytes, void* stream);
+
+/* What logits say.  With z = scale * logits (scale > 0, finite: an inverse temperature), for each row
+ *   logprob      z[token] - ln sum exp z
+ *   entropy      of the softmax of z (NULL: not stored); what has no weight adds nothing
+ *   rank         how many logits are larger than the token's (NULL: not stored)
+ *   top_id, top_logprob [row * top + j]  the `top` (0 .. 64, at most vocab) largest logits, largest first, equal
+ *                ones by index (-0 equals 0), and their log probabilities; NULL with top 0
+ * Logits of -infinity, or of their type's lowest value beside larger ones, have no weight.  A row of
+ * nothing but -infinity: log probabilities -infinity, entropy 0.  One with NaN or +infinity: its
+ * log probabilities and entropy are NaN; NaN is no alternative and larger than nothing, and
+ * places without an alternative hold id -1 and NaN.  A token outside [0, vocab) (padding) has log probability
+ * -infinity and rank vocab.  All outputs are packed arrays on the device.
+ * `ws` holds mopar_token_logprobs_workspace_bytes, which does not fall as rows, vocab or top grow;
+ * NULL: a row is not shared out among blocks, which is right and slower for few rows.  Its contents need not survive
+ * between calls, and calls that overlap need one each.  rows 0: nothing to do.
+ * Errors: MOPAR_E_ARG, MOPAR_E_DTYPE, MOPAR_E_UNSUPPORTED (2^24 rows, vocab of 2^28, 2^46 elements from the
+ * first to the last row), MOPAR_E_WORKSPACE, MOPAR_E_HIP. */
+int mopar_token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t top, size_t* bytes);
+int mopar_token_logprobs(int32_t dtype, int64_t rows, int32_t vocab, const mopar_matrix* logits, float scale,
+                         const int32_t* token_dev, int32_t top, float* logprob_dev, float* entropy_dev, int32_t* rank_dev,
+                         float* top_logprob_dev, int32_t* top_id_dev, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Model description                                                         */
 /* ------------------------------------------------------------------------ */
 

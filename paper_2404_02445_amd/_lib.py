@@ -23,6 +23,7 @@ OP_ROTARY, OP_CAUSAL_ATTENTION = 10, 11
 ROTARY_LAYOUT, ROTARY_SCALING = {"half": 0, "interleaved": 1}, {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 ACT = {"none": 0, "relu": 1, "gelu": 2}
 CODEC_RAW, CODEC_AE = 0, 1
+GATE = {"none": 0, "silu": 1, "gelu": 2}
 # MOPAR_STATIC_WORKSPACE_BYTES of include/mopar.h: the static workspace of mopar_model_forward_static
 STATIC_WORKSPACE_BYTES = 64 << 20
 STATUS_NAMES = {0: "OK", 1: "E_ARG", 2: "E_SHAPE", 3: "E_DTYPE", 4: "E_UNSUPPORTED", 5: "E_INFEASIBLE",
@@ -103,6 +104,15 @@ class Attention(ctypes.Structure):
                 ("reserved", c_i32)]
 
 
+class Matrix(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("stride", c_i64)]
+
+
+class Rows8(ctypes.Structure):
+    _fields_ = [("q", c_vp), ("stride", c_i64), ("scale", c_vp)]
+
+
+P_MATRIX, P_ROWS8 = ctypes.POINTER(Matrix), ctypes.POINTER(Rows8)
 P_ROWS, P_CACHE, P_ATT = ctypes.POINTER(Rows), ctypes.POINTER(Cache), ctypes.POINTER(Attention)
 
 # every exported symbol of include/mopar.h, with its signature
@@ -145,6 +155,13 @@ SIGNATURES = {
     "mopar_attention_cache_workspace_bytes": (c_i32, [P_ATT, P_CACHE, c_i64, c_i32, c_i32, ctypes.POINTER(ctypes.c_size_t)]),
     "mopar_attention_cache": (c_i32, [P_ATT, P_CACHE, c_i64, c_vp, c_i32, c_vp, c_i32, c_vp, c_i32, P_ROWS, P_ROWS, c_vp,
                                       ctypes.c_size_t, c_vp]),
+    "mopar_rms_norm": (c_i32, [c_i32, c_i64, c_i32, P_MATRIX, P_MATRIX, P_MATRIX, c_vp, c_f32, P_MATRIX, P_ROWS8, c_vp]),
+    "mopar_quantize_rows": (c_i32, [c_i32, c_i64, c_i32, P_MATRIX, P_MATRIX, c_i32, P_ROWS8, c_vp]),
+    "mopar_linear8_workspace_bytes": (c_i32, [c_i64, c_i64, c_i32, ctypes.POINTER(ctypes.c_size_t)]),
+    "mopar_linear8": (c_i32, [c_i32, c_i64, c_i64, c_i32, P_ROWS8, P_ROWS8, c_vp, P_MATRIX, c_vp, ctypes.c_size_t, c_vp]),
+    "mopar_token_logprobs_workspace_bytes": (c_i32, [c_i64, c_i32, c_i32, ctypes.POINTER(ctypes.c_size_t)]),
+    "mopar_token_logprobs": (c_i32, [c_i32, c_i64, c_i32, P_MATRIX, c_f32, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                     ctypes.c_size_t, c_vp]),
     "mopar_last_error": (ctypes.c_char_p, []),
     "mopar_version": (ctypes.c_char_p, []),
 }

@@ -258,6 +258,47 @@ hipError_t launch_attention_cache(const mopar_attention& a, const mopar_cache& c
                                   int max_q, const int32_t* len, int max_len, const uint64_t* mask, int mask_words,
                                   const mopar_rows* q, const mopar_rows* out, void* ws, hipStream_t s);
 
+// Decoder steps in 8 bits (sizes checked by the entry points)
+struct RowsJob {
+    int dtype;
+    int64_t tokens;
+    int width;
+    mopar_matrix x, residual, total, out;      // data null: absent
+    const void* weight;                        // null: no norm
+    float eps;
+    mopar_matrix gate;
+    int act;                                   // mopar_gate
+    mopar_rows8 out8;                          // q null: absent
+};
+hipError_t launch_rows8(const RowsJob& j, hipStream_t s);
+
+// How a product of 8-bit rows is cut: tile sizes and shares of its sum.  A function of the sizes alone.
+struct Linear8Plan {
+    int bm, bn, splits;
+};
+Linear8Plan linear8_plan(int64_t m, int64_t n, int k, size_t ws_bytes);
+size_t linear8_ws_bytes(int64_t m, int64_t n, int k);
+hipError_t launch_linear8(int dtype, int64_t m, int64_t n, int k, const mopar_rows8& x, const mopar_rows8& w, const void* bias,
+                          const mopar_matrix& out, void* ws, const Linear8Plan& plan, hipStream_t s);
+
+struct LogprobJob {
+    int dtype;
+    int64_t rows;
+    int vocab;
+    mopar_matrix logits;
+    float scale;
+    const int32_t* token;
+    int top;
+    float *logprob, *entropy;
+    int32_t* rank;
+    float* top_logprob;
+    int32_t* top_id;
+};
+// blocks that share a row, and the bytes of their partial results
+int logprob_splits(int64_t rows, int vocab);
+size_t logprob_ws_bytes(int64_t rows, int vocab, int top);
+hipError_t launch_token_logprobs(const LogprobJob& j, int splits, void* ws, hipStream_t s);
+
 size_t dtype_size(int dtype);
 
 }  // namespace mopar
