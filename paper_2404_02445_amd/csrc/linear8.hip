@@ -8,6 +8,7 @@
 // rows (1 KB) a load instruction; chunk c of row r sits at place c ^ (r % 8), which keeps the fragment reads (16 rows, one
 // chunk each) off each other's banks.  Chunks past the sum read zeros; a chunk that the sum ends in is cut in
 // the fragments of x.
+#pragma clang diagnostic ignored "-Winline-asm"      // (m0, which the loads into LDS take, is in no other use)
 #include <algorithm>
 #include <type_traits>
 
@@ -39,22 +40,29 @@ struct Linear8Params {
     int k, splits;
     int mt, nt, total, per_xcd;  // tiles, those of all shares, and an XCD's
     int nk;                      // 128-byte steps of a share
+    // linear8_pair_kernel: tiles a block, and the divisors of the tiles' order
+    int chunk;
+    FastDiv div_group, div_last;
 };
 
 // Direct loads into LDS are inline asm, so that the compiler does not take every later read of LDS for a reader of theirs (it would
 // wait for all loads in flight); they have no result in registers.  What they write is read after a counted wait and a
 // barrier.  (Five wait states between a vector instruction's write of a scalar register and its use as a resource or offset.)
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
+// in a scalar register (a step that the compiler knows is none that a load takes)
+__device__ __forceinline__ unsigned opaque(unsigned v) {
+    v = __builtin_amdgcn_readfirstlane(v);
+    asm volatile("" : "+s"(v));
+    return v;
+}
 __device__ __forceinline__ void load_lds(u32x4 rsrc, unsigned dst, unsigned voff, unsigned soff) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 ::"s"(dst), "v"(voff), "s"(rsrc), "s"(soff)
+                 ::"s"(opaque(dst)), "v"(voff), "s"(rsrc), "s"(opaque(soff))
                  : "memory", "m0");
 }
-#pragma clang diagnostic pop
 __device__ __forceinline__ u32x4 resource(const int8_t* base) {
-    const uint64_t a = reinterpret_cast<uint64_t>(base);
-    return u32x4{static_cast<unsigned>(a), static_cast<unsigned>(a >> 32) & 0xffffu, 0x7fffffffu, kRsrcWord3};
+    const uint64_t a = reinterpret_cast<uint64_t>(base);          // (the same in every lane)
+    const unsigned lo = __builtin_amdgcn_readfirstlane(static_cast<unsigned>(a)), hi = __builtin_amdgcn_readfirstlane(static_cast<unsigned>(a >> 32));
+    return u32x4{lo, hi & 0xffffu, 0x7fffffffu, kRsrcWord3};
 }
 
 // the first n bytes of a chunk (n < 16; none with n <= 0)
@@ -205,6 +213,434 @@ __global__ __launch_bounds__(WM * WN * 64) void linear8_kernel(const Linear8Para
     }
 }
 
+// ---------------------------------------------------------------------------
+// Large products: 256 x 256 or 128 x 128 tiles on v_mfma_i32_32x32x32_i8, eight waves in two groups that take turns on
+// the matrix units.
+//
+// Waves 0-3 (one a SIMD) own the upper half of the tile's rows, waves 4-7 the lower, each TILE / 2 x TILE / 4 results.
+// A step of k is 128 bytes; with 256 x 256 tiles it is worked in two phases, the upper (A0) and the lower half (A1) of the wave's
+// rows against all its columns.  A phase is a memory step (fragment reads, loads of later steps) and an MFMA step, with a
+// barrier behind each, and the second group runs one step behind the first: while one wave of a SIMD multiplies, the other
+// reads and loads.  256: two stages of 64 KB in LDS; A0 and the columns' halves (B) are read in the first phase and loaded again,
+// for the step after next, in the second; A1 the other way round.  128: one phase, four stages of 32 KB, loads three steps
+// ahead.  At the end of a memory step eight later loads stay in flight.
+//
+// A block runs up to kPairTiles tiles, and the loads go on into the next one during the last steps of a tile.  The scales of a
+// tile come to LDS with its first step, into the wave's own space, where its results turn at the end so that a store covers
+// whole rows of the wave's part.
+// ---------------------------------------------------------------------------
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+constexpr int kPairTiles = 4;
+
+// the lane, worked out anew from here on: what a loop needs rarely is not kept in registers across it
+__device__ __forceinline__ int lane_again(int lane) {
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+// one word a lane from its own address into word `lane` of dst
+__device__ __forceinline__ void load_lds_word(const float* src, unsigned dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(opaque(dst)), "v"(src) : "memory", "m0");
+}
+
+template <int N, typename F, int I = 0> __device__ __forceinline__ void static_for(F&& f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<N, F, I + 1>(static_cast<F&&>(f));
+    }
+}
+
+// WHOLE: every row of results is whole 16-byte groups on 16-byte addresses
+template <typename T, int TILE, bool WHOLE>
+__global__ __launch_bounds__(512, 2) void linear8_pair_kernel(const Linear8Params p) {
+    constexpr int TM = TILE / 2, TN = TILE / 4;          // a wave's part
+    constexpr int IA = TM / 32, NJ = TN / 32;            // its 32 x 32 tiles
+    constexpr int HALVES = TILE / 128;                   // 128-row halves of an operand's stage
+    constexpr unsigned HALF = 16384, STAGE = 2 * HALVES * HALF, RING = 131072;   // a stage holds A0 (A1) B0 (B1)
+    constexpr unsigned OWN = 4096;                       // a wave's space: scales, then results
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[RING + 8 * OWN];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 2, wn = wave & 3, lrow = lane & 31, lhalf = lane >> 5;
+    const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<size_t>((lds_ptr_t)(&lds[0])));
+
+    // --- the block's tiles: number first + 32 j of its XCD's run ---------------------------------
+    const int t_lo = static_cast<int>(blockIdx.x & 7) * p.per_xcd, t_end = min(p.per_xcd, p.total - t_lo);
+    const int li = static_cast<int>(blockIdx.x >> 3);
+    int t_next = (li >> 5) * 32 * p.chunk + (li & 31);
+    const int t_last = min(t_end, ((li >> 5) + 1) * 32 * p.chunk);
+    struct Tile { int64_t m0, n0; };
+    auto take = [&](Tile& tl) __attribute__((always_inline)) -> bool {
+        if (t_next >= t_last) return false;
+        const unsigned t = static_cast<unsigned>(t_lo + t_next);
+        t_next += 32;
+        const unsigned group = p.div_group.div(t), within = t - group * static_cast<unsigned>(8 * p.nt);
+        const bool last = static_cast<int>(group) == (p.mt - 1) / 8;
+        const unsigned gm = last ? static_cast<unsigned>(p.mt) - group * 8 : 8;
+        const unsigned nti = last ? p.div_last.div(within) : within / 8;
+        tl.n0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(nti))) * TILE;
+        tl.m0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(group * 8 + (within - nti * gm)))) * TILE;
+        return true;
+    };
+    Tile cur, ahead;
+    if (!take(cur)) return;                              // (the whole block, before any barrier)
+    ahead = cur;
+    bool live = true;                                    // the loads still have a tile
+
+    // --- operand loads -----------------------------------------------------------------------------
+    // A half is 16 blocks of 1 KB (8 rows x 128 bytes); wave w loads blocks w and w + 8.  Chunk c of row r sits at place
+    // c ^ (r % 8) ^ (bit 4 of r), which keeps the 32-row fragment reads off each other's banks.  Row r of A half i is tile row
+    // TM (r / 64) + 64 i + r % 64, row r of B half j tile column TN (r / 32) + 32 j + r % 32.
+    const int nk = p.nk, ktail = (p.k & 127) ? nk - 1 : nk;      // nk >= 2 (256) or 3 (128): see the launcher
+    u32x4 va = {}, vb = {};                              // element 2 half + slot
+    const int8_t *xb = nullptr, *wb = nullptr;           // of the tile that loads are at
+    int ikt = 0;
+    unsigned koff = 0, dst = lds0 + static_cast<unsigned>(wave) * 1024u;
+    auto offsets = [&]() __attribute__((always_inline)) {
+        xb = p.x + ahead.m0 * p.xs, wb = p.w + ahead.n0 * p.ws;
+        const int mleft = static_cast<int>(min<int64_t>(p.m - 1 - ahead.m0, TILE - 1)), nleft = static_cast<int>(min<int64_t>(p.n - 1 - ahead.n0, TILE - 1));
+        const int ln = lane_again(lane), cl = (ln & 7) ^ (ln >> 3) ^ ((wave >> 1) & 1);
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int r = (wave + 8 * s) * 8 + (ln >> 3);
+                const int m = min((r >> 6) * TM + h * 64 + (r & 63), mleft), n = min((r >> 5) * TN + h * 32 + (r & 31), nleft);
+                va[2 * h + s] = static_cast<unsigned>(m) * static_cast<unsigned>(p.xs) + static_cast<unsigned>(cl * 16);
+                vb[2 * h + s] = static_cast<unsigned>(n) * static_cast<unsigned>(p.ws) + static_cast<unsigned>(cl * 16);
+            }
+    };
+    auto load_a = [&](auto h) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) load_lds(resource(xb), dst + h * HALF + s * 8192, va[2 * h + s], koff);
+    };
+    auto load_b = [&](auto h) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) load_lds(resource(wb), dst + (HALVES + h) * HALF + s * 8192, vb[2 * h + s], koff);
+    };
+    // the loads go on to the next step: of the same tile, or the first of the block's next one
+    unsigned ring = 0;
+    auto load_next = [&]() __attribute__((always_inline)) {
+        ring = (ring + STAGE) & (RING - 1);
+        dst = lds0 + ring + static_cast<unsigned>(wave) * 1024u;
+        koff += 128;
+        ++ikt;
+        if (ikt == nk) {
+            ikt = 0;
+            koff = 0;
+            live = live && take(ahead);
+            if (live) {
+                offsets();
+            } else {
+                va = vb = u32x4{kOOB, kOOB, kOOB, kOOB};
+            }
+        } else if (ikt == ktail) {                       // chunks past the sum
+            const int ln = lane_again(lane), cl = (ln & 7) ^ (ln >> 3) ^ ((wave >> 1) & 1);
+            const unsigned past = ikt * 128 + cl * 16 >= p.k ? kOOB : 0u;
+            va |= past, vb |= past;
+        }
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, HALVES - 1>;
+    offsets();
+    if constexpr (TILE == 256) {                         // step 0, and step 1 but for A1
+        load_b(I0{}), load_b(I1{}), load_a(I0{}), load_a(I1{});
+        load_next();
+        load_b(I0{}), load_b(I1{}), load_a(I0{});
+    } else {                                             // steps 0, 1 and 2
+#pragma unroll
+        for (int u = 0; u < 3; ++u) {
+            if (u) load_next();
+            load_b(I0{}), load_a(I0{});
+        }
+    }
+    // the scales of the wave's rows and columns to its own space: TM row scales, then at 512 TN column scales
+    constexpr int SCALES = (TM + 63) / 64 + 1;
+    const unsigned own = RING + static_cast<unsigned>(wave) * OWN;
+    auto load_scales = [&]() __attribute__((always_inline)) {
+        const int ln = lane_again(lane);
+#pragma unroll
+        for (int i = 0; i < SCALES - 1; ++i)
+            load_lds_word(p.sx + min<int64_t>(cur.m0 + wm * TM + i * 64 + ln, p.m - 1), lds0 + own + i * 256);
+        load_lds_word(p.sw + min<int64_t>(cur.n0 + wn * TN + ln, p.n - 1), lds0 + own + 512);
+    };
+
+    // --- fragments: lane's 16 bytes of 32 of k, row l % 32 of a 32-row tile, chunk 2 kk + l / 32 -----
+    unsigned fa[4], fb[4];
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+        const unsigned f = lds0 + (lrow >> 3) * 1024 + (lrow & 7) * 128 + (((2 * kk + lhalf) ^ (lrow & 7) ^ (lrow >> 4)) << 4);
+        fa[kk] = f + wm * 8192;
+        fb[kk] = f + wn * 4096;
+    }
+    u32x4 af[2][4], bf[NJ][4];
+    i32x16 acc[HALVES][2][NJ];                           // [A half][row tile][column tile]
+    unsigned roff = 0;                                   // the stage that fragments come from
+    bool stored = false;                                 // a tile's stores, of a known number, are behind
+    constexpr int STORES = WHOLE ? IA * NJ * (sizeof(T) == 4 ? 4 : 2) : 0;
+    const int cut = p.k & 15 ? p.k >> 7 : -1;            // the step that a chunk is cut in
+    int kt = 0;
+    // The end of a memory step, whose reads are there: wait for the loads that the next memory step reads, the eight issued since staying in
+    // flight (in a tile's first step the scales' loads and the stores of the tile before lie between them).  Then the MFMAs.
+    auto mfma_step = [&](auto i, auto first) __attribute__((always_inline)) {
+        if constexpr (decltype(first)::value) {
+            if (WHOLE && stored)
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(8 + SCALES + STORES) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(8 + SCALES) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        }
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        if (kt == cut) {
+            const int left = p.k - kt * 128 - (lane_again(lane) >> 5) * 16;
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+                for (int a = 0; a < 2; ++a) af[a][kk] = first_bytes(af[a][kk], left - kk * 32);
+        }
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+                    acc[i][a][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, bf[j][kk]), __builtin_bit_cast(i32x4, af[a][kk]),
+                                                                         acc[i][a][j], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // The reads and loads of a memory step, and the wait for the reads, in one piece of assembly: the compiler would not let
+    // the reads go ahead of the loads' issue, which holds a wave for some 50 cycles each.
+    auto step = [&](auto first) __attribute__((always_inline)) {
+        unsigned a[4], b[4];
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) a[kk] = fa[kk] + roff, b[kk] = fb[kk] + roff;
+        if constexpr (TILE == 256) {
+            const u32x4 rx1 = resource(xb);              // A1 of the step that load_next leaves
+            const unsigned dst1 = dst + HALF, koff1 = opaque(koff), v0 = va[2 * HALVES - 2], v1 = va[2 * HALVES - 1];
+            load_next();
+            asm volatile(
+                "ds_read_b128 %0, %16 offset:32768\n\tds_read_b128 %8, %20\n\tds_read_b128 %4, %16 offset:49152\n\tds_read_b128 %12, %20 offset:4096\n\t"
+                "ds_read_b128 %1, %17 offset:32768\n\tds_read_b128 %9, %21\n\tds_read_b128 %5, %17 offset:49152\n\tds_read_b128 %13, %21 offset:4096\n\t"
+                "ds_read_b128 %2, %18 offset:32768\n\tds_read_b128 %10, %22\n\tds_read_b128 %6, %18 offset:49152\n\tds_read_b128 %14, %22 offset:4096\n\t"
+                "ds_read_b128 %3, %19 offset:32768\n\tds_read_b128 %11, %23\n\tds_read_b128 %7, %19 offset:49152\n\tds_read_b128 %15, %23 offset:4096\n\t"
+                "s_mov_b32 m0, %24\n\ts_nop 0\n\tbuffer_load_dwordx4 %25, %27, %28 offen lds\n\t"
+                "s_add_u32 m0, m0, 8192\n\ts_nop 0\n\tbuffer_load_dwordx4 %26, %27, %28 offen lds\n\t"
+                "s_waitcnt lgkmcnt(0)"
+                : "=&v"(bf[0][0]), "=&v"(bf[0][1]), "=&v"(bf[0][2]), "=&v"(bf[0][3]), "=&v"(bf[NJ - 1][0]), "=&v"(bf[NJ - 1][1]), "=&v"(bf[NJ - 1][2]),
+                  "=&v"(bf[NJ - 1][3]), "=&v"(af[0][0]), "=&v"(af[0][1]), "=&v"(af[0][2]), "=&v"(af[0][3]), "=&v"(af[1][0]), "=&v"(af[1][1]),
+                  "=&v"(af[1][2]), "=&v"(af[1][3])
+                : "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "s"(opaque(dst1)), "v"(v0), "v"(v1), "s"(rx1), "s"(koff1)
+                : "memory", "m0", "scc");
+            if constexpr (decltype(first)::value) load_scales();
+            mfma_step(I0{}, first);
+            const unsigned ko = opaque(koff);
+            asm volatile(
+                "ds_read_b128 %0, %8 offset:16384\n\tds_read_b128 %4, %8 offset:20480\n\tds_read_b128 %1, %9 offset:16384\n\tds_read_b128 %5, %9 offset:20480\n\t"
+                "ds_read_b128 %2, %10 offset:16384\n\tds_read_b128 %6, %10 offset:20480\n\tds_read_b128 %3, %11 offset:16384\n\tds_read_b128 %7, %11 offset:20480\n\t"
+                "s_add_u32 m0, %12, 32768\n\ts_nop 0\n\tbuffer_load_dwordx4 %13, %20, %21 offen lds\n\t"
+                "s_add_u32 m0, m0, 8192\n\ts_nop 0\n\tbuffer_load_dwordx4 %14, %20, %21 offen lds\n\t"
+                "s_add_u32 m0, m0, 8192\n\ts_nop 0\n\tbuffer_load_dwordx4 %15, %20, %21 offen lds\n\t"
+                "s_add_u32 m0, m0, 8192\n\ts_nop 0\n\tbuffer_load_dwordx4 %16, %20, %21 offen lds\n\t"
+                "s_mov_b32 m0, %12\n\ts_nop 0\n\tbuffer_load_dwordx4 %17, %19, %21 offen lds\n\t"
+                "s_add_u32 m0, m0, 8192\n\ts_nop 0\n\tbuffer_load_dwordx4 %18, %19, %21 offen lds\n\t"
+                "s_waitcnt lgkmcnt(0)"
+                : "=&v"(af[0][0]), "=&v"(af[0][1]), "=&v"(af[0][2]), "=&v"(af[0][3]), "=&v"(af[1][0]), "=&v"(af[1][1]), "=&v"(af[1][2]), "=&v"(af[1][3])
+                : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "s"(opaque(dst)), "v"(vb[0]), "v"(vb[1]), "v"(vb[2 * HALVES - 2]), "v"(vb[2 * HALVES - 1]), "v"(va[0]),
+                  "v"(va[1]), "s"(resource(xb)), "s"(resource(wb)), "s"(ko)
+                : "memory", "m0", "scc");
+            roff ^= STAGE;
+            mfma_step(I1{}, first);
+        } else {
+            load_next();
+            const unsigned ko = opaque(koff);
+            asm volatile(
+                "ds_read_b128 %0, %12 offset:16384\n\tds_read_b128 %4, %16\n\tds_read_b128 %8, %16 offset:4096\n\t"
+                "ds_read_b128 %1, %13 offset:16384\n\tds_read_b128 %5, %17\n\tds_read_b128 %9, %17 offset:4096\n\t"
+                "ds_read_b128 %2, %14 offset:16384\n\tds_read_b128 %6, %18\n\tds_read_b128 %10, %18 offset:4096\n\t"
+                "ds_read_b128 %3, %15 offset:16384\n\tds_read_b128 %7, %19\n\tds_read_b128 %11, %19 offset:4096\n\t"
+                "s_add_u32 m0, %20, 16384\n\ts_nop 0\n\tbuffer_load_dwordx4 %21, %26, %27 offen lds\n\t"
+                "s_add_u32 m0, m0, 8192\n\ts_nop 0\n\tbuffer_load_dwordx4 %22, %26, %27 offen lds\n\t"
+                "s_mov_b32 m0, %20\n\ts_nop 0\n\tbuffer_load_dwordx4 %23, %25, %27 offen lds\n\t"
+                "s_add_u32 m0, m0, 8192\n\ts_nop 0\n\tbuffer_load_dwordx4 %24, %25, %27 offen lds\n\t"
+                "s_waitcnt lgkmcnt(0)"
+                : "=&v"(bf[0][0]), "=&v"(bf[0][1]), "=&v"(bf[0][2]), "=&v"(bf[0][3]), "=&v"(af[0][0]), "=&v"(af[0][1]), "=&v"(af[0][2]), "=&v"(af[0][3]),
+                  "=&v"(af[1][0]), "=&v"(af[1][1]), "=&v"(af[1][2]), "=&v"(af[1][3])
+                : "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "s"(opaque(dst)), "v"(vb[0]), "v"(vb[1]), "v"(va[0]),
+                  "v"(va[1]), "s"(resource(xb)), "s"(resource(wb)), "s"(ko)
+                : "memory", "m0", "scc");
+            if constexpr (decltype(first)::value) load_scales();
+            roff = (roff + STAGE) & (RING - 1);
+            mfma_step(I0{}, first);
+        }
+    };
+    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");     // what the first phase of step 0 reads
+    __builtin_amdgcn_s_barrier();
+    if (wave >= 4) __builtin_amdgcn_s_barrier();         // the second group runs one step behind
+    asm volatile("" ::: "memory");
+    for (;;) {
+#pragma unroll
+        for (int i = 0; i < HALVES; ++i)
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[i][a][j][e] = 0;
+        kt = 0;
+        step(std::true_type{});
+        for (kt = 1; kt < nk; ++kt) step(std::false_type{});
+        // --- results: rows m0 + TM wm + 32 ia + l % 32, columns n0 + TN wn + 32 j + 8 g + 4 (l / 32) .. + 3 ------
+        const int64_t mb = cur.m0 + wm * TM, nb = cur.n0 + wn * TN;
+        const int ln = lane_again(lane), lrow = ln & 31, lhalf = ln >> 5;
+        float sx[IA];
+        f32x4 sw[NJ][4], bias[NJ][4];
+#pragma unroll
+        for (int ia = 0; ia < IA; ++ia) sx[ia] = *reinterpret_cast<const float*>(lds + own + (ia * 32 + lrow) * 4);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int n = j * 32 + g * 8 + lhalf * 4;
+                sw[j][g] = *reinterpret_cast<const f32x4*>(lds + own + 512 + n * 4);
+                bias[j][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (p.bias) {
+                    float b[4];
+                    load4(static_cast<const T*>(p.bias) + min(nb + n, p.n), static_cast<int>(max<int64_t>(min<int64_t>(p.n - nb - n, 4), 0)), b);
+                    bias[j][g] = f32x4{b[0], b[1], b[2], b[3]};
+                }
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        // results turn in the wave's space, 32 rows at a time: CPR 16-byte chunks a row, chunk c of row r at place c ^ (r % CPR)
+        constexpr int CPR = sizeof(T) == 4 ? 8 : TN * 2 / 16, ROWS = 64 / CPR, PASSES = sizeof(T) == 4 ? NJ : 1;
+        constexpr int CC = 16 / sizeof(T);               // columns of a chunk
+        const int sc = ln & (CPR - 1), sr = ln / CPR;
+        const int64_t left_m = p.m - mb;
+        const auto rs = __builtin_amdgcn_make_buffer_rsrc(static_cast<T*>(p.out) + mb * p.os + nb, static_cast<short>(0), 0x7fffffff, kRsrcWord3);
+        static_for<IA>([&](auto ia) __attribute__((always_inline)) {
+            static_for<PASSES>([&](auto pass) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = sizeof(T) == 4 ? pass : 0; j < (sizeof(T) == 4 ? pass + 1 : NJ); ++j)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        f32x4 v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            v[e] = static_cast<float>(acc[ia / 2][ia % 2][j][4 * g + e]) * sx[ia] * sw[j][g][e] + bias[j][g][e];
+                        if constexpr (sizeof(T) == 4) {
+                            const int c = 2 * g + lhalf;
+                            *reinterpret_cast<f32x4*>(lds + own + (lrow * CPR + (c ^ (lrow & (CPR - 1)))) * 16) = v;
+                        } else {
+                            const bf16x4 o = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+                            const int c = 4 * j + g;
+                            *reinterpret_cast<bf16x4*>(lds + own + (lrow * CPR + (c ^ (lrow & (CPR - 1)))) * 16 + lhalf * 8) = o;
+                        }
+                    }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                const int col = pass * 32 + sc * CC;
+                const int some = static_cast<int>(max<int64_t>(min<int64_t>(p.n - nb - col, CC), 0));
+#pragma unroll
+                for (int i = 0; i < 32 / ROWS; ++i) {
+                    const int r = sr + i * ROWS, row = ia * 32 + r;
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(lds + own + (r * CPR + (sc ^ (r & (CPR - 1)))) * 16);
+                    if constexpr (WHOLE) {               // what is not stored gets an offset past the results: every lane issues the same stores
+                        const unsigned off = row < left_m && some == CC ? static_cast<unsigned>(row) * static_cast<unsigned>(p.os * sizeof(T)) + col * sizeof(T) : kOOB;
+                        __builtin_amdgcn_raw_buffer_store_b128(w, rs, static_cast<int>(off), 0, 0);
+                    } else if (row < left_m) {
+                        T* const q = static_cast<T*>(p.out) + (mb + row) * p.os + nb + col;
+                        if (some == CC) {
+                            __builtin_memcpy(__builtin_assume_aligned(q, sizeof(T)), &w, 16);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < CC; ++e)
+                                if (e < some) {
+                                    if constexpr (sizeof(T) == 4)
+                                        reinterpret_cast<unsigned*>(q)[e] = w[e];
+                                    else
+                                        reinterpret_cast<unsigned short*>(q)[e] = static_cast<unsigned short>(w[e / 2] >> (16 * (e & 1)));
+                                }
+                        }
+                    }
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            });
+        });
+        stored = WHOLE;
+        if (!live) break;                                // (the loads have at least begun the next tile)
+        cur = ahead;
+    }
+    if (wave < 4) __builtin_amdgcn_s_barrier();          // the second group's last step
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // no load into LDS outlives the block
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: a block of W waves takes 16 FM rows by 16 columns, and its waves share out the sum; what counts is that each
+// weight is asked for early.  Operands go straight to registers in the layout of v_mfma_i32_16x16x64_i8 (16 rows, 64 bytes of
+// k), four or eight steps in flight; the waves' sums meet in LDS.
+// ---------------------------------------------------------------------------
+template <typename T, int FM, int W>
+__global__ __launch_bounds__(W * 64) void linear8_few_kernel(const Linear8Params p) {
+    constexpr int AHEAD = FM * W >= 64 ? 4 : 8;          // steps of 64 bytes of k whose loads are sent together
+    __shared__ i32x4 sums[W][FM][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = static_cast<int>(blockIdx.x) * 16;
+    const int m = static_cast<int>(p.m);
+    const int lo = wave * p.nk * 64, hi = min(p.k, lo + p.nk * 64);       // the wave's part of the sum
+    const auto rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.x), static_cast<short>(0), 0x7fffffff, kRsrcWord3);
+    const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.w) + n0 * p.ws, static_cast<short>(0), 0x7fffffff, kRsrcWord3);
+    const int row = lane & 15, kl = (lane >> 4) * 16;
+    const unsigned ow = static_cast<unsigned>(min<int64_t>(row, p.n - 1 - n0)) * static_cast<unsigned>(p.ws) + kl;
+    unsigned ox[FM];
+#pragma unroll
+    for (int a = 0; a < FM; ++a) ox[a] = static_cast<unsigned>(min(a * 16 + row, m - 1)) * static_cast<unsigned>(p.xs) + kl;
+    i32x4 acc[FM];
+#pragma unroll
+    for (int a = 0; a < FM; ++a) acc[a] = i32x4{0, 0, 0, 0};
+    for (int k0 = lo; k0 < hi; k0 += 64 * AHEAD) {
+        u32x4 xf[AHEAD][FM], wf[AHEAD];
+        const bool last = k0 + 64 * AHEAD > hi;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const unsigned past = last && k0 + i * 64 + kl >= hi ? kOOB : 0u;       // chunks past the sum read zeros
+            wf[i] = __builtin_amdgcn_raw_buffer_load_b128(rw, ow | past, k0 + i * 64, 0);
+#pragma unroll
+            for (int a = 0; a < FM; ++a) xf[i][a] = __builtin_amdgcn_raw_buffer_load_b128(rx, ox[a] | past, k0 + i * 64, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (last && (p.k & 15)) {
+#pragma unroll
+                for (int a = 0; a < FM; ++a) xf[i][a] = first_bytes(xf[i][a], hi - k0 - i * 64 - kl);
+            }
+#pragma unroll
+            for (int a = 0; a < FM; ++a)
+                acc[a] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, wf[i]), __builtin_bit_cast(i32x4, xf[i][a]), acc[a], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int a = 0; a < FM; ++a) sums[wave][a][lane] = acc[a];
+    __syncthreads();
+    for (int t = threadIdx.x; t < FM * 64; t += W * 64) {
+        const int a = t >> 6, l = t & 63, mr = a * 16 + (l & 15), n = n0 + (l >> 4) * 4;
+        const int some = static_cast<int>(min<int64_t>(p.n - n, 4));
+        if (mr >= m || some <= 0) continue;
+        i32x4 s = sums[0][a][l];
+#pragma unroll
+        for (int w = 1; w < W; ++w) s += sums[w][a][l];
+        float sw[4], bias[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4];
+        load4(p.sw + n, some, sw);
+        if (p.bias) load4(static_cast<const T*>(p.bias) + n, some, bias);
+        const float sx = p.sx[mr];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = static_cast<float>(s[i]) * sx * sw[i] + bias[i];
+        store4(static_cast<T*>(p.out) + mr * p.os + n, some, v);
+    }
+}
+
 // The shares of a sum added up: a thread takes four columns of a row.
 template <typename T>
 __global__ __launch_bounds__(256) void linear8_join_kernel(const Linear8Params p) {
@@ -228,6 +664,16 @@ __global__ __launch_bounds__(256) void linear8_join_kernel(const Linear8Params p
 
 }  // namespace
 
+// Tile edge of linear8_pair_kernel for a product, 0 where the others run it.
+static int pair_tile(int64_t m, int64_t n, int k) {
+    if (k <= 256) return 0;
+    const int64_t tiles = (m + 255) / 256 * ((n + 255) / 256), rounds = (tiles + kCUs - 1) / kCUs;
+    const int64_t small = (m + 127) / 128 * ((n + 127) / 128), srounds = (small + kCUs - 1) / kCUs;
+    if (rounds == 1 ? tiles >= 140 : tiles * 10 >= rounds * kCUs * 6) return 256;
+    if (k > 256 && small >= 140 && small * 10 >= srounds * kCUs * 6) return 128;
+    return 0;
+}
+
 // The most that shares of any smaller product may take, too.
 size_t linear8_ws_bytes(int64_t m, int64_t n, int k) {
     const size_t splits = static_cast<size_t>(std::min((k + 127) / 128, kMostSplits));
@@ -237,6 +683,9 @@ size_t linear8_ws_bytes(int64_t m, int64_t n, int k) {
 }
 
 Linear8Plan linear8_plan(int64_t m, int64_t n, int k, size_t ws_bytes) {
+    if (m <= 16) return Linear8Plan{16, 16, 8};
+    const int pair = pair_tile(m, n, k);
+    if (pair) return Linear8Plan{pair, pair, 1};
     Linear8Plan plan{64, 64, 1};
     const int64_t tiles = (m + plan.bm - 1) / plan.bm * ((n + plan.bn - 1) / plan.bn), steps = (k + 127) / 128;
     const size_t all = static_cast<size_t>(m) * static_cast<size_t>(n) * 4;
@@ -263,8 +712,40 @@ hipError_t launch_linear8(int dtype, int64_t m, int64_t n, int k, const mopar_ro
     p.per_xcd = (p.total + 7) / 8;
     p.nk = ((k + 127) / 128 + p.splits - 1) / p.splits;
     const dim3 grid(static_cast<unsigned>(p.per_xcd) * 8);
+    const int64_t es = dtype == MOPAR_BF16 ? 2 : 4;
+    // (the pair kernel addresses the results of a tile with 32 bits)
+    const bool pair = plan.bm >= 128, whole = n * es % 16 == 0 && p.os * es % 16 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && p.os * es < (int64_t(1) << 23);
+    auto go_pair = [&](auto t, auto tile) {
+        using T = decltype(t);
+        constexpr int TILE = decltype(tile)::value;
+        p.div_group = FastDiv(static_cast<unsigned>(8 * p.nt));
+        p.div_last = FastDiv(static_cast<unsigned>(p.mt - (p.mt - 1) / 8 * 8));
+        p.chunk = std::min((p.per_xcd + 31) / 32, kPairTiles);
+        const int per = 32 * p.chunk;
+        const dim3 blocks(static_cast<unsigned>((p.per_xcd + per - 1) / per * 32 * 8));
+        if (whole)
+            launch_kernel((linear8_pair_kernel<T, TILE, true>), blocks, dim3(512), 0, s, p);
+        else
+            launch_kernel((linear8_pair_kernel<T, TILE, false>), blocks, dim3(512), 0, s, p);
+        return hipGetLastError();
+    };
+    auto go_few = [&](auto t, auto fm, auto w) {
+        using T = decltype(t);
+        constexpr int FM = decltype(fm)::value, W = decltype(w)::value;
+        p.nk = (((k + 63) / 64 + W - 1) / W + 1) / 2 * 2;       // 64-byte steps of a wave, whole lines
+        launch_kernel((linear8_few_kernel<T, FM, W>), dim3(static_cast<unsigned>((n + 15) / 16)), dim3(W * 64), 0, s, p);
+        return hipGetLastError();
+    };
     auto go = [&](auto t) {
         using T = decltype(t);
+        using std::integral_constant;
+        if (plan.bn == 16) {
+            auto waves = [&](auto fm) {
+                return plan.splits >= 16 ? go_few(t, fm, integral_constant<int, 16>{}) : plan.splits >= 8 ? go_few(t, fm, integral_constant<int, 8>{}) : go_few(t, fm, integral_constant<int, 4>{});
+            };
+            return plan.bm == 16 ? waves(integral_constant<int, 1>{}) : plan.bm == 32 ? waves(integral_constant<int, 2>{}) : waves(integral_constant<int, 4>{});
+        }
+        if (pair) return plan.bm == 256 ? go_pair(t, std::integral_constant<int, 256>{}) : go_pair(t, std::integral_constant<int, 128>{});
         launch_kernel((linear8_kernel<T, 64, 64, 2, 2, 3>), grid, dim3(256), 0, s, p);
         if (p.splits > 1) {
             const int64_t threads = m * ((n + 3) / 4);

@@ -215,6 +215,37 @@ def test_linear(dt, m, n, k):
     assert torch.equal(out, shared)
 
 
+def linear_on_gpu(x, w, bias, dt):
+    """The reference of large products (float64 on the GPU)."""
+    y = x.values.double() @ w.values.double().t().contiguous() * x.scales.double()[:, None] * w.scales.double()[None]
+    tol = y.abs() * 4 * U
+    if bias is not None:
+        y = y + bias.double()
+        tol += y.abs() * U
+    return y, tol * 1.01 + y.abs() * R.HALF_STEP[DT[dt]] * 1.01
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(3100, 3504, 272), (3101, 3503, 513), (4096, 2304, 1031), (8000, 9000, 384), (300, 40001, 520), (1500, 1600, 700), (1537, 1603, 257),
+                                   (2100, 2200, 400), (128, 24000, 1008), (70, 30011, 330), (5000, 5000, 301)])
+def test_linear_large(dt, m, n, k):
+    """Tiles of 256 and 128, several a block; sums that end inside a step and inside a chunk; edges of tiles in both directions."""
+    g = gen(m + n + k)
+    x, w = rows8(g, m, k, extra=16), rows8(g, n, k)
+    bias = randn(g, n, dt=dt) if k % 2 else None
+    out = torch.full((m, n), 7.0, device="cuda", dtype=DT[dt])
+    P.mopar_linear8(x, w, out, bias=bias)
+    want, tol = linear_on_gpu(x, w, bias, dt)
+    assert bool(((out.double() - want).abs() <= tol).all())
+    again = torch.full((m + 2, n + 24), 7.0, device="cuda", dtype=DT[dt])          # inside wider rows, on and off 16 bytes
+    for at in (8, 3):
+        again.fill_(7.0)
+        P.mopar_linear8(x, w, again[1:m + 1, at:at + n], bias=bias)
+        assert torch.equal(again[1:m + 1, at:at + n], out)
+        again[1:m + 1, at:at + n] = 7.0
+        assert bool((again == 7).all())
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("m,n,k", [(3, 37, 100), (70, 135, 272), (300, 517, 1040), (1030, 1043, 2064)])
 def test_linear_strides_and_alignment(dt, m, n, k):
