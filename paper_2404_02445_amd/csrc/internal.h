@@ -272,9 +272,10 @@ struct RowsJob {
 };
 hipError_t launch_rows8(const RowsJob& j, hipStream_t s);
 
-// How a product of 8-bit rows is cut: tile sizes and shares of its sum.  A function of the sizes alone.
+// How a product of 8-bit rows is cut: a block's tile (rows 8: of 16, of which eight are read), its waves (0: the pair
+// kernel) and their stages, and the blocks that share a sum.  A function of the sizes and of the workspace's.
 struct Linear8Plan {
-    int bm, bn, splits;
+    int bm, bn, waves, stages, splits;
 };
 Linear8Plan linear8_plan(int64_t m, int64_t n, int k, size_t ws_bytes);
 size_t linear8_ws_bytes(int64_t m, int64_t n, int k);

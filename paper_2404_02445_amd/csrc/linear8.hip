@@ -3,11 +3,9 @@
 // Sums are int32 and exact, so the order and the cut of a sum are free: tiles, the waves' share of a stage and the
 // blocks' share of a sum change no bit of a result.
 //
-// linear8_kernel: a BM x BN tile of results by WM x WN waves on v_mfma_i32_16x16x64_i8, the weight fragment first: a lane ends
-// up with four neighbouring columns of one row.  Operands come straight to LDS, 128 bytes of k a row and stage, eight
-// rows (1 KB) a load instruction; chunk c of row r sits at place c ^ (r % 8), which keeps the fragment reads (16 rows, one
-// chunk each) off each other's banks.  Chunks past the sum read zeros; a chunk that the sum ends in is cut in
-// the fragments of x.
+// Operands come straight to LDS, 128 bytes of k a row and stage, eight rows (1 KB) a load instruction, whole lines where rows
+// start at multiples of 128 bytes.  The weight fragment is the MFMA's first operand: a lane ends up with four neighbouring columns of
+// one row.  Chunks past the sum read zeros; a chunk that the sum ends in is cut in the fragments of x.
 #pragma clang diagnostic ignored "-Winline-asm"      // (m0, which the loads into LDS take, is in no other use)
 #include <algorithm>
 #include <type_traits>
@@ -27,8 +25,6 @@ typedef __attribute__((address_space(3))) void* lds_ptr_t;
 constexpr int kRsrcWord3 = 0x00020000;       // raw buffer, 32-bit data format
 constexpr unsigned kOOB = 0x80000000u;       // a lane offset past every resource: reads zeros
 constexpr int kCUs = 256;
-constexpr size_t kMostPartial = size_t(64) << 20;
-constexpr int kMostSplits = 16;
 
 struct Linear8Params {
     const int8_t *x, *w;
@@ -39,7 +35,7 @@ struct Linear8Params {
     int64_t m, n, xs, ws, os;
     int k, splits;
     int mt, nt, total, per_xcd;  // tiles, those of all shares, and an XCD's
-    int nk;                      // 128-byte steps of a share
+    int nk;                      // 128-byte steps of a wave's share, or of the sum
     // linear8_pair_kernel: tiles a block, and the divisors of the tiles' order
     int chunk;
     FastDiv div_group, div_last;
@@ -102,6 +98,16 @@ template <typename T> __device__ __forceinline__ void store4(T* p, int n, const 
         if (i < n) p[i] = static_cast<T>(v[i]);
 }
 
+__device__ __forceinline__ void store4(int* p, int n, const i32x4& v) {
+    if (n >= 4) {
+        __builtin_memcpy(__builtin_assume_aligned(p, 4), &v, 16);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < n) p[i] = v[i];
+}
+
 // Tile t of all: its share of the sum, and its place.  The eight XCDs take blocks round-robin: each gets a run of
 // tiles, eight m tiles of one n tile after the other, so that the blocks it runs together share rows in its L2.
 struct Place { int m0, n0, split; };
@@ -115,102 +121,6 @@ __device__ __forceinline__ bool place_of(const Linear8Params& p, int bm, int bn,
     at.n0 = n * bn;
     at.m0 = (group * 8 + (within - n * gm)) * bm;
     return true;
-}
-
-template <typename T, int BM, int BN, int WM, int WN, int NS>
-__global__ __launch_bounds__(WM * WN * 64) void linear8_kernel(const Linear8Params p) {
-    constexpr int W = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
-    constexpr int STAGE = (BM + BN) * 128, L = (BM + BN) / 8 / W;          // bytes; loads a wave and stage
-    static_assert((BM + BN) / 8 % W == 0 && BM / 8 % W == 0, "a wave's loads are all of x or all of w");
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[NS * STAGE];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / WN, wn = wave % WN;
-    Place at;
-    if (!place_of(p, BM, BN, at)) return;                                 // (the whole block)
-    const int k_lo = at.split * p.nk * 128, nk = min(p.nk, (p.k - k_lo + 127) / 128);   // (at least 1: see the launcher)
-
-    // this wave's loads: 1 KB blocks wave, wave + W, ... of the stage's rows, x before w; lane l chunk (l % 8) ^ row
-    const u32x4 rx = resource(p.x + at.m0 * p.xs + k_lo), rw = resource(p.w + at.n0 * p.ws + k_lo);
-    const int cl = (lane & 7) ^ (lane >> 3);
-    unsigned off[L];
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-        const int r = (wave + W * i) * 8 + (lane >> 3);
-        const bool of_x = i < BM / 8 / W;
-        const int row = of_x ? static_cast<int>(min<int64_t>(r, p.m - 1 - at.m0)) : static_cast<int>(min<int64_t>(r - BM, p.n - 1 - at.n0));
-        off[i] = static_cast<unsigned>(row) * static_cast<unsigned>(of_x ? p.xs : p.ws) + static_cast<unsigned>(cl * 16);
-    }
-    const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<size_t>((lds_ptr_t)(&lds[0])));
-    unsigned slot = 0;
-    auto load_stage = [&](int kt) __attribute__((always_inline)) {
-        const bool past = kt >= nk || k_lo + kt * 128 + cl * 16 >= p.k;
-#pragma unroll
-        for (int i = 0; i < L; ++i)
-            load_lds(i < BM / 8 / W ? rx : rw, lds0 + slot * STAGE + (wave + W * i) * 1024, past ? kOOB : off[i], kt * 128);
-        slot = slot + 1 == NS ? 0 : slot + 1;
-    };
-    i32x4 acc[FM][FN];
-#pragma unroll
-    for (int a = 0; a < FM; ++a)
-#pragma unroll
-        for (int b = 0; b < FN; ++b) acc[a][b] = i32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < NS - 1; ++i) load_stage(i);
-    unsigned from = 0;
-    const int cut = p.k & 15 ? (p.k - k_lo) >> 7 : -1;                    // the step that a chunk is cut in
-    for (int kt = 0; kt < nk; ++kt) {
-        // this wave's loads of the stage are there, and its reads of the one before; then everyone's
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NS - 2) * L) : "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        load_stage(kt + NS - 1);
-        const unsigned char* const st = lds + from * STAGE;
-        from = from + 1 == NS ? 0 : from + 1;
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            const int c = 4 * kk + (lane >> 4), place = (c ^ (lane & 7)) * 16, r = lane & 15;
-            u32x4 xf[FM], wf[FN];
-#pragma unroll
-            for (int a = 0; a < FM; ++a) xf[a] = *reinterpret_cast<const u32x4*>(st + (wm * TM + a * 16 + r) * 128 + place);
-#pragma unroll
-            for (int b = 0; b < FN; ++b) wf[b] = *reinterpret_cast<const u32x4*>(st + (BM + wn * TN + b * 16 + r) * 128 + place);
-            if (kt == cut) {
-#pragma unroll
-                for (int a = 0; a < FM; ++a) xf[a] = first_bytes(xf[a], p.k - k_lo - kt * 128 - c * 16);
-            }
-#pragma unroll
-            for (int a = 0; a < FM; ++a)
-#pragma unroll
-                for (int b = 0; b < FN; ++b)
-                    acc[a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, wf[b]), __builtin_bit_cast(i32x4, xf[a]), acc[a][b], 0, 0, 0);
-        }
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                       // no load into LDS outlives the block
-#pragma unroll
-    for (int a = 0; a < FM; ++a) {
-        const int64_t m = at.m0 + wm * TM + a * 16 + (lane & 15);
-        if (m >= p.m) continue;
-        const float sx = p.sx[m];
-#pragma unroll
-        for (int b = 0; b < FN; ++b) {
-            const int64_t n = at.n0 + wn * TN + b * 16 + (lane >> 4) * 4;
-            const int some = static_cast<int>(min<int64_t>(p.n - n, 4));
-            if (some <= 0) continue;
-            if (p.splits > 1) {
-                int* const q = p.partial + (at.split * p.m + m) * p.n + n;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < some) q[i] = acc[a][b][i];
-                continue;
-            }
-            float sw[4], bias[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4];
-            load4(p.sw + n, some, sw);
-            if (p.bias) load4(static_cast<const T*>(p.bias) + n, some, bias);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = static_cast<float>(acc[a][b][i]) * sx * sw[i] + bias[i];
-            store4(static_cast<T*>(p.out) + m * p.os + n, some, v);
-        }
-    }
 }
 
 // ---------------------------------------------------------------------------
@@ -578,66 +488,103 @@ __global__ __launch_bounds__(512, 2) void linear8_pair_kernel(const Linear8Param
 }
 
 // ---------------------------------------------------------------------------
-// Few rows: a block of W waves takes 16 FM rows by 16 columns, and its waves share out the sum; what counts is that each
-// weight is asked for early.  Operands go straight to registers in the layout of v_mfma_i32_16x16x64_i8 (16 rows, 64 bytes of
-// k), four or eight steps in flight; the waves' sums meet in LDS.
+// Few tiles: a block of W waves takes 16 FM rows by 16 FN columns, and its waves share out the sum: what counts is that the
+// operands are asked for early and in whole lines, and that no wave waits for another.  Each wave has a ring of NS stages of its
+// own, 128 bytes of k of all the tile's rows and columns; the waves' sums meet in LDS at the end.  XL: 8-row loads of x a
+// stage (rows past them are never stored).
 // ---------------------------------------------------------------------------
-template <typename T, int FM, int W>
-__global__ __launch_bounds__(W * 64) void linear8_few_kernel(const Linear8Params p) {
-    constexpr int AHEAD = FM * W >= 64 ? 4 : 8;          // steps of 64 bytes of k whose loads are sent together
-    __shared__ i32x4 sums[W][FM][64];
+template <typename T, int FM, int XL, int FN, int W, int NS>
+__global__ __launch_bounds__(W * 64) void linear8_wave_kernel(const Linear8Params p) {
+    constexpr int STAGE = (FM + FN) * 2048, L = XL + 2 * FN, RING = NS * STAGE;
+    static_assert(FM * FN * 1024 <= RING && W * RING <= 163840, "the sums take the place of the rings");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[W * RING];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = static_cast<int>(blockIdx.x) * 16;
-    const int m = static_cast<int>(p.m);
-    const int lo = wave * p.nk * 64, hi = min(p.k, lo + p.nk * 64);       // the wave's part of the sum
-    const auto rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.x), static_cast<short>(0), 0x7fffffff, kRsrcWord3);
-    const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.w) + n0 * p.ws, static_cast<short>(0), 0x7fffffff, kRsrcWord3);
-    const int row = lane & 15, kl = (lane >> 4) * 16;
-    const unsigned ow = static_cast<unsigned>(min<int64_t>(row, p.n - 1 - n0)) * static_cast<unsigned>(p.ws) + kl;
-    unsigned ox[FM];
+    Place at;
+    if (!place_of(p, 16 * FM, 16 * FN, at)) return;                       // (the whole block)
+    const int lo = (at.split * W + wave) * p.nk * 128, hi = min(p.k, lo + p.nk * 128);   // the wave's part of the sum
+    const int nk = hi > lo ? (hi - lo + 127) >> 7 : 0;
+    // loads: row l / 8 of eight, chunk (l % 8) ^ row
+    const u32x4 rx = resource(p.x + at.m0 * p.xs + lo), rw = resource(p.w + at.n0 * p.ws + lo);
+    const int cl = (lane & 7) ^ (lane >> 3);
+    unsigned ox[XL], ow[2 * FN];
 #pragma unroll
-    for (int a = 0; a < FM; ++a) ox[a] = static_cast<unsigned>(min(a * 16 + row, m - 1)) * static_cast<unsigned>(p.xs) + kl;
-    i32x4 acc[FM];
+    for (int i = 0; i < XL; ++i) ox[i] = static_cast<unsigned>(min<int64_t>(i * 8 + (lane >> 3), p.m - 1 - at.m0)) * static_cast<unsigned>(p.xs) + cl * 16;
 #pragma unroll
-    for (int a = 0; a < FM; ++a) acc[a] = i32x4{0, 0, 0, 0};
-    for (int k0 = lo; k0 < hi; k0 += 64 * AHEAD) {
-        u32x4 xf[AHEAD][FM], wf[AHEAD];
-        const bool last = k0 + 64 * AHEAD > hi;
+    for (int i = 0; i < 2 * FN; ++i)
+        ow[i] = static_cast<unsigned>(min<int64_t>(i * 8 + (lane >> 3), p.n - 1 - at.n0)) * static_cast<unsigned>(p.ws) + cl * 16;
+    const unsigned mine = static_cast<unsigned>(reinterpret_cast<size_t>((lds_ptr_t)(&lds[0]))) + wave * RING;
+    unsigned slot = 0;
+    auto load_stage = [&](int kt) __attribute__((always_inline)) {
+        const unsigned past = kt >= nk || kt * 128 + cl * 16 >= hi - lo ? kOOB : 0u;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const unsigned past = last && k0 + i * 64 + kl >= hi ? kOOB : 0u;       // chunks past the sum read zeros
-            wf[i] = __builtin_amdgcn_raw_buffer_load_b128(rw, ow | past, k0 + i * 64, 0);
+        for (int i = 0; i < 2 * FN; ++i) load_lds(rw, mine + slot + (FM * 2 + i) * 1024, ow[i] | past, kt * 128);
 #pragma unroll
-            for (int a = 0; a < FM; ++a) xf[i][a] = __builtin_amdgcn_raw_buffer_load_b128(rx, ox[a] | past, k0 + i * 64, 0);
-        }
+        for (int i = 0; i < XL; ++i) load_lds(rx, mine + slot + i * 1024, ox[i] | past, kt * 128);
+        slot = slot + STAGE == RING ? 0 : slot + STAGE;
+    };
+    i32x4 acc[FM][FN];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            if (last && (p.k & 15)) {
+    for (int a = 0; a < FM; ++a)
 #pragma unroll
-                for (int a = 0; a < FM; ++a) xf[i][a] = first_bytes(xf[i][a], hi - k0 - i * 64 - kl);
+        for (int b = 0; b < FN; ++b) acc[a][b] = i32x4{0, 0, 0, 0};
+    if (nk > 0) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) load_stage(i);
+    }
+    const int cut = (hi - lo) & 15 ? (hi - lo) >> 7 : -1;                 // the step that a chunk is cut in
+    unsigned from = 0;
+    for (int kt = 0; kt < nk; ++kt) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 1) * L) : "memory");
+        const unsigned char* const st = lds + wave * RING + from;
+        from = from + STAGE == RING ? 0 : from + STAGE;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            const int c = 4 * kk + (lane >> 4), place = (c ^ (lane & 7)) * 16, r = (lane & 15) * 128;
+            u32x4 xf[FM], wf[FN];
+#pragma unroll
+            for (int b = 0; b < FN; ++b) wf[b] = *reinterpret_cast<const u32x4*>(st + (FM + b) * 2048 + r + place);
+#pragma unroll
+            for (int a = 0; a < FM; ++a) xf[a] = *reinterpret_cast<const u32x4*>(st + a * 2048 + r + place);
+            if (kt == cut) {
+#pragma unroll
+                for (int a = 0; a < FM; ++a) xf[a] = first_bytes(xf[a], hi - lo - kt * 128 - c * 16);
             }
 #pragma unroll
             for (int a = 0; a < FM; ++a)
-                acc[a] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, wf[i]), __builtin_bit_cast(i32x4, xf[i][a]), acc[a], 0, 0, 0);
+#pragma unroll
+                for (int b = 0; b < FN; ++b)
+                    acc[a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, wf[b]), __builtin_bit_cast(i32x4, xf[a]), acc[a][b], 0, 0, 0);
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                 // the stage is read: it can be loaded again
+        load_stage(kt + NS);
     }
-#pragma unroll
-    for (int a = 0; a < FM; ++a) sums[wave][a][lane] = acc[a];
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                       // no load into LDS outlives the loop
     __syncthreads();
-    for (int t = threadIdx.x; t < FM * 64; t += W * 64) {
-        const int a = t >> 6, l = t & 63, mr = a * 16 + (l & 15), n = n0 + (l >> 4) * 4;
-        const int some = static_cast<int>(min<int64_t>(p.n - n, 4));
-        if (mr >= m || some <= 0) continue;
-        i32x4 s = sums[0][a][l];
+    i32x4* const sums = reinterpret_cast<i32x4*>(lds);                     // [W][FM][FN][64]
 #pragma unroll
-        for (int w = 1; w < W; ++w) s += sums[w][a][l];
+    for (int a = 0; a < FM; ++a)
+#pragma unroll
+        for (int b = 0; b < FN; ++b) sums[((wave * FM + a) * FN + b) * 64 + lane] = acc[a][b];
+    __syncthreads();
+    for (int t = threadIdx.x; t < FM * FN * 64; t += W * 64) {
+        const int l = t & 63, b = (t >> 6) % FN, a = (t >> 6) / FN;
+        const int64_t m = at.m0 + a * 16 + (l & 15), n = at.n0 + b * 16 + (l >> 4) * 4;
+        const int some = static_cast<int>(min<int64_t>(p.n - n, 4));
+        if (m >= p.m || some <= 0) continue;
+        i32x4 s = sums[t];
+#pragma unroll
+        for (int w = 1; w < W; ++w) s += sums[w * FM * FN * 64 + t];
+        if (p.splits > 1) {
+            store4(p.partial + (at.split * p.m + m) * p.n + n, some, s);
+            continue;
+        }
         float sw[4], bias[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4];
         load4(p.sw + n, some, sw);
         if (p.bias) load4(static_cast<const T*>(p.bias) + n, some, bias);
-        const float sx = p.sx[mr];
+        const float sx = p.sx[m];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = static_cast<float>(s[i]) * sx * sw[i] + bias[i];
-        store4(static_cast<T*>(p.out) + mr * p.os + n, some, v);
+        store4(static_cast<T*>(p.out) + m * p.os + n, some, v);
     }
 }
 
@@ -648,11 +595,18 @@ __global__ __launch_bounds__(256) void linear8_join_kernel(const Linear8Params p
     const int64_t m = t / groups, n = (t - m * groups) * 4;
     if (m >= p.m) return;
     const int some = static_cast<int>(min<int64_t>(p.n - n, 4));
-    int sum[4] = {0, 0, 0, 0};
-    for (int s = 0; s < p.splits; ++s) {
-        const int* const q = p.partial + (s * p.m + m) * p.n + n;
+    i32x4 sum = {0, 0, 0, 0};
+    const int* q = p.partial + m * p.n + n;
+    if (some >= 4) {
+        for (int s = 0; s < p.splits; ++s, q += p.m * p.n) {
+            i32x4 part;
+            __builtin_memcpy(&part, __builtin_assume_aligned(q, 4), 16);
+            sum += part;
+        }
+    } else {
+        for (int s = 0; s < p.splits; ++s, q += p.m * p.n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] += i < some ? q[i] : 0;
+            for (int i = 0; i < 4; ++i) sum[i] += i < some ? q[i] : 0;
     }
     float sw[4], bias[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4];
     load4(p.sw + n, some, sw);
@@ -664,40 +618,52 @@ __global__ __launch_bounds__(256) void linear8_join_kernel(const Linear8Params p
 
 }  // namespace
 
-// Tile edge of linear8_pair_kernel for a product, 0 where the others run it.
+// Tile edge of linear8_pair_kernel for a product, 0 where linear8_wave_kernel runs it: its tiles have to fill the CUs.
 static int pair_tile(int64_t m, int64_t n, int k) {
-    if (k <= 256) return 0;
+    if (k <= 256 || m <= 64) return 0;
     const int64_t tiles = (m + 255) / 256 * ((n + 255) / 256), rounds = (tiles + kCUs - 1) / kCUs;
     const int64_t small = (m + 127) / 128 * ((n + 127) / 128), srounds = (small + kCUs - 1) / kCUs;
     if (rounds == 1 ? tiles >= 140 : tiles * 10 >= rounds * kCUs * 6) return 256;
-    if (k > 256 && small >= 140 && small * 10 >= srounds * kCUs * 6) return 128;
-    return 0;
+    return small >= 140 && small * 10 >= srounds * kCUs * 6 ? 128 : 0;
 }
 
-// The most that shares of any smaller product may take, too.
+constexpr int kLongShare = 512 << 10, kShortShare = 128 << 10;     // operand bytes of a tile: shared out from here, and down to here
+constexpr int kMostSplits = 8;
+
+// Partial sums of blocks that fill the CUs once; a size that does not fall as a product grows.
 size_t linear8_ws_bytes(int64_t m, int64_t n, int k) {
-    const size_t splits = static_cast<size_t>(std::min((k + 127) / 128, kMostSplits));
-    if (splits < 2 || m == 0 || n == 0) return 0;
-    const size_t all = static_cast<size_t>(m) * static_cast<size_t>(n);                     // (less than 2^36: see the entry points)
-    return std::min(kMostPartial, all * splits * 4);
+    if (k < kLongShare / 128 || m == 0 || n == 0) return 0;
+    constexpr int64_t most = int64_t(kCUs) * 64 * 64;               // results of all blocks
+    return static_cast<size_t>(m >= most / n ? most : std::min(most, m * n * kMostSplits)) * 4;
 }
 
 Linear8Plan linear8_plan(int64_t m, int64_t n, int k, size_t ws_bytes) {
-    if (m <= 16) return Linear8Plan{16, 16, 8};
-    const int pair = pair_tile(m, n, k);
-    if (pair) return Linear8Plan{pair, pair, 1};
-    Linear8Plan plan{64, 64, 1};
-    const int64_t tiles = (m + plan.bm - 1) / plan.bm * ((n + plan.bn - 1) / plan.bn), steps = (k + 127) / 128;
-    const size_t all = static_cast<size_t>(m) * static_cast<size_t>(n) * 4;
-    int64_t splits = std::min<int64_t>({2 * kCUs / tiles, steps / 4, kMostSplits, static_cast<int64_t>(std::min(ws_bytes, kMostPartial) / all)});
-    splits = std::max<int64_t>(splits, 1);
-    const int64_t nk = (steps + splits - 1) / splits;
-    plan.splits = static_cast<int>((steps + nk - 1) / nk);      // no share without a step
+    auto tiles = [&](int bm, int bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); };
+    Linear8Plan plan{64, 64, 4, 1, 1};
+    if (const int pair = pair_tile(m, n, k)) {
+        plan = {pair, pair, 0, 0, 1};
+    } else if (m <= 16 && n <= 1 << 25) {
+        plan = {m <= 8 ? 8 : 16, 16, 4, tiles(16, 16) <= kCUs ? 4 : 2, 1};
+    } else if (m <= 32 && n <= 1 << 25) {
+        plan = tiles(32, 16) <= kCUs ? Linear8Plan{32, 16, 4, 3, 1} : Linear8Plan{32, 32, 4, 2, 1};
+    } else if (tiles(32, 32) <= kCUs) {
+        plan = {32, 32, 8, 2, 1};
+    } else if (tiles(64, 32) <= kCUs) {
+        plan = {64, 32, 8, 1, 1};
+    } else if (tiles(64, 64) <= kCUs) {
+        plan = {64, 64, 8, 1, 1};
+    }
+    const int64_t blocks = tiles(plan.bm, plan.bn), bytes = int64_t(plan.bm + plan.bn) * k;
+    if (plan.waves && blocks <= kCUs / 2 && bytes >= kLongShare) {
+        const int64_t fit = static_cast<int64_t>(ws_bytes / 4) / (m * n);
+        plan.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kCUs / blocks, bytes / kShortShare, kMostSplits, fit})));
+    }
     return plan;
 }
 
 hipError_t launch_linear8(int dtype, int64_t m, int64_t n, int k, const mopar_rows8& x, const mopar_rows8& w, const void* bias,
                           const mopar_matrix& out, void* ws, const Linear8Plan& plan, hipStream_t s) {
+    const int tile_m = plan.bm == 8 ? 16 : plan.bm;
     Linear8Params p{};
     p.x = x.q, p.w = w.q, p.sx = x.scale, p.sw = w.scale;
     p.bias = bias;
@@ -706,16 +672,13 @@ hipError_t launch_linear8(int dtype, int64_t m, int64_t n, int k, const mopar_ro
     p.m = m, p.n = n, p.k = k;
     p.xs = x.stride, p.ws = w.stride, p.os = out.stride;
     p.splits = plan.splits;
-    p.mt = static_cast<int>((m + plan.bm - 1) / plan.bm);
+    p.mt = static_cast<int>((m + tile_m - 1) / tile_m);
     p.nt = static_cast<int>((n + plan.bn - 1) / plan.bn);
     p.total = p.mt * p.nt * p.splits;
     p.per_xcd = (p.total + 7) / 8;
-    p.nk = ((k + 127) / 128 + p.splits - 1) / p.splits;
-    const dim3 grid(static_cast<unsigned>(p.per_xcd) * 8);
-    const int64_t es = dtype == MOPAR_BF16 ? 2 : 4;
-    // (the pair kernel addresses the results of a tile with 32 bits)
-    const bool pair = plan.bm >= 128, whole = n * es % 16 == 0 && p.os * es % 16 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && p.os * es < (int64_t(1) << 23);
-    auto go_pair = [&](auto t, auto tile) {
+    const int steps = (k + 127) / 128, waves = std::max(plan.waves, 1) * plan.splits;
+    p.nk = (steps + waves - 1) / waves;
+    auto pair = [&](auto t, auto tile) {
         using T = decltype(t);
         constexpr int TILE = decltype(tile)::value;
         p.div_group = FastDiv(static_cast<unsigned>(8 * p.nt));
@@ -723,30 +686,37 @@ hipError_t launch_linear8(int dtype, int64_t m, int64_t n, int k, const mopar_ro
         p.chunk = std::min((p.per_xcd + 31) / 32, kPairTiles);
         const int per = 32 * p.chunk;
         const dim3 blocks(static_cast<unsigned>((p.per_xcd + per - 1) / per * 32 * 8));
-        if (whole)
+        // (the results of a tile are addressed with 32 bits there)
+        const int64_t es = sizeof(T);
+        if (n * es % 16 == 0 && p.os * es % 16 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && p.os * es < (int64_t(1) << 23))
             launch_kernel((linear8_pair_kernel<T, TILE, true>), blocks, dim3(512), 0, s, p);
         else
             launch_kernel((linear8_pair_kernel<T, TILE, false>), blocks, dim3(512), 0, s, p);
         return hipGetLastError();
     };
-    auto go_few = [&](auto t, auto fm, auto w) {
-        using T = decltype(t);
-        constexpr int FM = decltype(fm)::value, W = decltype(w)::value;
-        p.nk = (((k + 63) / 64 + W - 1) / W + 1) / 2 * 2;       // 64-byte steps of a wave, whole lines
-        launch_kernel((linear8_few_kernel<T, FM, W>), dim3(static_cast<unsigned>((n + 15) / 16)), dim3(W * 64), 0, s, p);
-        return hipGetLastError();
-    };
     auto go = [&](auto t) {
         using T = decltype(t);
         using std::integral_constant;
-        if (plan.bn == 16) {
-            auto waves = [&](auto fm) {
-                return plan.splits >= 16 ? go_few(t, fm, integral_constant<int, 16>{}) : plan.splits >= 8 ? go_few(t, fm, integral_constant<int, 8>{}) : go_few(t, fm, integral_constant<int, 4>{});
-            };
-            return plan.bm == 16 ? waves(integral_constant<int, 1>{}) : plan.bm == 32 ? waves(integral_constant<int, 2>{}) : waves(integral_constant<int, 4>{});
-        }
-        if (pair) return plan.bm == 256 ? go_pair(t, std::integral_constant<int, 256>{}) : go_pair(t, std::integral_constant<int, 128>{});
-        launch_kernel((linear8_kernel<T, 64, 64, 2, 2, 3>), grid, dim3(256), 0, s, p);
+        if (!plan.waves) return plan.bm == 256 ? pair(t, integral_constant<int, 256>{}) : pair(t, integral_constant<int, 128>{});
+        bool found = false;
+        auto form = [&](auto bm, auto bn, auto wv, auto st) {
+            constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value, W = decltype(wv)::value, NS = decltype(st)::value;
+            if (plan.bm != BM || plan.bn != BN || plan.waves != W || plan.stages != NS) return;
+            found = true;
+            launch_kernel((linear8_wave_kernel<T, (BM + 15) / 16, BM / 8, BN / 16, W, NS>), dim3(static_cast<unsigned>(p.per_xcd) * 8), dim3(W * 64), 0, s, p);
+        };
+        integral_constant<int, 1> one;
+        integral_constant<int, 2> two;
+        integral_constant<int, 3> three;
+        integral_constant<int, 4> four;
+        integral_constant<int, 8> eight;
+        integral_constant<int, 16> r16;
+        integral_constant<int, 32> r32;
+        integral_constant<int, 64> r64;
+        form(eight, r16, four, two), form(eight, r16, four, four), form(r16, r16, four, two), form(r16, r16, four, four);
+        form(r32, r16, four, three), form(r32, r32, four, two), form(r32, r32, eight, two);
+        form(r64, r32, eight, one), form(r64, r64, eight, one), form(r64, r64, four, one);
+        if (!found) return hipErrorInvalidValue;
         if (p.splits > 1) {
             const int64_t threads = m * ((n + 3) / 4);
             launch_kernel(linear8_join_kernel<T>, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, p);
