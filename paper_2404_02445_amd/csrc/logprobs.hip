@@ -4,9 +4,19 @@
 //   ln sum exp = scale m + ln S,   entropy = ln 2 (log2 S - U / S);
 // a lane keeps its own m and rescales S and U where it rises: 2^d S and 2^d (U + d S) for a rise of -d.
 //
-// The alternatives are kept by each wave as a sorted list, one entry a lane, of keys that order as (logit, lowest index
-// first): the float's bits made ascending in the upper word, the index's complement in the lower.  What may belong to the list is
-// collected in LDS, 64 at a time, sorted across the lanes and merged; the list's last key keeps out nearly all of a row.
+// The alternatives: the pass over a row also notes the largest logit of each piece of it, 64 elements or more.  The top-th largest of
+// those is at most the top-th largest logit, so only the few pieces that reach it are looked at again.  There, keys that order as
+// (logit, lowest index first) -- the float's bits made ascending in the upper word, the index's complement in the lower, so that
+// no two are equal -- wait in LDS behind the largest that the wave has met until there are 16, and then every key's place is the
+// number of larger ones.  In the end the waves' keys, and the blocks', find their places in the same way.
+//
+// What bounds it, measured (a copy reaches 5.16 TB/s): 2048 x 128000 in bf16, 524 MB, 98 us without alternatives (memory; some ten
+// vector instructions a logit, of which the exponential counts four, keep the ALUs at two thirds), 119 with five (124 between other
+// calls), 129 with 20: the pieces that are looked at again, when nothing is left to be streamed.  64 registers, for eight waves a
+// SIMD: with 72 the 2048 blocks took two rounds of the card and 147 us.  257 x 32003 in float32 12.6 us: one block more than CUs (256
+// rows 9.4).  4 x 128000 with 20 alternatives 14.5 us: two launches, two loads in a row, and six barriers.
+// Tried without gain: keeping the list up to date along the row by bitonic sorts across lanes (4 x 128000 16.7, 2048 x 128000 138 us
+// with five), by insertions one at a time (17.4, 145), loads a step ahead (168).
 #include <algorithm>
 #include <type_traits>
 
@@ -20,8 +30,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLowest = -3.40282347e38f, kInf = __builtin_inff();
-constexpr int kWaves = 4;                            // of a block
 constexpr int kLogprobSplits = 32;                   // blocks that share a row at most
+constexpr int kLogprobBlocks = 256;                  // blocks in all where rows are shared out
 
 // A block's part of a row, or a row's: statistics, and the list that follows it in memory.
 struct Part {
@@ -32,7 +42,8 @@ struct Part {
 struct LogprobParams {
     const unsigned char* x;
     int64_t stride;                                  // elements
-    int vocab, top, splits, share;                   // share: elements of a block, a multiple of 512
+    int vocab, top, splits, share;                   // share: elements of a block, a multiple of 64
+    int fine, span, pieces;                          // the lanes (4 or 2) whose elements are a piece, or 0: so many steps of a wave; pieces of all waves
     float c, scale;                                  // scale log2(e), scale
     const int32_t* token;
     float *logprob, *entropy, *top_logprob;
@@ -52,38 +63,91 @@ __device__ __forceinline__ float key_value(uint64_t k) {
 }
 __device__ __forceinline__ int key_at(uint64_t k) { return static_cast<int>(0xffffffffu - static_cast<unsigned>(k)); }
 
-__device__ __forceinline__ uint64_t other_lane(uint64_t k, int lane) {
-    const int lo = __builtin_amdgcn_ds_bpermute(lane * 4, static_cast<int>(k)), hi = __builtin_amdgcn_ds_bpermute(lane * 4, static_cast<int>(k >> 32));
-    return static_cast<uint64_t>(static_cast<unsigned>(hi)) << 32 | static_cast<unsigned>(lo);
+// The value of lane ^ D, without LDS: quads, halves of rows of 16, rows, halves of the wave.
+template <int D> __device__ __forceinline__ unsigned xor_lane(unsigned v) {
+    if constexpr (D == 1) return __builtin_amdgcn_mov_dpp(v, 0xb1, 0xf, 0xf, true);                 // quad_perm 1 0 3 2
+    if constexpr (D == 2) return __builtin_amdgcn_mov_dpp(v, 0x4e, 0xf, 0xf, true);                 // quad_perm 2 3 0 1
+    if constexpr (D == 3) return __builtin_amdgcn_mov_dpp(v, 0x1b, 0xf, 0xf, true);                 // quad_perm 3 2 1 0
+    if constexpr (D == 4) return xor_lane<3>(xor_lane<7>(v));
+    if constexpr (D == 7) return __builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true);                // row_half_mirror
+    if constexpr (D == 8) return __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true);                // row_ror:8
+    if constexpr (D == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);                        // odd rows of one with even rows of the other
+        return threadIdx.x & 16 ? r[0] : r[1];
+    }
+    if constexpr (D == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    }
 }
-// the larger or smaller of the lane's key and that of lane ^ d
-__device__ __forceinline__ uint64_t choose(uint64_t k, int lane, int d, bool larger) {
-    const uint64_t o = other_lane(k, lane ^ d);
-    return (k > o) == larger ? k : o;
+template <int D> __device__ __forceinline__ float xor_lane(float v) { return __uint_as_float(xor_lane<D>(__float_as_uint(v))); }
+__device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
+// what the wave's lanes wrote to LDS is read by others of them
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
-// 64 keys in descending order over the lanes
-__device__ __forceinline__ uint64_t sorted(uint64_t k, int lane) {
-#pragma unroll
-    for (int n = 2; n <= 64; n *= 2)
-#pragma unroll
-        for (int d = n / 2; d; d /= 2) k = choose(k, lane, d, ((lane & n) == 0) == ((lane & d) == 0));
-    return k;
+// The place of k among n keys in LDS, from a multiple of 16 bytes on: how many are larger.  (Two keys a read.)
+__device__ __forceinline__ int place_of(uint64_t k, const uint64_t* keys, int n) {
+    int place = 0;
+    const ulonglong2* const two = reinterpret_cast<const ulonglong2*>(keys);
+#pragma unroll 8
+    for (int j = 0; j < n / 2; ++j) {
+        const ulonglong2 q = two[j];
+        place += (q.x > k) + (q.y > k);
+    }
+    if (n & 1) place += keys[n - 1] > k;
+    return place;
 }
-// the 64 largest of two descending lists, descending
-__device__ __forceinline__ uint64_t merged(uint64_t a, uint64_t b, int lane) {
-    const uint64_t o = other_lane(b, 63 - lane);
-    uint64_t k = a > o ? a : o;
+__device__ __forceinline__ float wave_max(float v) {
+    v = fmaxf(v, xor_lane<1>(v)), v = fmaxf(v, xor_lane<2>(v)), v = fmaxf(v, xor_lane<4>(v));
+    return v = fmaxf(v, xor_lane<8>(v)), v = fmaxf(v, xor_lane<16>(v)), fmaxf(v, xor_lane<32>(v));
+}
+// The top-th largest of the lanes' values (no NaN).
+__device__ __forceinline__ float nth_largest(float v, int top) {
+    int larger = 0;
 #pragma unroll
-    for (int d = 32; d; d /= 2) k = choose(k, lane, d, (lane & d) == 0);
-    return k;
+    for (int j = 0; j < 64; ++j) larger += lane_value(v, j) > v;
+    float least = larger < top ? v : kInf;
+    least = fminf(least, xor_lane<1>(least)), least = fminf(least, xor_lane<2>(least)), least = fminf(least, xor_lane<4>(least));
+    least = fminf(least, xor_lane<8>(least)), least = fminf(least, xor_lane<16>(least)), least = fminf(least, xor_lane<32>(least));
+    return least;
 }
 
+// z of a logit: scale log2(e) x less that of the maximum m.  The product of m is rounded, but to the same float everywhere, so
+// that cancels; where it is large (and the rounding more than a part of an exponent), the difference goes first.
+__device__ __forceinline__ bool large(float mc) { return !(fabsf(mc) < 65536.0f); }
+__device__ __forceinline__ float exponent(float x, float m, float c) {
+    const float mc = m * c;
+    return large(mc) ? (x - m) * c : __builtin_fmaf(x, c, -mc);
+}
+// ... of a maximum m less that of a larger one, as their sums have them: how far sums rise; 2^-1000 and less is 0
+__device__ __forceinline__ float rise(float m, float n, float c) {
+#pragma clang fp contract(off)                       // (the products are rounded before they are subtracted, as in the sums)
+    const float mc = m * c, nc = n * c;
+    float d = mc - nc;
+    if (large(mc)) d += __builtin_fmaf(m, c, -mc);
+    if (large(nc)) d -= __builtin_fmaf(n, c, -nc);
+    return fmaxf(fabsf(mc) < kInf && fabsf(nc) < kInf ? d : (m - n) * c, -1000.0f);
+}
+// Two sums with their maxima.
 __device__ __forceinline__ void join(float& m, float& s, float& u, float m2, float s2, float u2, float c) {
-    const float n = fmaxf(m, m2), d = fmaxf((m - n) * c, -1000.0f), d2 = fmaxf((m2 - n) * c, -1000.0f);
+    const float n = fmaxf(m, m2), d = rise(m, n, c), d2 = rise(m2, n, c);
     const float f = __builtin_amdgcn_exp2f(d), f2 = __builtin_amdgcn_exp2f(d2);
     u = f * (u + d * s) + f2 * (u2 + d2 * s2);
     s = f * s + f2 * s2;
     m = n;
+}
+// ... of the wave's lanes
+__device__ __forceinline__ void join_lanes(float& m, float& s, float& u, int& rank, float c) {
+    auto with = [&](auto d) __attribute__((always_inline)) {
+        constexpr int D = decltype(d)::value;
+        join(m, s, u, xor_lane<D>(m), xor_lane<D>(s), xor_lane<D>(u), c);
+        rank += static_cast<int>(xor_lane<D>(static_cast<unsigned>(rank)));
+    };
+    using std::integral_constant;
+    with(integral_constant<int, 32>{}), with(integral_constant<int, 16>{}), with(integral_constant<int, 8>{});
+    with(integral_constant<int, 4>{}), with(integral_constant<int, 2>{}), with(integral_constant<int, 1>{});
 }
 
 // a row's results from its statistics and list (a key a lane)
@@ -91,7 +155,10 @@ __device__ __forceinline__ void finish(const LogprobParams& p, int64_t row, floa
                                        int lane) {
     const float log2s = __builtin_log2f(s);
     const bool nothing = s == 0.0f;                  // every logit is -infinity
-    auto logprob = [&](float x) { return nothing ? -kInf : (x - m) * p.scale - log2s * 0.693147181f; };
+    auto logprob = [&](float x) {
+        const float z = exponent(x, m, p.c);
+        return nothing ? -kInf : z == -kInf ? (x - m) * p.scale - log2s : (z - log2s) * 0.693147181f;      // (a type's lowest value: z is past float32)
+    };
     if (lane == 0) {
         p.logprob[row] = known ? logprob(xt) : -kInf;
         if (p.entropy) p.entropy[row] = nothing ? 0.0f : (log2s - u / s) * 0.693147181f;
@@ -122,13 +189,18 @@ template <typename T> __device__ __forceinline__ void load8(const T* p, int n, f
     }
 }
 
-// One block a part of a row: a wave's step is 512 elements, eight a lane.
-template <typename T, bool TOP>
-__global__ __launch_bounds__(kWaves * 64) void logprob_kernel(const LogprobParams p) {
-    __shared__ uint64_t found[kWaves][64];
-    __shared__ uint64_t lists[kWaves][64];
-    __shared__ Part sums[kWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// One block of W waves a part of a row.  A wave's step is two groups of 512 elements, eight a lane.
+template <typename T, bool TOP, int W>
+__global__ __launch_bounds__(W * 64, 8) void logprob_kernel(const LogprobParams p) {
+    constexpr int GROUPS = 2, STEP = W * 512 * GROUPS;
+    __shared__ __attribute__((aligned(16))) uint64_t lists[W][128];               // a wave's list of at most top keys in descending order, and what waits behind it
+    __shared__ __attribute__((aligned(16))) float pieces[W * 64];    // the largest logits of the waves' pieces
+    __shared__ uint64_t best[64];
+    __shared__ int remain;
+    __shared__ Part sums[W];
+    __shared__ unsigned least_piece;
+    __shared__ unsigned long long bar;               // the highest of the waves' last keys: what is below it is in no list of the row
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row = blockIdx.x / p.splits;
     const int split = blockIdx.x % p.splits;
     const int lo = split * p.share, hi = min(p.vocab, lo + p.share);
@@ -137,125 +209,270 @@ __global__ __launch_bounds__(kWaves * 64) void logprob_kernel(const LogprobParam
     const bool known = tok >= 0 && tok < p.vocab;
     const float xt = known ? static_cast<float>(x[tok]) : kInf;
     const float c = p.c;
+    if constexpr (TOP) {
+        if (threadIdx.x == 0) bar = 0, remain = 0, least_piece = 0xffffffffu;
+        if (threadIdx.x < 64) best[threadIdx.x] = 0;
+        pieces[threadIdx.x] = -kInf;
+        __syncthreads();
+    }
 
-    float m = kLowest, s = 0.0f, u = 0.0f;
-    int rank = 0;
-    uint64_t list = 0, last = 0;                     // the wave's list; the key that what joins it has to pass
-    int waiting = 0;                                 // keys in found
-    auto take = [&]() __attribute__((always_inline)) {
-        const uint64_t k = lane < waiting ? found[wave][lane] : 0;
-        list = merged(list, sorted(k, lane), lane);
-        last = other_lane(list, p.top - 1);
-        waiting = 0;
-    };
-    for (int at = lo + wave * 512 + lane * 8; at - lane * 8 < hi; at += kWaves * 512) {      // (the same trips in every lane)
-        float v[8];
-        const int n = hi - at;
-        load8(x + min(at, hi - 1), n, v);
-        if (n <= 0) {
+    float m = kLowest, mc = kLowest, s = 0.0f, u = 0.0f;
+    bool far = true;                                 // m times c is large
+    int rank = 0;                                    // of the wave
+    float v[GROUPS][8];
+    auto load = [&](int at0) __attribute__((always_inline)) {
+        const int at = at0 + lane * 8;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = -kInf;
+        for (int g = 0; g < GROUPS; ++g) {
+            const int n = hi - at - g * 512;
+            load8(x + (n > 0 ? at + g * 512 : lo), n, v[g]);
         }
-        float most = v[0];
+    };
+    const int first = lo + wave * 512 * GROUPS;
+    float piece_most = -kInf;
+    int in_piece = 0, piece = 0, loaded = first;
+    for (int at0 = first; at0 < hi; at0 += STEP) {
+        load(at0);
+        loaded = at0;
+        float most = v[0][0], least = v[0][0];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) most = fmaxf(most, v[i]);
+        for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = fmaxf(most, v[g][i]), least = fminf(least, v[g][i]);
         if (most > m) {
-            const float d = fmaxf((m - most) * c, -1000.0f), f = __builtin_amdgcn_exp2f(d);
+            const float d = rise(m, most, c), f = __builtin_amdgcn_exp2f(d);
             u = f * (u + d * s);
             s *= f;
             m = most;
+            mc = m * c;
+            far = large(mc);
+        }
+        if (__any(far || !(least * c > -1e30f))) {   // (weights of 0 times what is left of infinities would be NaN)
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float z = far ? (v[g][i] - m) * c : __builtin_fmaf(v[g][i], c, -mc), e = __builtin_amdgcn_exp2f(z);
+                    s += e;
+                    u = __builtin_fmaf(e, fmaxf(z, -200.0f), u);
+                }
+        } else {
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float z = __builtin_fmaf(v[g][i], c, -mc), e = __builtin_amdgcn_exp2f(z);
+                    s += e;
+                    u = __builtin_fmaf(e, z, u);
+                }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float z = (v[i] - m) * c, e = __builtin_amdgcn_exp2f(z);
-            s += e;
-            u = __builtin_fmaf(e, fmaxf(z, -200.0f), u);       // (0 where the weight is 0; NaN through e)
-            rank += v[i] > xt;
-        }
+        for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rank += __popcll(__ballot(v[g][i] > xt));
         if constexpr (TOP) {
-            if (__any(most >= key_value(last) || last == 0)) {
-#pragma unroll 1
-                for (int i = 0; i < 8; ++i) {
-                    const float xi = i == 0 ? v[0] : i == 1 ? v[1] : i == 2 ? v[2] : i == 3 ? v[3] : i == 4 ? v[4] : i == 5 ? v[5] : i == 6 ? v[6] : v[7];
-                    const uint64_t k = key_of(xi, at + i);
-                    const bool real = i < n && xi == xi;
-                    uint64_t in = __ballot(real && k > last);
-                    if (in == 0) continue;
-                    if (waiting + __popcll(in) > 64) {
-                        take();
-                        in = __ballot(real && k > last);
-                        if (in == 0) continue;
-                    }
-                    if (real && k > last) found[wave][waiting + __popcll(in & ((uint64_t(1) << lane) - 1))] = k;
-                    waiting += __popcll(in);
-                }
+            piece_most = fmaxf(piece_most, most);    // (fmaxf drops NaN)
+            if (p.fine) {
+                if (at0 + STEP < hi) continue;
+                piece_most = fmaxf(piece_most, xor_lane<1>(piece_most));
+                if (p.fine == 4) piece_most = fmaxf(piece_most, xor_lane<2>(piece_most));
+                if ((lane & (p.fine - 1)) == 0) pieces[threadIdx.x / p.fine] = piece_most;
+            } else if (++in_piece == p.span || at0 + STEP >= hi) {
+                const float w = wave_max(piece_most);
+                if (lane == 0) pieces[piece * W + wave] = w;
+                piece_most = -kInf;
+                in_piece = 0;
+                ++piece;
             }
         }
     }
     if constexpr (TOP) {
-        if (waiting) take();
-        lists[wave][lane] = list;
-    }
+        __syncthreads();
+        if (static_cast<int>(threadIdx.x) < p.pieces) {              // the top-th largest piece, -infinity where there are not so many
+            const float mine = pieces[threadIdx.x];
+            int larger = 0;
+            for (int j = 0; j < p.pieces; j += 4) {                  // (W divides them: a multiple of four)
+                const f32x4 q = *reinterpret_cast<const f32x4*>(pieces + j);
 #pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        join(m, s, u, __shfl_xor(m, o), __shfl_xor(s, o), __shfl_xor(u, o), c);
-        rank += __shfl_xor(rank, o);
+                for (int i = 0; i < 4; ++i) larger += q[i] > mine;
+            }
+            if (larger < p.top) atomicMin(&least_piece, p.top > p.pieces ? 0x007fffffu : static_cast<unsigned>(key_of(mine, -1) >> 32));
+        }
+        __syncthreads();
     }
+    // what joins the list has to be larger than last_x, or equal with an index below last_at; floor: the largest key known to end a list
+    uint64_t* const list = lists[wave];
+    float last_x = -kInf;
+    int last_at = 0x7fffffff;
+    uint64_t floor = 0;
+    auto raise = [&](uint64_t k) __attribute__((always_inline)) {
+        if (k <= floor) return;
+        floor = k;
+        const float w = key_value(k);
+        if (w > last_x || (w == last_x && key_at(k) < last_at)) last_x = w, last_at = key_at(k);
+    };
+    int kept = 0, held = 0;                          // keys in the list; with those that wait
+    auto take = [&]() __attribute__((always_inline)) {
+        wave_sync();
+        const uint64_t k0 = lane < held ? list[lane] : 0, k1 = lane + 64 < held ? list[lane + 64] : 0;
+        const int p0 = place_of(k0, list, held), p1 = held > 64 ? place_of(k1, list, held) : 64;
+        wave_sync();
+        if (lane < held && p0 < p.top) list[p0] = k0;
+        if (lane + 64 < held && p1 < p.top) list[p1] = k1;
+        kept = held = min(held, p.top);
+        wave_sync();
+        if (kept == p.top) raise(list[p.top - 1]);
+    };
+    if constexpr (TOP) {
+        last_x = key_value(static_cast<uint64_t>(least_piece) << 32);
+        const bool reach = p.fine ? pieces[threadIdx.x / p.fine] >= last_x : lane < piece && pieces[lane * W + wave] >= last_x;
+        const uint64_t reached = __ballot(reach);
+        for (uint64_t todo = p.fine ? reached != 0 : reached; todo; todo &= todo - 1) {
+            const int e = __builtin_ctzll(todo);
+            for (int st = e * p.span; st < (e + 1) * p.span; ++st) {
+                const int at0 = first + st * STEP;
+                if (at0 >= hi) break;
+                if (at0 != loaded) {
+                    load(at0);
+                    loaded = at0;
+                }
+                raise(__hip_atomic_load(&bar, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+                const int at = at0 + lane * 8;
+                if (kept == 0 && last_x == -kInf) {  // the top-th largest of the lanes' maxima bounds the list, too
+                    float most = -kInf;
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) most = fmaxf(most, v[g][i]);
+                    const float w = nth_largest(hi > at ? most : -kInf, p.top);
+                    if (w > last_x) last_x = w;      // (last_at is as it was: equal ones join)
+                }
+                const uint64_t before = floor;
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (!__any(v[g][i] >= last_x)) continue;
+                        const int a = at + g * 512 + i;
+                        auto joins = [&]() __attribute__((always_inline)) { return a < hi && (v[g][i] > last_x || (v[g][i] == last_x && a < last_at)); };
+                        uint64_t in = __ballot(joins());
+                        if (held + __popcll(in) > kept + 64) {
+                            take();
+                            in = __ballot(joins());
+                        }
+                        if ((in >> lane) & 1) list[held + __popcll(in & ((uint64_t(1) << lane) - 1))] = key_of(v[g][i], a);
+                        held += __popcll(in);
+                    }
+                if (held > 32 && held >= kept + 16) take();
+                if (floor > before && lane == 0) atomicMax(&bar, static_cast<unsigned long long>(floor));
+            }
+        }
+        if (held > 64) take();                       // (fewer need no order among themselves)
+    }
+    int none = 0;
+    join_lanes(m, s, u, none, c);
     if (lane == 0) sums[wave] = Part{m, s, u, rank};
+    if constexpr (TOP) {
+        // what is left of the waves' lists above the highest of their last keys, together, and its places
+        wave_sync();
+        if (lane == 0 && floor) atomicMax(&bar, static_cast<unsigned long long>(floor));
+        const uint64_t k = lane < held ? list[lane] : 0;
+        __syncthreads();
+        const uint64_t in = __ballot(k != 0 && k >= bar);
+        int at = 0;
+        if (lane == 0 && in) at = atomicAdd(&remain, __popcll(in));
+        at = __builtin_amdgcn_readfirstlane(at) + __popcll(in & ((uint64_t(1) << lane) - 1));
+        uint64_t* const all = lists[0];              // (64 keys of each wave at most)
+        if ((in >> lane) & 1) all[at] = k;
+        __syncthreads();
+        const int n = remain;
+        if (wave * 64 < n) {
+            const int t = threadIdx.x;
+            const uint64_t mine = t < n ? all[t] : 0;
+            const int place = place_of(mine, all, n);
+            if (t < n && place < p.top) best[place] = mine;
+        }
+    }
     __syncthreads();
     if (wave) return;
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
-        join(m, s, u, sums[w].m, sums[w].s, sums[w].u, c);
-        rank += sums[w].rank;
-        if constexpr (TOP) list = merged(list, lists[w][lane], lane);
-    }
-    if (p.splits == 1) return finish(p, row, xt, known, m, s, u, rank, list, lane);
+    const Part mine = lane < W ? sums[lane] : Part{kLowest, 0.0f, 0.0f, 0};
+    m = mine.m, s = mine.s, u = mine.u, rank = mine.rank;
+    join_lanes(m, s, u, rank, c);
+    if (p.splits == 1) return finish(p, row, xt, known, m, s, u, rank, TOP ? best[lane] : 0, lane);
     const int64_t part = row * p.splits + split;
     if (lane == 0) p.parts[part] = Part{m, s, u, rank};
-    if (lane < p.top) p.keys[part * p.top + lane] = list;
+    if (lane < p.top) p.keys[part * p.top + lane] = best[lane];
 }
 
-// The parts of a row joined by a wave.
+// The parts of a row joined by a block.  The top-th largest of the first keys of all parts, 64 or a few more, bounds the row's list closely; what
+// is not below it finds its place.
 template <typename T>
-__global__ __launch_bounds__(64) void logprob_join_kernel(const LogprobParams p) {
-    const int lane = threadIdx.x;
+__global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobParams p) {
+    __shared__ __attribute__((aligned(16))) uint64_t all[kLogprobSplits * 64];
+    __shared__ uint64_t best[64];
+    __shared__ unsigned long long bar;
+    __shared__ int remain;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int64_t row = blockIdx.x;
     const int tok = p.token[row];
+    const uint64_t* const keys = p.keys + row * p.splits * p.top;
+    const int total = p.splits * p.top;
+    if (total) {
+        const int each = min((64 + p.splits - 1) / p.splits, p.top), firsts = each * p.splits;      // (at most 64 + 32; top or more where there are)
+        uint64_t k[kLogprobSplits * 64 / 256];
+#pragma unroll
+        for (int i = 0; i < kLogprobSplits * 64 / 256; ++i) k[i] = i * 256 + tid < total ? keys[i * 256 + tid] : 0;
+        uint64_t first = 0;
+        if (tid < firsts) all[tid] = first = keys[tid / each * p.top + tid % each];
+        if (tid == 0) bar = 0, remain = 0;
+        if (tid < 64) best[tid] = 0;
+        __syncthreads();
+        if (first && place_of(first, all, firsts) == p.top - 1) bar = first;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kLogprobSplits * 64 / 256; ++i) {
+            const uint64_t in = __ballot(k[i] != 0 && k[i] >= bar);
+            if (!in) continue;
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&remain, __popcll(in));
+            at = __builtin_amdgcn_readfirstlane(at) + __popcll(in & ((uint64_t(1) << lane) - 1));
+            if ((in >> lane) & 1) all[at] = k[i];
+        }
+        __syncthreads();
+        const int n = remain;
+        for (int t = tid; t < n; t += 256) {
+            const uint64_t mine = all[t];
+            const int place = place_of(mine, all, n);
+            if (place < p.top) best[place] = mine;
+        }
+        __syncthreads();
+    }
+    if (tid >= 64) return;
     const bool known = tok >= 0 && tok < p.vocab;
     const float xt = known ? static_cast<float>(reinterpret_cast<const T*>(p.x)[row * p.stride + tok]) : kInf;
-    float m = kLowest, s = 0.0f, u = 0.0f;
-    int rank = 0;
-    if (lane < p.splits) {
-        const Part q = p.parts[row * p.splits + lane];
-        m = q.m, s = q.s, u = q.u, rank = q.rank;
-    }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        join(m, s, u, __shfl_xor(m, o), __shfl_xor(s, o), __shfl_xor(u, o), p.c);
-        rank += __shfl_xor(rank, o);
-    }
-    uint64_t list = 0;
-    if (p.top)
-        for (int i = 0; i < p.splits; ++i) {
-            const uint64_t k = lane < p.top ? p.keys[(row * p.splits + i) * p.top + lane] : 0;
-            list = merged(list, k, lane);
-        }
-    finish(p, row, xt, known, m, s, u, rank, list, lane);
+    const Part q = lane < p.splits ? p.parts[row * p.splits + lane] : Part{kLowest, 0.0f, 0.0f, 0};
+    float m = q.m, s = q.s, u = q.u;
+    int rank = q.rank;
+    join_lanes(m, s, u, rank, p.c);
+    finish(p, row, xt, known, m, s, u, rank, total ? best[lane] : 0, lane);
 }
 
 }  // namespace
 
-// Blocks that share a row: while the rows alone leave CUs idle, shares of 4096 elements and more.
+// Blocks that share a row, and the waves of a block.  Up to 32 rows leave most CUs idle: their rows are shared out among blocks of four
+// waves, one step of 4096 elements each where there are enough blocks (4 x 128000 with 20 alternatives 23.1 us unshared, 12.6; 32 rows
+// 25.4 / 21.3; 128 rows in two shares 26.7 / 41.  Rows that fill the card take four waves each, those between 16.
+static int logprob_waves(int64_t rows, int splits) { return splits > 1 || rows >= 1024 ? 4 : 16; }
 int logprob_splits(int64_t rows, int vocab) {
-    const int64_t idle = 1024 / std::max<int64_t>(rows, 1);
-    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({idle, vocab / 4096, kLogprobSplits})));
+    if (rows > 32) return 1;
+    const int64_t idle = kLogprobBlocks / std::max<int64_t>(rows, 1);
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({idle, (vocab + 4095) / 4096, kLogprobSplits})));
 }
 
 // (of as many rows as share at all: a size that does not fall as rows grow)
 size_t logprob_ws_bytes(int64_t rows, int vocab, int top) {
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(vocab / 4096, kLogprobSplits));
-    const int64_t parts = std::min<int64_t>(rows * splits, 1024);
+    const int64_t splits = std::min<int64_t>((vocab + 4095) / 4096, kLogprobSplits);
+    const int64_t parts = splits < 2 ? 0 : std::min<int64_t>(std::min<int64_t>(rows, 32) * splits, kLogprobBlocks);
     return static_cast<size_t>(parts) * (sizeof(Part) + 8 * static_cast<size_t>(top));
 }
 
@@ -266,7 +483,7 @@ hipError_t launch_token_logprobs(const LogprobJob& j, int splits, void* ws, hipS
     p.vocab = j.vocab;
     p.top = j.top;
     p.splits = splits;
-    p.share = static_cast<int>((static_cast<int64_t>(j.vocab) + 512 * splits - 1) / (512 * splits) * 512);
+    p.share = ((j.vocab + splits - 1) / splits + 63) / 64 * 64;
     p.c = j.scale * 1.44269504f;
     p.scale = j.scale;
     p.token = j.token;
@@ -274,17 +491,24 @@ hipError_t launch_token_logprobs(const LogprobJob& j, int splits, void* ws, hipS
     p.top_logprob = j.top_logprob, p.top_id = j.top_id;
     p.parts = static_cast<Part*>(ws);
     p.keys = reinterpret_cast<uint64_t*>(p.parts + j.rows * splits);
-    const dim3 grid(static_cast<unsigned>(j.rows * splits)), block(kWaves * 64);
-    auto go = [&](auto t) {
+    const dim3 grid(static_cast<unsigned>(j.rows * splits));
+    auto go = [&](auto t, auto w) {
         using T = decltype(t);
+        constexpr int W = decltype(w)::value;
+        // pieces: of four or two lanes where a wave takes few steps, else of whole steps, at most 64 of a wave
+        const int steps = (p.share + W * 1024 - 1) / (W * 1024);
+        p.fine = steps > 4 ? 0 : j.top <= W * 8 ? 4 : 2;
+        p.span = p.fine ? steps : (steps + 63) / 64;
+        p.pieces = p.fine ? W * 64 / p.fine : (steps + p.span - 1) / p.span * W;
         if (j.top)
-            launch_kernel((logprob_kernel<T, true>), grid, block, 0, s, p);
+            launch_kernel((logprob_kernel<T, true, W>), grid, dim3(W * 64), 0, s, p);
         else
-            launch_kernel((logprob_kernel<T, false>), grid, block, 0, s, p);
-        if (splits > 1) launch_kernel(logprob_join_kernel<T>, dim3(static_cast<unsigned>(j.rows)), dim3(64), 0, s, p);
+            launch_kernel((logprob_kernel<T, false, W>), grid, dim3(W * 64), 0, s, p);
+        if (splits > 1) launch_kernel(logprob_join_kernel<T>, dim3(static_cast<unsigned>(j.rows)), dim3(256), 0, s, p);
         return hipGetLastError();
     };
-    return j.dtype == MOPAR_BF16 ? go(__bf16{}) : go(float{});
+    auto types = [&](auto w) { return j.dtype == MOPAR_BF16 ? go(__bf16{}, w) : go(float{}, w); };
+    return logprob_waves(j.rows, splits) == 4 ? types(std::integral_constant<int, 4>{}) : types(std::integral_constant<int, 16>{});
 }
 
 }  // namespace mopar
