@@ -5,10 +5,10 @@
 // maximum come from one pass, and a row is read once, kept in registers and written once; rows past 32768 elements are read
 // again for the second pass.
 //
-// The steps are those of 64-bit arithmetic.  In float32 127 p / a is off by a few 2^-24 of itself, which decides
-// nothing unless it lies within that of the middle between two steps: those values (one in ten thousand) are worked out
-// again in float64.  So that a is exact too, the values within float32's error of the largest are reduced a second
-// time in float64; bf16 norms need neither, their products of two 8-bit mantissas are exact in float32.
+// The steps are those of 64-bit arithmetic.  In float32 127 p / a is off by a part that is known (value()), which decides nothing
+// unless the value lies within it of the middle between two steps: those, one in some thousands, are worked out again in float64 (a row
+// that float32 knows too little of, as one of gates all far below zero, altogether).  So that a is exact too, the values within float32's
+// error of the largest are worked out in float64 first; bf16 norms and plain rows need neither, their p is exact in float32.
 #include <type_traits>
 
 #include "internal.h"
@@ -58,34 +58,48 @@ template <typename T> __device__ __forceinline__ void store8(T* p, int n, const 
     }
 }
 
-// e^v for v <= 88: v log2(e) as a rounded product and its remainder, 2^ of each; off by at most 2 half steps of float32.
+// e^v for v <= 88: v log2(e) as a rounded product and its remainder, 2^ of each; off by at most 4 half steps of float32.
 __device__ __forceinline__ float exp_(float v) {
     constexpr float kLog2e = 1.44269502f, kLog2eLow = 1.92596303e-8f;          // their sum: log2(e)
     const float hi = v * kLog2e, lo = __builtin_fmaf(v, kLog2e, -hi) + v * kLog2eLow;
     const float e = __builtin_amdgcn_exp2f(hi);
     return __builtin_fmaf(e, lo * 0.693147181f, e);
 }
-
-// activation(g) in float32
-template <int KIND> __device__ __forceinline__ float activation(float g) {
-    if constexpr (KIND == MOPAR_GATE_SILU) return g * __builtin_amdgcn_rcpf(1.0f + exp_(fminf(fmaxf(-g, -104.0f), 88.0f)));
-    return 0.5f * g * erfcf(g * -0.707106781f);
+// erf by formula 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical Functions, off by at most 1.5e-7, and by float32's roundings:
+// of t (2 half steps, where the polynomial in t changes by at most 1.1 of itself), its five steps, e^(-x^2) and their product, of at most 1
+__device__ __forceinline__ float erf_(float x) {
+    const float ax = __builtin_fabsf(x), t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * ax);
+    const float poly = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    return __builtin_copysignf(1.0f - poly * __builtin_amdgcn_exp2f(ax * ax * -1.44269504f), x);
 }
-// The bound of p's relative error in float32, in units of 2^-24.  A product of two elements: 1.  SiLU: the exponential 4, the
-// sum 1, the reciprocal 2, products 2.  GELU: erfc itself 16, products 3, and the rounding of its argument z > 0, of which it
-// changes by 2 z^2 + 2 parts in one.
-template <int KIND> __device__ __forceinline__ float bound_of(float g) {
-    if constexpr (KIND == NORM) return 1.0f;
-    if constexpr (KIND == MOPAR_GATE_SILU) return 10.0f;
-    const float z = fminf(g, 0.0f);
-    return 24.0f + 3.0f * z * z;
+
+constexpr float kHalfStep = 6.0e-8f;                 // 2^-24, and the roundings of the bounds
+// p in float32, and how far it may be off.  A product of two elements: half a step.  SiLU: exponential 4 half steps, sum 1,
+// reciprocal 2, products 3.  GELU: erf 1.5e-7 + 20 half steps (1.35e-6 in all) and 12 more
+// of its argument, the sum and the products, all times |g x| / 2.
+template <int KIND> __device__ __forceinline__ float value(float v, float w, float& off) {
+    if constexpr (KIND == NORM) {
+        const float p = v * w;
+        off = fabsf(p) * kHalfStep;
+        return p;
+    } else if constexpr (KIND == MOPAR_GATE_SILU) {
+        const float p = w * __builtin_amdgcn_rcpf(1.0f + exp_(fminf(fmaxf(-w, -104.0f), 88.0f))) * v;
+        off = fabsf(p) * (10.0f * kHalfStep);
+        return p;
+    } else if constexpr (KIND == MOPAR_GATE_GELU) {
+        const float half = 0.5f * w * v, p = half * (1.0f + erf_(w * 0.707106781f));
+        off = fabsf(half) * (1.35e-6f + 12.0f * kHalfStep);          // (1 + erf is at most 2)
+        return p;
+    } else {
+        off = 0.0f;
+        return v;
+    }
 }
 template <int KIND> __device__ __forceinline__ double value64(double v, double w) {
     if constexpr (KIND == MOPAR_GATE_SILU) return w / (1.0 + exp(-w)) * v;
     if constexpr (KIND == MOPAR_GATE_GELU) return 0.5 * w * erfc(w * -0.70710678118654752) * v;
     return v * w;
 }
-constexpr float kHalfStep = 6.0e-8f;                 // 2^-24, and the roundings of the bounds
 
 struct RowsParams {
     const unsigned char *x, *residual, *gate, *weight;
@@ -97,56 +111,56 @@ struct RowsParams {
     float eps, inv_width;
 };
 
-template <int TPR> struct RowSum {              // TPR threads of a row: reductions over them
-    __device__ static float all(float v, bool sum, float* lds) {
-#pragma unroll
-        for (int o = 32; o; o >>= 1) {
-            const float w = __shfl_xor(v, o);
-            v = sum ? v + w : fmaxf(v, w);
-        }
-        if constexpr (TPR > 64) {
-            __syncthreads();
-            if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-            __syncthreads();
-            v = lds[0];
-#pragma unroll
-            for (int i = 1; i < TPR / 64; ++i) v = sum ? v + lds[i] : fmaxf(v, lds[i]);
-        }
-        return v;
+// The value of lane ^ D.
+template <int D> __device__ __forceinline__ unsigned xor_lane(unsigned v) {
+    if constexpr (D == 1) return __builtin_amdgcn_mov_dpp(v, 0xb1, 0xf, 0xf, true);                 // quad_perm 1 0 3 2
+    if constexpr (D == 2) return __builtin_amdgcn_mov_dpp(v, 0x4e, 0xf, 0xf, true);                 // quad_perm 2 3 0 1
+    if constexpr (D == 4) return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true), 0x1b, 0xf, 0xf, true);   // 7 - i, then 3 - i
+    if constexpr (D == 8) return __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true);                // row_ror:8
+    if constexpr (D == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);                        // odd rows of one with even rows of the other
+        return threadIdx.x & 16 ? r[0] : r[1];
     }
-    __device__ static double top(double v, double* lds) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+}
+template <int D> __device__ __forceinline__ float xor_lane(float v) { return __uint_as_float(xor_lane<D>(__float_as_uint(v))); }
+template <int D> __device__ __forceinline__ double xor_lane(double v) {
+    const uint64_t k = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, static_cast<uint64_t>(xor_lane<D>(static_cast<unsigned>(k >> 32))) << 32 | xor_lane<D>(static_cast<unsigned>(k)));
+}
+// v of all the TPR threads of a row, combined by f; each value of several threads' rows has its own lds[16]
+template <int TPR, typename V, typename F> __device__ __forceinline__ V over_row(V v, F f, V* lds) {
+    if constexpr (TPR > 32) v = f(v, xor_lane<32>(v));
+    v = f(v, xor_lane<16>(v)), v = f(v, xor_lane<8>(v)), v = f(v, xor_lane<4>(v)), v = f(v, xor_lane<2>(v)), v = f(v, xor_lane<1>(v));
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = lds[0];
 #pragma unroll
-        for (int o = 32; o; o >>= 1) v = fmax(v, __shfl_xor(v, o));
-        if constexpr (TPR > 64) {
-            __syncthreads();
-            if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-            __syncthreads();
-            v = lds[0];
-#pragma unroll
-            for (int i = 1; i < TPR / 64; ++i) v = fmax(v, lds[i]);
-        }
-        return v;
+        for (int i = 1; i < TPR / 64; ++i) v = f(v, lds[i]);
     }
-};
+    return v;
+}
 
 // TPR threads take a row, CH chunks each (0: any number, read twice); a block takes the rows of 256 threads, or one.
 template <typename T, int KIND, int TPR, int CH>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const RowsParams p) {
     constexpr int THREADS = TPR > 256 ? TPR : 256;
     constexpr bool EXACT = KIND == MOPAR_GATE_NONE || (KIND == NORM && sizeof(T) == 2);      // p is exact in float32
-    __shared__ double lds[16];
-    float* const ldsf = reinterpret_cast<float*>(lds);
+    __shared__ double lds64[16];
+    __shared__ float lds[3][16];
     const int64_t row = static_cast<int64_t>(blockIdx.x) * (THREADS / TPR) + threadIdx.x / TPR;
     const int me = threadIdx.x % TPR;
-    if (row >= p.tokens) return;                                   // (whole waves, and whole blocks where rows take several)
+    if (row >= p.tokens) return;                     // (lanes of one row stay together: none is missed by others, and no barrier by rows of several waves)
     const T* const x = reinterpret_cast<const T*>(p.x) + row * p.xs;
     const T* const res = p.residual ? reinterpret_cast<const T*>(p.residual) + row * p.rs : nullptr;
     const T* const other = KIND == NORM ? reinterpret_cast<const T*>(p.weight) : reinterpret_cast<const T*>(p.gate) + row * p.gs;
     T* const total = p.total ? reinterpret_cast<T*>(p.total) + row * p.ts : nullptr;
     T* const out = p.out ? reinterpret_cast<T*>(p.out) + row * p.os : nullptr;
 
-    float squares = 0.0f, top = 0.0f;       // top: what the row's largest |p| is at least
-    bool odd = false;                       // an infinity or NaN among the p
+    float squares = 0.0f, far = 0.0f;                // far: how far a p of the row may be off
+    unsigned top_bits = 0;                           // of the row's largest |p|; infinities and NaN are above all others
     // p of chunk c; the first time, total is stored and the row's sums go on
     auto read = [&](int c, float (&f)[8], bool first) __attribute__((always_inline)) {
         const int at = c * 8, n = p.width - at;
@@ -166,22 +180,19 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
         if constexpr (KIND != MOPAR_GATE_NONE) load8(other + at, n, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if constexpr (KIND == NORM) {
-                if (first) squares = __builtin_fmaf(f[i], f[i], squares);
-                f[i] *= w[i];
-            } else if constexpr (KIND != MOPAR_GATE_NONE) {
-                f[i] *= activation<KIND>(w[i]);
-            }
+            if (KIND == NORM && first) squares = __builtin_fmaf(f[i], f[i], squares);
+            float off;
+            f[i] = value<KIND>(f[i], w[i], off);
             if (first) {
-                const float a = fabsf(f[i]);
-                odd |= !(a < __builtin_inff());
-                top = fmaxf(top, EXACT ? a : a - a * (bound_of<KIND>(w[i]) * kHalfStep));
+                top_bits = max(top_bits, __float_as_uint(f[i]) & 0x7fffffffu);
+                if constexpr (KIND == MOPAR_GATE_GELU) far = fmaxf(far, off);
             }
         }
     };
     // p of element at in float64; read again, as few are
     auto exact = [&](int at) __attribute__((always_inline)) -> double {
         float h = static_cast<float>(total ? total[at] : x[at]);
+        if constexpr (KIND == MOPAR_GATE_NONE) return h;
         if (KIND == NORM && res && !total) h = static_cast<float>(static_cast<T>(h + static_cast<float>(res[at])));
         return value64<KIND>(h, static_cast<float>(other[at]));
     };
@@ -194,87 +205,119 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
     } else {
         for (int c = me; c < p.chunks; c += TPR) read(c, f[0], true);
     }
-    // the thread's chunks again
-    auto each = [&](auto&& g) __attribute__((always_inline)) {
-        if constexpr (CH > 0) {
-#pragma unroll
-            for (int k = 0; k < CH; ++k)
-                if (me + k * TPR < p.chunks) g(me + k * TPR, f[k]);
-        } else {
-            for (int c = me; c < p.chunks; c += TPR) {
-                read(c, f[0], false);
-                g(c, f[0]);
-            }
-        }
-    };
+    auto place = [&](int bit) { return (me + (bit >> 3) * TPR) * 8 + (bit & 7); };      // of element bit % 8 of the thread's chunk bit / 8
+    auto most = [](float a, float b) { return fmaxf(a, b); };
     float r = 1.0f;
-    if constexpr (KIND == NORM) r = 1.0f / __builtin_sqrtf(RowSum<TPR>::all(squares, true, ldsf) * p.inv_width + p.eps);
-    bool finite = false;
+    if constexpr (KIND == NORM) r = 1.0f / __builtin_sqrtf(over_row<TPR>(squares, [](float a, float b) { return a + b; }, lds[0]) * p.inv_width + p.eps);
+    float top = 0.0f;
     double top64 = 0.0;
+    bool finite = false;
     if (p.q) {
-        top = RowSum<TPR>::all(odd ? __builtin_inff() : top, false, ldsf);
+        const float mine = __uint_as_float(min(top_bits, 0x7f800000u));        // (NaN counts as infinity)
+        top = over_row<TPR>(mine, most, lds[1]);
         finite = top < __builtin_inff();
         top64 = top;
         if constexpr (!EXACT) {
-            double mine = 0.0;
-            if (finite && top > 0.0f)
-                each([&](int c, const float (&a)[8]) __attribute__((always_inline)) {
-                    float w[8];
-                    if constexpr (KIND == MOPAR_GATE_GELU) load8(other + c * 8, p.width - c * 8, w);
-                    unsigned near = 0;
+            if constexpr (KIND == MOPAR_GATE_GELU)
+                far = over_row<TPR>(far, most, lds[2]);
+            else
+                far = top * (KIND == NORM ? kHalfStep : 10.0f * kHalfStep);
+            // the row's largest in float64 is among those that float32 has within twice that of its largest
+            double best = 0.0;
+            if (finite && top + far > 0.0f && mine >= top - 2.0f * far) {
+                if constexpr (CH > 0) {
+                    uint64_t near = 0;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        near |= fabsf(a[i]) * (1.0f + bound_of<KIND>(w[i]) * kHalfStep) >= top ? 1u << i : 0u;
-                    for (; near; near &= near - 1) mine = fmax(mine, fabs(exact(c * 8 + __builtin_ctz(near))));
-                });
-            top64 = RowSum<TPR>::top(mine, lds);
+                    for (int k = 0; k < CH; ++k)
+                        if (me + k * TPR < p.chunks)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) near |= fabsf(f[k][i]) >= top - 2.0f * far ? uint64_t(1) << (8 * k + i) : 0u;
+                    for (; near; near &= near - 1) {
+                        const int at = place(__builtin_ctzll(near));
+                        if (at < p.width) best = fmax(best, fabs(exact(at)));
+                    }
+                } else {
+                    for (int c = me; c < p.chunks; c += TPR) {
+                        read(c, f[0], false);
+                        for (int i = 0; i < min(8, p.width - c * 8); ++i)
+                            if (fabsf(f[0][i]) >= top - 2.0f * far) best = fmax(best, fabs(exact(c * 8 + i)));
+                    }
+                }
+            }
+            top64 = over_row<TPR>(best, [](double a, double b) { return fmax(a, b); }, lds64);
         }
         if (me == 0) p.scale[row] = finite ? static_cast<float>(top64 * static_cast<double>(r) / 127.0) : __builtin_nanf("");
     }
-    const bool some = finite && top64 > 0.0, tiny = top64 < 1e-30;     // (127 / a within float32)
+    // (a row whose 127 / a is past float32, or that float32 knows too little of, has all of its steps worked out in float64)
+    const bool some = finite && top64 > 0.0, tiny = top64 < 1e-30;
     const float inv = some && !tiny ? static_cast<float>(127.0 / top64) : 0.0f;
+    const float middle = tiny ? -1.0f : 0.5f - (far * inv * 1.01f + 127.0f * 3.0f * kHalfStep);   // how far a sure step may be from its value
     int8_t* const q = p.q ? p.q + row * p.qs : nullptr;
-    each([&](int c, const float (&a)[8]) __attribute__((always_inline)) {
+    auto right = [&](int at) __attribute__((always_inline)) { return static_cast<int8_t>(rint(exact(at) * 127.0 / top64)); };
+    // the steps of chunk c to its place; those that are not sure are marked
+    auto store_steps = [&](int c, const float (&a)[8]) __attribute__((always_inline)) -> unsigned {
         const int at = c * 8, n = p.width - at;
         uint64_t steps = 0;
-        if (q && some) {
-            float w[8];
-            if constexpr (KIND == MOPAR_GATE_GELU) load8(other + at, n, w);
-            unsigned near = 0, s[2] = {0, 0};
+        unsigned near = 0;
+        if (some) {
+            // 1.5 * 2^23 added: rounded to whole numbers, halves to even, with the step in the low bits
+            float m[8], apart = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                // off by the bound of p, and 2 half steps of 127 / a and of the product
-                const float t = a[i] * inv, step = __builtin_rintf(t);
-                const float off = EXACT ? 127.0f * 3.0f * kHalfStep : fabsf(t) * ((bound_of<KIND>(w[i]) + 3.0f) * kHalfStep) + 1e-6f;
-                near |= fabsf(t - step) > 0.5f - off ? 1u << i : 0u;
-                s[i / 4] |= (static_cast<unsigned>(static_cast<int>(step)) & 255u) << (8 * (i & 3));
+                const float t = a[i] * inv;
+                m[i] = t + 12582912.0f;
+                apart = fmaxf(apart, fabsf(t - (m[i] - 12582912.0f)));
             }
-            steps = static_cast<uint64_t>(s[1]) << 32 | s[0];
-            for (near = tiny ? 255u : near; near; near &= near - 1) {
-                const int i = __builtin_ctz(near);
-                if (i >= n) break;
-                double v;
-                if constexpr (KIND == MOPAR_GATE_NONE)
-                    v = static_cast<float>(x[at + i]);
-                else
-                    v = exact(at + i);
-                const uint64_t step = static_cast<uint64_t>(static_cast<int64_t>(rint(v * 127.0 / top64))) & 255u;
-                steps = (steps & ~(uint64_t(255) << (8 * i))) | step << (8 * i);
-            }
-        }
-        if (out) {
-            float o[8];
+            auto low = [&](int i) { return __float_as_uint(m[i]); };
+            const unsigned s0 = __builtin_amdgcn_perm(low(1), low(0), 0x0c0c0400), s1 = __builtin_amdgcn_perm(low(3), low(2), 0x04000c0c);
+            const unsigned s2 = __builtin_amdgcn_perm(low(5), low(4), 0x0c0c0400), s3 = __builtin_amdgcn_perm(low(7), low(6), 0x04000c0c);
+            steps = static_cast<uint64_t>(s2 | s3) << 32 | (s0 | s1);
+            if (apart > middle) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = a[i] * r;
-            store8(out + at, n, o);
+                for (int i = 0; i < 8; ++i) near |= !(fabsf(a[i] * inv - (m[i] - 12582912.0f)) <= middle) ? 1u << i : 0u;
+                if (n < 8) near &= (1u << n) - 1;
+            }
         }
-        if (!q) return;
         if (n >= 8) {
             *reinterpret_cast<uint64_t*>(q + at) = steps;
         } else {
             for (int i = 0; i < n; ++i) q[at + i] = static_cast<int8_t>(steps >> (8 * i));
         }
-    });
+        return near;
+    };
+    auto store_out = [&](int c, const float (&a)[8]) __attribute__((always_inline)) {
+        float o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = a[i] * r;
+        store8(out + c * 8, p.width - c * 8, o);
+    };
+    // (out may be what the exact values are read from: it is stored after them)
+    if constexpr (CH > 0) {
+        if (q) {
+            uint64_t near = 0;
+#pragma unroll
+            for (int k = 0; k < CH; ++k)
+                if (me + k * TPR < p.chunks) near |= static_cast<uint64_t>(store_steps(me + k * TPR, f[k])) << (8 * k);
+            for (; near; near &= near - 1) {
+                const int at = place(__builtin_ctzll(near));
+                q[at] = right(at);
+            }
+        }
+        if (out)
+#pragma unroll
+            for (int k = 0; k < CH; ++k)
+                if (me + k * TPR < p.chunks) store_out(me + k * TPR, f[k]);
+    } else {
+        for (int c = me; c < p.chunks; c += TPR) {
+            read(c, f[0], false);
+            if (q)
+                for (unsigned near = store_steps(c, f[0]); near; near &= near - 1) {
+                    const int at = c * 8 + __builtin_ctz(near);
+                    q[at] = right(at);
+                }
+            if (out) store_out(c, f[0]);
+        }
+    }
 }
 
 template <typename T, int KIND> hipError_t launch(const RowsParams& p, hipStream_t s) {
@@ -284,12 +327,27 @@ template <typename T, int KIND> hipError_t launch(const RowsParams& p, hipStream
         return hipGetLastError();
     };
     using std::integral_constant;
-    if (p.chunks <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    if (p.chunks <= 256) return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    if (p.chunks <= 512) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-    if (p.chunks <= 1024) return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-    if (p.chunks <= 4096) return go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
-    return go(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
+    integral_constant<int, 1> one;
+    integral_constant<int, 2> two;
+    integral_constant<int, 4> four;
+    integral_constant<int, 8> eight;
+    integral_constant<int, 32> t32;
+    integral_constant<int, 64> t64;
+    integral_constant<int, 256> t256;
+    integral_constant<int, 1024> t1024;
+    if (p.chunks > 256 && p.tokens <= 512) {
+        if (p.chunks <= 1024) return go(t1024, one);
+        if (p.chunks <= 2048) return go(t1024, two);
+    }
+    if (p.chunks <= 32) return go(t32, one);
+    if (p.chunks <= 64) return go(t64, one);
+    if (p.chunks <= 128) return go(t64, two);
+    if (p.chunks <= 256) return go(t64, four);
+    if (p.chunks <= 512) return go(t256, two);
+    if (p.chunks <= 1024) return go(t256, four);
+    if (p.chunks <= 2048) return go(t256, eight);
+    if (p.chunks <= 4096) return go(t1024, four);
+    return go(t1024, integral_constant<int, 0>{});
 }
 
 }  // namespace
