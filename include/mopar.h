@@ -392,8 +392,7 @@ typedef enum { MOPAR_GATE_NONE = 0, MOPAR_GATE_SILU = 1, MOPAR_GATE_GELU = 2 } m
 
 /* Rows in 8 bits: p = x (MOPAR_GATE_NONE; gate NULL), silu(gate) x = gate x / (1 + e^-gate),
  * or gelu(gate) x = gate (1 + erf(gate / sqrt 2)) / 2 x, not rounded before; q and scale = a / 127
- * as for mopar_rms_norm, as 64-bit arithmetic gives them where the gate's activation stays in
- * float32's normal range.  Also how weights [n_out][width] are made: a row of theirs is
+ * as for mopar_rms_norm, as 64-bit arithmetic gives them.  Also how weights [n_out][width] are made: a row of theirs is
  * a channel.  Errors: as mopar_rms_norm. */
 int mopar_quantize_rows(int32_t dtype, int64_t tokens, int32_t width, const mopar_matrix* x, const mopar_matrix* gate,
                         int32_t act, const mopar_rows8* out8, void* stream);

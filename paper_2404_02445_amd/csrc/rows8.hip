@@ -8,7 +8,12 @@
 // The steps are those of 64-bit arithmetic.  In float32 127 p / a is off by a part that is known (value()), which decides nothing
 // unless the value lies within it of the middle between two steps: those, one in some thousands, are worked out again in float64 (a row
 // that float32 knows too little of, as one of gates all far below zero, altogether).  So that a is exact too, the values within float32's
-// error of the largest are worked out in float64 first; bf16 norms and plain rows need neither, their p is exact in float32.
+// error of the largest are worked out in float64 first; bf16 norms and plain rows need not, their p is exact in float32.
+//
+// Bound by memory from some hundred rows on: bf16 norms with a residual, to 8 bits, of 16384 x 4096 take 89 us (5.3 TB/s, a large copy
+// 5.2), 65536 x 256 25 us, float32 4096 x 4096 53; rows of 4096 x 14336 42 us plain, 74 by SiLU (4.0 TB/s), 87 by GELU, which
+// its 23 instructions a value bound.  Few rows wait for their loads and one reduction: 8 x 8192 4.0 us, 64 x 14336 by SiLU 7.1.  Rows that
+// start between 16-byte places cost about half of the rate (4001 x 11007 by SiLU 87 us): each load touches two lines.
 #include <type_traits>
 
 #include "internal.h"
@@ -74,28 +79,32 @@ __device__ __forceinline__ float erf_(float x) {
 }
 
 constexpr float kHalfStep = 6.0e-8f;                 // 2^-24, and the roundings of the bounds
-// p in float32, and how far it may be off.  A product of two elements: half a step.  SiLU: exponential 4 half steps, sum 1,
-// reciprocal 2, products 3.  GELU: erf 1.5e-7 + 20 half steps (1.35e-6 in all) and 12 more
-// of its argument, the sum and the products, all times |g x| / 2.
-template <int KIND> __device__ __forceinline__ float value(float v, float w, float& off) {
+// p in float32.  How far it may be off follows (in far_of()) from the row's largest |p| and its largest reach.
+template <int KIND> __device__ __forceinline__ float value(float v, float w, float& reach) {
     if constexpr (KIND == NORM) {
-        const float p = v * w;
-        off = fabsf(p) * kHalfStep;
-        return p;
+        return v * w;
     } else if constexpr (KIND == MOPAR_GATE_SILU) {
-        const float p = w * __builtin_amdgcn_rcpf(1.0f + exp_(fminf(fmaxf(-w, -104.0f), 88.0f))) * v;
-        off = fabsf(p) * (10.0f * kHalfStep);
-        return p;
+        const float g = __builtin_fmaf(w, 0.0f, fmaxf(w, -88.0f));      // (infinities and NaN give NaN)
+        reach = fabsf(v);
+        return g * __builtin_amdgcn_rcpf(1.0f + exp_(-fminf(g, 104.0f))) * v;
     } else if constexpr (KIND == MOPAR_GATE_GELU) {
-        const float half = 0.5f * w * v, p = half * (1.0f + erf_(w * 0.707106781f));
-        off = fabsf(half) * (1.35e-6f + 12.0f * kHalfStep);          // (1 + erf is at most 2)
-        return p;
+        const float g = __builtin_fmaf(w, 0.0f, fmaxf(w, -15.0f));
+        reach = fabsf(g * v);
+        return 0.5f * g * (1.0f + erf_(g * 0.707106781f)) * v;
     } else {
-        off = 0.0f;
         return v;
     }
 }
-template <int KIND> __device__ __forceinline__ double value64(double v, double w) {
+// A product of two elements: half a step.  SiLU: exponential 4 half steps, sum 1, reciprocal 2, products 3, and 88 e^-88 |x| where g
+// is below -88 or the reciprocal underflows.  GELU: erf 1.5e-7 + 20 half steps (1.35e-6 in all) and 12 more of its argument, the sum
+// and the products, all times |g x| / 2; g below -15 leaves less than that.
+template <int KIND> __device__ __forceinline__ float far_of(float top, float reach) {
+    if constexpr (KIND == NORM) return top * kHalfStep;
+    if constexpr (KIND == MOPAR_GATE_SILU) return top * (10.0f * kHalfStep) + reach * 1e-36f;
+    return reach * (0.5f * (1.35e-6f + 12.0f * kHalfStep));
+}
+// (a call of its own: with its registers the kernels of 14336 columns gated by GELU took 127 us for 84)
+template <int KIND> __device__ __attribute__((noinline)) double value64(double v, double w) {
     if constexpr (KIND == MOPAR_GATE_SILU) return w / (1.0 + exp(-w)) * v;
     if constexpr (KIND == MOPAR_GATE_GELU) return 0.5 * w * erfc(w * -0.70710678118654752) * v;
     return v * w;
@@ -159,7 +168,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
     T* const total = p.total ? reinterpret_cast<T*>(p.total) + row * p.ts : nullptr;
     T* const out = p.out ? reinterpret_cast<T*>(p.out) + row * p.os : nullptr;
 
-    float squares = 0.0f, far = 0.0f;                // far: how far a p of the row may be off
+    float squares = 0.0f, reach = 0.0f;
     unsigned top_bits = 0;                           // of the row's largest |p|; infinities and NaN are above all others
     // p of chunk c; the first time, total is stored and the row's sums go on
     auto read = [&](int c, float (&f)[8], bool first) __attribute__((always_inline)) {
@@ -181,11 +190,11 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (KIND == NORM && first) squares = __builtin_fmaf(f[i], f[i], squares);
-            float off;
-            f[i] = value<KIND>(f[i], w[i], off);
+            float its = 0.0f;
+            f[i] = value<KIND>(f[i], w[i], its);
             if (first) {
                 top_bits = max(top_bits, __float_as_uint(f[i]) & 0x7fffffffu);
-                if constexpr (KIND == MOPAR_GATE_GELU) far = fmaxf(far, off);
+                reach = fmaxf(reach, its);
             }
         }
     };
@@ -209,7 +218,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
     auto most = [](float a, float b) { return fmaxf(a, b); };
     float r = 1.0f;
     if constexpr (KIND == NORM) r = 1.0f / __builtin_sqrtf(over_row<TPR>(squares, [](float a, float b) { return a + b; }, lds[0]) * p.inv_width + p.eps);
-    float top = 0.0f;
+    float top = 0.0f, far = 0.0f;                    // far: how far a p of the row may be off
     double top64 = 0.0;
     bool finite = false;
     if (p.q) {
@@ -218,10 +227,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
         finite = top < __builtin_inff();
         top64 = top;
         if constexpr (!EXACT) {
-            if constexpr (KIND == MOPAR_GATE_GELU)
-                far = over_row<TPR>(far, most, lds[2]);
-            else
-                far = top * (KIND == NORM ? kHalfStep : 10.0f * kHalfStep);
+            if constexpr (KIND != NORM) reach = over_row<TPR>(reach, most, lds[2]);
+            far = far_of<KIND>(top, reach);
             // the row's largest in float64 is among those that float32 has within twice that of its largest
             double best = 0.0;
             if (finite && top + far > 0.0f && mine >= top - 2.0f * far) {
@@ -330,11 +337,13 @@ template <typename T, int KIND> hipError_t launch(const RowsParams& p, hipStream
     integral_constant<int, 1> one;
     integral_constant<int, 2> two;
     integral_constant<int, 4> four;
-    integral_constant<int, 8> eight;
     integral_constant<int, 32> t32;
     integral_constant<int, 64> t64;
     integral_constant<int, 256> t256;
     integral_constant<int, 1024> t1024;
+    // Threads by the row's length, so that each has 1 to 4 chunks, kept in registers: 32 threads for 256 columns 24 us at 65536 rows, 64
+    // (half of them idle) 39; 1024 threads of two chunks for 16384 columns 90 us at 4096 rows, 256 of eight 102.  Where the rows
+    // leave most of the card idle, a row's loads go out at once from as many threads as it has chunks: 8 x 8192 4.0 us, 256 threads 6.5.
     if (p.chunks > 256 && p.tokens <= 512) {
         if (p.chunks <= 1024) return go(t1024, one);
         if (p.chunks <= 2048) return go(t1024, two);
@@ -345,7 +354,7 @@ template <typename T, int KIND> hipError_t launch(const RowsParams& p, hipStream
     if (p.chunks <= 256) return go(t64, four);
     if (p.chunks <= 512) return go(t256, two);
     if (p.chunks <= 1024) return go(t256, four);
-    if (p.chunks <= 2048) return go(t256, eight);
+    if (p.chunks <= 2048) return go(t1024, two);
     if (p.chunks <= 4096) return go(t1024, four);
     return go(t1024, integral_constant<int, 0>{});
 }

@@ -177,6 +177,27 @@ def test_quantize_far_gates(dt, act):
     assert bool(out8.scales[5:9].isnan().all())
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("width", [600, 33000])
+def test_quantize_gates_beyond_float32(dt, act, width):
+    """Gates of the type's lowest value, and products of an activation that float32 hardly holds with a value near its largest."""
+    g = gen(9)
+    x = randn(g, 6, width, dt=dt).clamp(-3, 3)
+    gate = torch.zeros_like(x)
+    gate[0], gate[0, 7:9] = torch.finfo(gate.dtype).min, 1.5
+    x[1], gate[1] = x[1] * 1e38, -100.0 if act == "silu" else -9.0
+    gate[2], x[2], x[2, 1] = -95.0 if act == "silu" else -13.0, x[2] * 1e-3, 1e37
+    x[3], gate[3] = x[3] * 1e30, randn(g, 1, width, dt=dt)[0] - (88.0 if act == "silu" else 12.0)
+    gate[4], gate[4, 5], x[4, 5] = torch.finfo(gate.dtype).min, -12.0, 1e38
+    gate[5] = torch.finfo(gate.dtype).min
+    out8 = P.alloc_rows8(6, width, "cuda")
+    P.mopar_quantize_rows(x, out8, gate=gate, act=act)
+    steps, top = R.steps(R.gated(x, gate, act))
+    assert torch.equal(out8.values.cpu(), steps)
+    check(out8.scales, top / 127, top / 127 * 2.02 * U + 1e-38)
+
+
 def test_quantize_small_and_large_rows():
     """Rows at both ends of float32."""
     x = torch.tensor([[1e-38, -3e-39, 0.0], [1e-44, 7e-45, -1e-45], [3.3e38, -1e38, 1.0], [1e-31, 5e-32, 2e-33], [0.0, -0.0, 0.0]], device="cuda")
