@@ -11,9 +11,9 @@
 // error of the largest are worked out in float64 first; bf16 norms and plain rows need not, their p is exact in float32.
 //
 // Bound by memory from some hundred rows on: bf16 norms with a residual, to 8 bits, of 16384 x 4096 take 89 us (5.3 TB/s, a large copy
-// 5.2), 65536 x 256 25 us, float32 4096 x 4096 53; rows of 4096 x 14336 42 us plain, 74 by SiLU (4.0 TB/s), 87 by GELU, which
+// 5.2), 65536 x 256 25 us, float32 4096 x 4096 53; rows of 4096 x 14336 39 us plain, 69 by SiLU (4.3 TB/s), 76 by GELU, which
 // its 23 instructions a value bound.  Few rows wait for their loads and one reduction: 8 x 8192 4.0 us, 64 x 14336 by SiLU 7.1.  Rows that
-// start between 16-byte places cost about half of the rate (4001 x 11007 by SiLU 87 us): each load touches two lines.
+// start between 16-byte places lose a fifth (4001 x 11007 by GELU 77 us, 4096 x 11008 60): most loads touch two lines.
 #include <type_traits>
 
 #include "internal.h"
@@ -138,29 +138,29 @@ template <int D> __device__ __forceinline__ double xor_lane(double v) {
     const uint64_t k = __builtin_bit_cast(uint64_t, v);
     return __builtin_bit_cast(double, static_cast<uint64_t>(xor_lane<D>(static_cast<unsigned>(k >> 32))) << 32 | xor_lane<D>(static_cast<unsigned>(k)));
 }
-// v of all the TPR threads of a row, combined by f; each value of several threads' rows has its own lds[16]
+// v >= 0 of all the TPR threads of a row (0: of the block), combined by f, a sum or a maximum; each value of a block has its own lds[16]
 template <int TPR, typename V, typename F> __device__ __forceinline__ V over_row(V v, F f, V* lds) {
-    if constexpr (TPR > 32) v = f(v, xor_lane<32>(v));
+    if constexpr (TPR != 32) v = f(v, xor_lane<32>(v));
     v = f(v, xor_lane<16>(v)), v = f(v, xor_lane<8>(v)), v = f(v, xor_lane<4>(v)), v = f(v, xor_lane<2>(v)), v = f(v, xor_lane<1>(v));
-    if constexpr (TPR > 64) {
+    if constexpr (TPR == 0) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = lds[0];
-#pragma unroll
-        for (int i = 1; i < TPR / 64; ++i) v = f(v, lds[i]);
+        v = (threadIdx.x & 15) < blockDim.x / 64 ? lds[threadIdx.x & 15] : V(0);
+        v = f(v, xor_lane<8>(v)), v = f(v, xor_lane<4>(v)), v = f(v, xor_lane<2>(v)), v = f(v, xor_lane<1>(v));
     }
     return v;
 }
 
-// TPR threads take a row, CH chunks each (0: any number, read twice); a block takes the rows of 256 threads, or one.
+// TPR threads take a row and a block the rows of 256 threads, or a block (TPR 0, up to 1024 threads) takes one; CH chunks a thread (0: any
+// number, read twice).
 template <typename T, int KIND, int TPR, int CH>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const RowsParams p) {
-    constexpr int THREADS = TPR > 256 ? TPR : 256;
+__global__ __launch_bounds__(TPR ? 256 : 1024) void rows8_kernel(const RowsParams p) {
     constexpr bool EXACT = KIND == MOPAR_GATE_NONE || (KIND == NORM && sizeof(T) == 2);      // p is exact in float32
     __shared__ double lds64[16];
     __shared__ float lds[3][16];
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (THREADS / TPR) + threadIdx.x / TPR;
-    const int me = threadIdx.x % TPR;
+    const int many = TPR ? TPR : static_cast<int>(blockDim.x);
+    const int64_t row = TPR ? static_cast<int64_t>(blockIdx.x) * (256 / (TPR ? TPR : 1)) + threadIdx.x / many : blockIdx.x;
+    const int me = TPR ? threadIdx.x % many : threadIdx.x;
     if (row >= p.tokens) return;                     // (lanes of one row stay together: none is missed by others, and no barrier by rows of several waves)
     const T* const x = reinterpret_cast<const T*>(p.x) + row * p.xs;
     const T* const res = p.residual ? reinterpret_cast<const T*>(p.residual) + row * p.rs : nullptr;
@@ -210,11 +210,11 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
     if constexpr (CH > 0) {
 #pragma unroll
         for (int k = 0; k < CH; ++k)
-            if (me + k * TPR < p.chunks) read(me + k * TPR, f[k], true);
+            if (me + k * many < p.chunks) read(me + k * many, f[k], true);
     } else {
-        for (int c = me; c < p.chunks; c += TPR) read(c, f[0], true);
+        for (int c = me; c < p.chunks; c += many) read(c, f[0], true);
     }
-    auto place = [&](int bit) { return (me + (bit >> 3) * TPR) * 8 + (bit & 7); };      // of element bit % 8 of the thread's chunk bit / 8
+    auto place = [&](int bit) { return (me + (bit >> 3) * many) * 8 + (bit & 7); };      // of element bit % 8 of the thread's chunk bit / 8
     auto most = [](float a, float b) { return fmaxf(a, b); };
     float r = 1.0f;
     if constexpr (KIND == NORM) r = 1.0f / __builtin_sqrtf(over_row<TPR>(squares, [](float a, float b) { return a + b; }, lds[0]) * p.inv_width + p.eps);
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
                     uint64_t near = 0;
 #pragma unroll
                     for (int k = 0; k < CH; ++k)
-                        if (me + k * TPR < p.chunks)
+                        if (me + k * many < p.chunks)
 #pragma unroll
                             for (int i = 0; i < 8; ++i) near |= fabsf(f[k][i]) >= top - 2.0f * far ? uint64_t(1) << (8 * k + i) : 0u;
                     for (; near; near &= near - 1) {
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
                         if (at < p.width) best = fmax(best, fabs(exact(at)));
                     }
                 } else {
-                    for (int c = me; c < p.chunks; c += TPR) {
+                    for (int c = me; c < p.chunks; c += many) {
                         read(c, f[0], false);
                         for (int i = 0; i < min(8, p.width - c * 8); ++i)
                             if (fabsf(f[0][i]) >= top - 2.0f * far) best = fmax(best, fabs(exact(c * 8 + i)));
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
             uint64_t near = 0;
 #pragma unroll
             for (int k = 0; k < CH; ++k)
-                if (me + k * TPR < p.chunks) near |= static_cast<uint64_t>(store_steps(me + k * TPR, f[k])) << (8 * k);
+                if (me + k * many < p.chunks) near |= static_cast<uint64_t>(store_steps(me + k * many, f[k])) << (8 * k);
             for (; near; near &= near - 1) {
                 const int at = place(__builtin_ctzll(near));
                 q[at] = right(at);
@@ -313,9 +313,9 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
         if (out)
 #pragma unroll
             for (int k = 0; k < CH; ++k)
-                if (me + k * TPR < p.chunks) store_out(me + k * TPR, f[k]);
+                if (me + k * many < p.chunks) store_out(me + k * many, f[k]);
     } else {
-        for (int c = me; c < p.chunks; c += TPR) {
+        for (int c = me; c < p.chunks; c += many) {
             read(c, f[0], false);
             if (q)
                 for (unsigned near = store_steps(c, f[0]); near; near &= near - 1) {
@@ -328,9 +328,15 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rows8_kernel(const Rows
 }
 
 template <typename T, int KIND> hipError_t launch(const RowsParams& p, hipStream_t s) {
-    auto go = [&](auto tpr, auto ch) {
-        constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value, THREADS = TPR > 256 ? TPR : 256, PER = THREADS / TPR;
-        launch_kernel((rows8_kernel<T, KIND, TPR, CH>), dim3(static_cast<unsigned>((p.tokens + PER - 1) / PER)), dim3(THREADS), 0, s, p);
+    auto rows = [&](auto tpr, auto ch) {                 // several rows a block
+        constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value, PER = 256 / TPR;
+        launch_kernel((rows8_kernel<T, KIND, TPR, CH>), dim3(static_cast<unsigned>((p.tokens + PER - 1) / PER)), dim3(256), 0, s, p);
+        return hipGetLastError();
+    };
+    auto row = [&](auto ch) {                            // a row a block, its waves in fours, one a SIMD (4096 x 14336 by SiLU 86 us with 14 waves, 74 with 16)
+        constexpr int CH = decltype(ch)::value;
+        const int waves = CH ? 4 * ((p.chunks + 256 * CH - 1) / (256 * CH)) : 16;
+        launch_kernel((rows8_kernel<T, KIND, 0, CH>), dim3(static_cast<unsigned>(p.tokens)), dim3(waves * 64), 0, s, p);
         return hipGetLastError();
     };
     using std::integral_constant;
@@ -339,24 +345,28 @@ template <typename T, int KIND> hipError_t launch(const RowsParams& p, hipStream
     integral_constant<int, 4> four;
     integral_constant<int, 32> t32;
     integral_constant<int, 64> t64;
-    integral_constant<int, 256> t256;
-    integral_constant<int, 1024> t1024;
     // Threads by the row's length, so that each has 1 to 4 chunks, kept in registers: 32 threads for 256 columns 24 us at 65536 rows, 64
-    // (half of them idle) 39; 1024 threads of two chunks for 16384 columns 90 us at 4096 rows, 256 of eight 102.  Where the rows
-    // leave most of the card idle, a row's loads go out at once from as many threads as it has chunks: 8 x 8192 4.0 us, 256 threads 6.5.
-    if (p.chunks > 256 && p.tokens <= 512) {
-        if (p.chunks <= 1024) return go(t1024, one);
-        if (p.chunks <= 2048) return go(t1024, two);
+    // (half of them idle) 39.  Where the rows leave most of the card idle, a row's loads go out at once from as many threads as
+    // it has chunks: 8 x 8192 4.0 us, 256 threads 6.5; 64 x 14336 by SiLU 7.1 with two a thread, 7.8 with four.
+    if (p.chunks > 256 && p.chunks <= 2048 && p.tokens <= 512) return p.chunks <= 1024 ? row(one) : row(two);
+    if (p.chunks <= 32) return rows(t32, one);
+    if (p.chunks <= 64) return rows(t64, one);
+    if (p.chunks <= 128) return rows(t64, two);
+    if (p.chunks <= 256) return rows(t64, four);
+    if constexpr (KIND == NORM) {
+        // two a thread hide the loads of the others best: 4096 x 14336 80 us, four 86
+        if (p.chunks <= 2048) return row(two);
+    } else if (p.chunks <= 4096) {
+        // the fewest idle threads, then the fewest threads: 4096 x 11008 by GELU 72, 60 and 66 us with 2, 3 and 4 a thread, x 14336 86, 84, 76
+        // (float32, whose chunks are two loads: the most threads, x 14336 by SiLU 98, 99 and 103)
+        auto room = [&](int ch) { const int by = (p.chunks + 256 * ch - 1) / (256 * ch); return by <= 4 ? by * ch : 1 << 20; };
+        const int same = sizeof(T) == 4;
+        if (room(2) < room(3) + same && room(2) < room(4) + same) return row(two);
+        if (room(3) < room(4) + same) return row(integral_constant<int, 3>{});
+        return row(four);
     }
-    if (p.chunks <= 32) return go(t32, one);
-    if (p.chunks <= 64) return go(t64, one);
-    if (p.chunks <= 128) return go(t64, two);
-    if (p.chunks <= 256) return go(t64, four);
-    if (p.chunks <= 512) return go(t256, two);
-    if (p.chunks <= 1024) return go(t256, four);
-    if (p.chunks <= 2048) return go(t1024, two);
-    if (p.chunks <= 4096) return go(t1024, four);
-    return go(t1024, integral_constant<int, 0>{});
+    if (p.chunks <= 4096) return row(four);
+    return row(integral_constant<int, 0>{});
 }
 
 }  // namespace
