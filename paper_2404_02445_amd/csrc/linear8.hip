@@ -5,7 +5,8 @@
 //
 // Operands come straight to LDS, 128 bytes of k a row and stage, eight rows (1 KB) a load instruction, whole lines where rows
 // start at multiples of 128 bytes.  The weight fragment is the MFMA's first operand: a lane ends up with four neighbouring columns of
-// one row.  Chunks past the sum read zeros; a chunk that the sum ends in is cut in the fragments of x.
+// one row.  Chunks past the sum read zeros; a chunk that the sum ends in is cut in the fragments of x.  Rows that start off 128-byte
+// lines: 8192 x 4096 by 14336 columns 404 -> 458 us, 64 x 14336 by 4096 23 -> 34.
 #pragma clang diagnostic ignored "-Winline-asm"      // (m0, which the loads into LDS take, is in no other use)
 #include <algorithm>
 #include <type_traits>
@@ -133,7 +134,8 @@ __device__ __forceinline__ bool place_of(const Linear8Params& p, int bm, int bn,
 // barrier behind each, and the second group runs one step behind the first: while one wave of a SIMD multiplies, the other
 // reads and loads.  256: two stages of 64 KB in LDS; A0 and the columns' halves (B) are read in the first phase and loaded again,
 // for the step after next, in the second; A1 the other way round.  128: one phase, four stages of 32 KB, loads three steps
-// ahead.  At the end of a memory step eight later loads stay in flight.
+// ahead.  At the end of a memory step eight later loads stay in flight.  Bound by the matrix units: 8192 x 4096 by 14336 columns take
+// 400 us, 2.40 POP/s.
 //
 // A block runs up to kPairTiles tiles, and the loads go on into the next one during the last steps of a tile.  The scales of a
 // tile come to LDS with its first step, into the wave's own space, where its results turn at the end so that a store covers
@@ -492,6 +494,10 @@ __global__ __launch_bounds__(512, 2) void linear8_pair_kernel(const Linear8Param
 // operands are asked for early and in whole lines, and that no wave waits for another.  Each wave has a ring of NS stages of its
 // own, 128 bytes of k of all the tile's rows and columns; the waves' sums meet in LDS at the end.  XL: 8-row loads of x a
 // stage (rows past them are never stored).
+//
+// Up to 16 rows the weight's bytes bound it (1 x 4096 by 4096 columns 5.2 us, by 28672 23.2: 5.1 TB/s), past them what a CU
+// takes in by direct loads, some 45 to 50 GB/s for all that its tiles read (64 x 4096 by 4096 7.3 us, 64 x 14336 by 4096 15).  Operands
+// straight into registers took 38 us for 23 there, and 64 x 64 tiles of waves in step with each other 13.3 us for 8.5 at 128 x 4096.
 // ---------------------------------------------------------------------------
 template <typename T, int FM, int XL, int FN, int W, int NS>
 __global__ __launch_bounds__(W * 64) void linear8_wave_kernel(const Linear8Params p) {
@@ -588,7 +594,7 @@ __global__ __launch_bounds__(W * 64) void linear8_wave_kernel(const Linear8Param
     }
 }
 
-// The shares of a sum added up: a thread takes four columns of a row.
+// The shares of a sum added up: a thread takes four columns of a row.  Bound by its launch (2 us), as the partial sums fit the caches.
 template <typename T>
 __global__ __launch_bounds__(256) void linear8_join_kernel(const Linear8Params p) {
     const int64_t groups = (p.n + 3) / 4, t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
@@ -618,7 +624,9 @@ __global__ __launch_bounds__(256) void linear8_join_kernel(const Linear8Params p
 
 }  // namespace
 
-// Tile edge of linear8_pair_kernel for a product, 0 where linear8_wave_kernel runs it: its tiles have to fill the CUs.
+// Tile edge of linear8_pair_kernel for a product, 0 where linear8_wave_kernel runs it: its tiles have to fill the CUs.  Sums of
+// 4096 in us: 128 tiles take 31.2 for 96 rows by 28672 columns (224 tiles), the others 41.7, 22.0 and 28.1 for 512 by 6144 (192 tiles), 20.8 and
+// 16.4 for 192 by 6144 (96); 256 tiles 60.5 for 512 by 28672 (224 tiles), 128 tiles 87.8.  64 rows by 28672: 30.6 and 30.9.
 static int pair_tile(int64_t m, int64_t n, int k) {
     if (k <= 256 || m <= 64) return 0;
     const int64_t tiles = (m + 255) / 256 * ((n + 255) / 256), rounds = (tiles + kCUs - 1) / kCUs;
@@ -637,6 +645,12 @@ size_t linear8_ws_bytes(int64_t m, int64_t n, int k) {
     return static_cast<size_t>(m >= most / n ? most : std::min(most, m * n * kMostSplits)) * 4;
 }
 
+// Few rows: the fewest rows and columns a block that leave no CU two of them; more stages where a CU has one block.  In us, sums of 4096: one row
+// by 28672 columns 23.2 with two stages, 24.2 with four, 1 x 14336 by 4096 14.7 and 12.0; 32 rows by 4096, 6144 and 28672 5.8, 8.2 and 34.9
+// in blocks of 32 x 16, 6.5, 7.1 and 27.7 in 32 x 32.  64 rows by 4096: 32 x 32 7.3, 64 x 32 8.5, 64 x 64 10.5; 128 rows 11.7, 8.5, 10.5;
+// 192 rows by 4096 (192 blocks of 64 x 64) 10.6 with eight waves, 13.6 with four, by 6144 (288) 19.1 and 16.8.
+// Shares of a sum: 64 x 14336 by 1024 columns 13.1 whole, 11.0 in four, 1 x 28672 by 512 12.8 and 8.9; below kLongShare the join costs
+// more than it gives (64 x 4096 by 1024 6.9 and 8.9, 1 x 14336 by 1024 8.2 and 8.3).
 Linear8Plan linear8_plan(int64_t m, int64_t n, int k, size_t ws_bytes) {
     auto tiles = [&](int bm, int bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); };
     Linear8Plan plan{64, 64, 4, 1, 1};

@@ -14,6 +14,7 @@
 // 5.2), 65536 x 256 25 us, float32 4096 x 4096 53; rows of 4096 x 14336 39 us plain, 69 by SiLU (4.3 TB/s), 76 by GELU, which
 // its 23 instructions a value bound.  Few rows wait for their loads and one reduction: 8 x 8192 4.0 us, 64 x 14336 by SiLU 7.1.  Rows that
 // start between 16-byte places lose a fifth (4001 x 11007 by GELU 77 us, 4096 x 11008 60): most loads touch two lines.
+#include <algorithm>
 #include <type_traits>
 
 #include "internal.h"
@@ -115,7 +116,8 @@ struct RowsParams {
     unsigned char *total, *out;
     int8_t* q;
     float* scale;
-    int64_t tokens, xs, rs, gs, ts, os, qs;     // strides in elements
+    int64_t first, tokens;                      // rows of this launch: first .. tokens - 1
+    int64_t xs, rs, gs, ts, os, qs;             // strides in elements
     int width, chunks;                          // chunks of eight elements
     float eps, inv_width;
 };
@@ -159,7 +161,7 @@ __global__ __launch_bounds__(TPR ? 256 : 1024) void rows8_kernel(const RowsParam
     __shared__ double lds64[16];
     __shared__ float lds[3][16];
     const int many = TPR ? TPR : static_cast<int>(blockDim.x);
-    const int64_t row = TPR ? static_cast<int64_t>(blockIdx.x) * (256 / (TPR ? TPR : 1)) + threadIdx.x / many : blockIdx.x;
+    const int64_t row = p.first + (TPR ? static_cast<int64_t>(blockIdx.x) * (256 / (TPR ? TPR : 1)) + threadIdx.x / many : blockIdx.x);
     const int me = TPR ? threadIdx.x % many : threadIdx.x;
     if (row >= p.tokens) return;                     // (lanes of one row stay together: none is missed by others, and no barrier by rows of several waves)
     const T* const x = reinterpret_cast<const T*>(p.x) + row * p.xs;
@@ -328,16 +330,21 @@ __global__ __launch_bounds__(TPR ? 256 : 1024) void rows8_kernel(const RowsParam
 }
 
 template <typename T, int KIND> hipError_t launch(const RowsParams& p, hipStream_t s) {
-    auto rows = [&](auto tpr, auto ch) {                 // several rows a block
-        constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value, PER = 256 / TPR;
-        launch_kernel((rows8_kernel<T, KIND, TPR, CH>), dim3(static_cast<unsigned>((p.tokens + PER - 1) / PER)), dim3(256), 0, s, p);
+    auto go = [&](auto kernel, int threads, int per) {   // a launch takes less than 2^32 threads
+        RowsParams part = p;
+        for (constexpr int64_t kBlocks = 1 << 21; part.first < p.tokens; part.first += kBlocks * per) {
+            const int64_t blocks = std::min(kBlocks, (p.tokens - part.first + per - 1) / per);
+            launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(threads), 0, s, part);
+        }
         return hipGetLastError();
+    };
+    auto rows = [&](auto tpr, auto ch) {                 // several rows a block
+        constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
+        return go(rows8_kernel<T, KIND, TPR, CH>, 256, 256 / TPR);
     };
     auto row = [&](auto ch) {                            // a row a block, its waves in fours, one a SIMD (4096 x 14336 by SiLU 86 us with 14 waves, 74 with 16)
         constexpr int CH = decltype(ch)::value;
-        const int waves = CH ? 4 * ((p.chunks + 256 * CH - 1) / (256 * CH)) : 16;
-        launch_kernel((rows8_kernel<T, KIND, 0, CH>), dim3(static_cast<unsigned>(p.tokens)), dim3(waves * 64), 0, s, p);
-        return hipGetLastError();
+        return go(rows8_kernel<T, KIND, 0, CH>, CH ? 256 * ((p.chunks + 256 * CH - 1) / (256 * (CH ? CH : 1))) : 1024, 1);
     };
     using std::integral_constant;
     integral_constant<int, 1> one;

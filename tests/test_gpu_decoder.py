@@ -177,6 +177,21 @@ def test_quantize_far_gates(dt, act):
     assert bool(out8.scales[5:9].isnan().all())
 
 
+def test_more_rows_than_a_launch_takes():
+    """2^24 rows and some: the rows of a launch's end and of the next."""
+    rows = (1 << 24) + 1000
+    x = (torch.arange(rows, device="cuda", dtype=torch.int32) % 251 - 125).float()[:, None]
+    x = torch.cat([x, torch.full_like(x, 127)], 1)
+    out8 = P.alloc_rows8(rows, 2, "cuda")
+    out8.values.fill_(3)
+    P.mopar_quantize_rows(x, out8)
+    assert torch.equal(out8.values.float(), x) and bool((out8.scales == 1).all())
+    out = torch.empty_like(x)
+    P.mopar_rms_norm(x, torch.ones(2, device="cuda"), out=out)
+    r = 1 / torch.sqrt(x.double().square().mean(1, keepdim=True) + 1e-6)
+    assert bool(((out.double() - x * r).abs() <= (x * r).abs() * (R.sum_bound(2) + 9 * U)).all())
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 @pytest.mark.parametrize("width", [600, 33000])
