@@ -13,8 +13,8 @@
 // What bounds it, measured (a copy reaches 5.16 TB/s): 2048 x 128000 in bf16, 524 MB, 98 us without alternatives (memory; some ten
 // vector instructions a logit, of which the exponential counts four, keep the ALUs at two thirds), 119 with five (124 between other
 // calls), 129 with 20: the pieces that are looked at again, when nothing is left to be streamed.  64 registers, for eight waves a
-// SIMD: with 72 the 2048 blocks took two rounds of the card and 147 us.  257 x 32003 in float32 12.6 us: one block more than CUs (256
-// rows 9.4).  4 x 128000 with 20 alternatives 14.5 us: two launches, two loads in a row, and six barriers.
+// SIMD: with 72 the 2048 blocks took two rounds of the card and 147 us.  257 x 32003 in float32 10.6 us: one row more than CUs (256
+// rows 9.3).  4 x 128000 with 20 alternatives 14.4 us: two launches, two loads in a row, and six barriers.
 // Tried without gain: keeping the list up to date along the row by bitonic sorts across lanes (4 x 128000 16.7, 2048 x 128000 138 us
 // with five), by insertions one at a time (17.4, 145), loads a step ahead (168).
 #include <algorithm>
@@ -459,14 +459,24 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobParams p
 
 }  // namespace
 
-// Blocks that share a row, and the waves of a block.  Up to 32 rows leave most CUs idle: their rows are shared out among blocks of four
-// waves, one step of 4096 elements each where there are enough blocks (4 x 128000 with 20 alternatives 23.1 us unshared, 12.6; 32 rows
-// 25.4 / 21.3; 128 rows in two shares 26.7 / 41.  Rows that fill the card take four waves each, those between 16.
-static int logprob_waves(int64_t rows, int splits) { return splits > 1 || rows >= 1024 ? 4 : 16; }
+// Blocks that share a row.  Few rows leave most CUs idle: with 20 alternatives of 128000 4 rows take 23.2 us whole and 14.4 shared out, 64
+// rows 26.1 and 21.1, 128 rows 27.3 and 27.2 (without alternatives 16.7 and 14.0), 4 x 32000 14.1 either way, 64 x 32000 14.9 and 16.6: so up to 32
+// rows are, in pieces of 4096 elements and more, and up to 128 long ones.
 int logprob_splits(int64_t rows, int vocab) {
-    if (rows > 32) return 1;
+    if (rows > (vocab >= 65536 ? 128 : 32)) return 1;
     const int64_t idle = kLogprobBlocks / std::max<int64_t>(rows, 1);
     return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({idle, (vocab + 4095) / 4096, kLogprobSplits})));
+}
+
+// The waves of a block.  One share of a row: four (4 x 128000 14.4 us, by eight 14.8), of long rows, of which each CU has one share, eight up to 8192
+// elements and 16 past them (16 x 128000 17.1 by four, 15.0 by eight, 16.5 by 16, 32 rows 21.6, 17.9, 17.6).  Whole rows: four
+// where they fill the card many times; 16 hold two rows a CU, so past 512 rows eight (600 x 32000 29.1 us by 16, 22.8 by eight, 24.0 by
+// four), and past 256, or up to 8192 elements, where a wave of 16 has two steps and less (257 x 32003 in float32 12.5 and 10.6, 300 x
+// 128000 36.7 and 43.2, 64 x 8000 10.1 and 8.6, 200 x 32000 14.5 and 16.2).
+static int logprob_waves(int64_t rows, int vocab, int splits, int share) {
+    if (splits > 1) return rows <= 8 || vocab < 65536 ? 4 : share <= 8192 ? 8 : 16;
+    if (rows >= 1024) return 4;
+    return rows > 512 || vocab <= (rows > 256 ? 32768 : 8192) ? 8 : 16;
 }
 
 // (of as many rows as share at all: a size that does not fall as rows grow)
@@ -508,7 +518,11 @@ hipError_t launch_token_logprobs(const LogprobJob& j, int splits, void* ws, hipS
         return hipGetLastError();
     };
     auto types = [&](auto w) { return j.dtype == MOPAR_BF16 ? go(__bf16{}, w) : go(float{}, w); };
-    return logprob_waves(j.rows, splits) == 4 ? types(std::integral_constant<int, 4>{}) : types(std::integral_constant<int, 16>{});
+    switch (logprob_waves(j.rows, j.vocab, splits, p.share)) {
+    case 4: return types(std::integral_constant<int, 4>{});
+    case 8: return types(std::integral_constant<int, 8>{});
+    default: return types(std::integral_constant<int, 16>{});
+    }
 }
 
 }  // namespace mopar

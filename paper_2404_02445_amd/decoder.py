@@ -21,10 +21,11 @@ def _matrix(t, name, like, shape=None):
     st = t.stride()
     if len(st) != 2 or (st[1] != 1 and t.shape[1] != 1):
         raise ValueError(f"{name}: [rows, width] with contiguous rows")
-    if t is not like and (t.dtype != like.dtype or t.device != like.device):
-        raise ValueError(f"{name}: device or dtype differs")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name}: shape must be {tuple(shape)}")
+    if t is not like:
+        if t.dtype != like.dtype or t.device != like.device:
+            raise ValueError(f"{name}: device or dtype differs")
+        if shape is not None and t.shape != shape:
+            raise ValueError(f"{name}: shape must be {tuple(shape)}")
     return L.Matrix(t.data_ptr(), st[0])
 
 

@@ -31,29 +31,39 @@ def _size(n, name):
     return n
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)    # (torch's own handle lookup without a Stream object)
+# torch's own lookups, without a Stream object and without asking whether the GPU is up (the tensors are on it): a norm of
+# five rows takes 5.5 us on the host with them, 3.4 of them its launch, and 5.9 without
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _call(fn, device, stream, *args):
     """The entry point with the stream's handle as its last argument, the tensors' device being the current one."""
-    _need(device.type == "cuda", "the tensors must be on a GPU")
-    now = torch.cuda.current_device()
-    index = now if device.index is None else device.index
+    if device.type != "cuda":
+        raise ValueError("the tensors must be on a GPU")
+    now = _current_device()
+    index = device.index
+    if index is None:
+        index = now
     if stream is not None:
         _need(stream.device.index == index, "the stream is on another device than the tensors")
         handle = stream.cuda_stream
     else:
-        handle = _raw_stream(index) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
+        handle = _raw_stream(index)
     if index == now:
-        check(fn(*args, handle))
+        status = fn(*args, handle)
     else:
         with torch.cuda.device(index):
-            check(fn(*args, handle))
+            status = fn(*args, handle)
+    if status:
+        check(status)
 
 
 def _dtype(t):
-    _need(t.dtype in _DTYPE, "tensors must be float32 or bfloat16")
-    return _DTYPE[t.dtype]
+    dt = _DTYPE.get(t.dtype)
+    if dt is None:
+        raise ValueError("tensors must be float32 or bfloat16")
+    return dt
 
 
 def _rows(t, name, like, shape=None):

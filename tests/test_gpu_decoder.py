@@ -360,6 +360,21 @@ def test_logprobs(dt, rows, vocab, top):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab,top", [(5, 8192, 64), (257, 3001, 7), (300, 32768, 5), (300, 33001, 64), (513, 40000, 3), (1023, 1000, 0), (9, 65536, 64), (20, 70001, 20),
+                                            (60, 66001, 0), (128, 65536, 64), (129, 65536, 1), (33, 65537, 33)])
+def test_logprobs_of_many_rows_and_long_ones(dt, rows, vocab, top):
+    """Each choice of waves and shares, ties and rows without weight among them."""
+    g = gen(rows + vocab)
+    x = randn(g, rows, vocab, dt=dt, by=2.0)
+    x[1::7] = (x[1::7] * 2).round()
+    x[2::11] = x[2::11].sort(1).values
+    x[3::13, : vocab - 3] = -math.inf
+    x[4] = -math.inf
+    tokens = torch.randint(0, vocab, (rows,), generator=g, dtype=torch.int32).cuda()
+    check_logprobs(x, tokens, top=top)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("order", ["ascending", "descending", "equal", "two values", "last lane"])
 def test_logprobs_orders(dt, order):
     """Rows that a list of alternatives meets in the worst order, and ties, which go to the lowest index."""
