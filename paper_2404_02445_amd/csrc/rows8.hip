@@ -13,7 +13,7 @@
 // Bound by memory from some hundred rows on: bf16 norms with a residual, to 8 bits, of 16384 x 4096 take 89 us (5.3 TB/s, a large copy
 // 5.2), 65536 x 256 25 us, float32 4096 x 4096 53; rows of 4096 x 14336 39 us plain, 69 by SiLU (4.3 TB/s), 76 by GELU, which
 // its 23 instructions a value bound.  Few rows wait for their loads and one reduction: 8 x 8192 4.0 us, 64 x 14336 by SiLU 7.1.  Rows that
-// start between 16-byte places lose a fifth (4001 x 11007 by GELU 77 us, 4096 x 11008 60): most loads touch two lines.
+// start between 16-byte places cost nothing (4001 x 11007 by GELU 60 us, 11008 on such places 59).
 #include <algorithm>
 #include <type_traits>
 
@@ -29,19 +29,35 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 enum { NORM = 3 };                                   // beside mopar_gate's kinds
 
-// Eight elements from p on, of which n exist (any address that elements may have: the hardware takes unaligned vectors).
-template <typename T> __device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
-    if (n >= 8) {
+// Eight elements from p on, of which n exist (any address that elements may have: the hardware takes unaligned vectors).  The last, short chunk of a row
+// is cut from the row's last eight elements, `wide` where it has so many: element by element, rows of 11007 gated by
+// GELU took 77 us for 61 at 4001.
+template <typename T> __device__ __forceinline__ void load8(const T* p, int n, bool wide, float (&v)[8]) {
+    if (n >= 8 || wide) {
+        const int back = n < 8 ? 8 - n : 0;
         if constexpr (sizeof(T) == 2) {
             u32x4 r;
-            __builtin_memcpy(&r, __builtin_assume_aligned(p, 2), 16);
+            __builtin_memcpy(&r, __builtin_assume_aligned(p - back, 2), 16);
+            if (back) {
+                uint64_t lo = static_cast<uint64_t>(r[1]) << 32 | r[0], hi = static_cast<uint64_t>(r[3]) << 32 | r[2];
+                const int by = 16 * back;
+                lo = by < 64 ? lo >> by | hi << (64 - by) : hi >> (by - 64);
+                hi = by < 64 ? hi >> by : 0;
+                r = u32x4{static_cast<unsigned>(lo), static_cast<unsigned>(lo >> 32), static_cast<unsigned>(hi), static_cast<unsigned>(hi >> 32)};
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(r[i] << 16), v[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
         } else {
             f32x4 r[2];
-            __builtin_memcpy(&r, __builtin_assume_aligned(p, 4), 32);
+            __builtin_memcpy(&r, __builtin_assume_aligned(p - back, 4), 32);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = r[i / 4][i % 4];
+            if (back) {
+#pragma unroll
+                for (int by = 1; by < 8; by *= 2)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = back & by ? (i + by < 8 ? v[i + by < 8 ? i + by : 7] : 0.0f) : v[i];
+            }
         }
     } else {
 #pragma unroll
@@ -107,7 +123,11 @@ template <int KIND> __device__ __forceinline__ float far_of(float top, float rea
 // (a call of its own: with its registers the kernels of 14336 columns gated by GELU took 127 us for 84)
 template <int KIND> __device__ __attribute__((noinline)) double value64(double v, double w) {
     if constexpr (KIND == MOPAR_GATE_SILU) return w / (1.0 + exp(-w)) * v;
-    if constexpr (KIND == MOPAR_GATE_GELU) return 0.5 * w * erfc(w * -0.70710678118654752) * v;
+    // (1 + erf as it stands where it loses nothing: values of the top's own gate are ratios of x, ties among them, and go as this formula rounds)
+    if constexpr (KIND == MOPAR_GATE_GELU) {
+        const double z = w * 0.70710678118654752;
+        return 0.5 * w * (w >= 0.0 ? 1.0 + erf(z) : erfc(-z)) * v;
+    }
     return v * w;
 }
 
@@ -173,22 +193,23 @@ __global__ __launch_bounds__(TPR ? 256 : 1024) void rows8_kernel(const RowsParam
     float squares = 0.0f, reach = 0.0f;
     unsigned top_bits = 0;                           // of the row's largest |p|; infinities and NaN are above all others
     // p of chunk c; the first time, total is stored and the row's sums go on
+    const bool wide = p.width >= 8;
     auto read = [&](int c, float (&f)[8], bool first) __attribute__((always_inline)) {
         const int at = c * 8, n = p.width - at;
         float w[8];
         if (KIND == NORM && !first && total) {
-            load8<T>(total + at, n, f);
+            load8<T>(total + at, n, false, f);
         } else {
-            load8(x + at, n, f);
+            load8(x + at, n, wide, f);
             if (KIND == NORM && res) {
                 float r[8];
-                load8(res + at, n, r);
+                load8(res + at, n, wide, r);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] = static_cast<float>(static_cast<T>(f[i] + r[i]));
                 if (total) store8(total + at, n, f);
             }
         }
-        if constexpr (KIND != MOPAR_GATE_NONE) load8(other + at, n, w);
+        if constexpr (KIND != MOPAR_GATE_NONE) load8(other + at, n, wide, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (KIND == NORM && first) squares = __builtin_fmaf(f[i], f[i], squares);

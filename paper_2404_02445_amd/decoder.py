@@ -69,40 +69,43 @@ def alloc_rows8(rows, width, device):
     return Rows8(q[:, :width], torch.empty(rows, dtype=torch.float32, device=device))
 
 
-def _rows8(r, name, like, rows=None, width=None):
+def _rows8(r, name, device, rows, width):
     if not isinstance(r, Rows8):
         raise ValueError(f"{name}: a Rows8")
-    if r.device != like.device:
+    if r.device is not device and r.device != device:
         raise ValueError(f"{name}: another device")
-    if (rows is not None and r.rows != rows) or (width is not None and r.width != width):
+    if r.rows != rows or r.width != width:
         raise ValueError(f"{name}: {rows} rows of {width} expected")
     return r.raw
 
 
 def mopar_rms_norm(x, weight, eps=1e-6, residual=None, total=None, out=None, out8=None, stream=None):
     """Root mean square norm of x (+ residual, the sum going to total): to out, to 8-bit rows out8, or both."""
-    _need(x.dim() == 2, "x: [tokens, width]")
-    t, w = x.shape
+    if x.dim() != 2:
+        raise ValueError("x: [tokens, width]")
+    (t, w), device = x.shape, x.device
     dt = _dtype(x)
     rx = _matrix(x, "x", x)
     rr = None if residual is None else _matrix(residual, "residual", x, x.shape)
     rt = None if total is None else _matrix(total, "total", x, x.shape)
     ro = None if out is None else _matrix(out, "out", x, x.shape)
-    r8 = None if out8 is None else _rows8(out8, "out8", x, t, w)
+    r8 = None if out8 is None else _rows8(out8, "out8", device, t, w)
     wt = _vector(weight, "weight", x, w)
-    _call(lib().mopar_rms_norm, x.device, stream, dt, t, _size(w, "width"), rx, rr, rt, wt, eps, ro, r8)
+    _call(lib().mopar_rms_norm, device, stream, dt, t, _size(w, "width"), rx, rr, rt, wt, eps, ro, r8)
 
 
 def mopar_quantize_rows(x, out8, gate=None, act="silu", stream=None):
     """x, or act(gate) x ("silu" or "gelu"), as 8-bit rows out8."""
-    _need(x.dim() == 2, "x: [tokens, width]")
-    _need(act in L.GATE and (gate is None or act != "none"), "act: silu or gelu")
-    t, w = x.shape
+    if x.dim() != 2:
+        raise ValueError("x: [tokens, width]")
+    if act not in L.GATE or (gate is not None and act == "none"):
+        raise ValueError("act: silu or gelu")
+    (t, w), device = x.shape, x.device
     dt = _dtype(x)
     rx = _matrix(x, "x", x)
     rg = None if gate is None else _matrix(gate, "gate", x, x.shape)
-    r8 = _rows8(out8, "out8", x, t, w)
-    _call(lib().mopar_quantize_rows, x.device, stream, dt, t, _size(w, "width"), rx, rg, 0 if gate is None else L.GATE[act], r8)
+    r8 = _rows8(out8, "out8", device, t, w)
+    _call(lib().mopar_quantize_rows, device, stream, dt, t, _size(w, "width"), rx, rg, 0 if gate is None else L.GATE[act], r8)
     return out8
 
 
@@ -117,23 +120,27 @@ def alloc_linear8_workspace(x, w, out):
     return torch.empty(max(mopar_linear8_workspace_bytes(x.rows, w.rows, w.width), 16), dtype=torch.uint8, device=out.device)
 
 
-def _workspace(ws, like):
+def _workspace(ws, device):
     if ws is None:
         return None, 0
-    _need(ws.device == like.device and ws.is_contiguous(), "ws: a contiguous tensor on the same device")
-    return ws.data_ptr(), ws.nbytes
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError("ws: a contiguous tensor on the same device")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def mopar_linear8(x, w, out, bias=None, ws=None, stream=None):
     """out = x w^T (+ bias) of 8-bit rows x [tokens, width] and w [n_out, width]."""
-    _need(out.dim() == 2, "out: [tokens, n_out]")
-    _need(isinstance(x, Rows8) and isinstance(w, Rows8), "x and w: Rows8")
-    dt = _dtype(out)
-    rx, rw = _rows8(x, "x", out, out.shape[0], w.width), _rows8(w, "w", out, out.shape[1], w.width)
+    if out.dim() != 2:
+        raise ValueError("out: [tokens, n_out]")
+    if not isinstance(w, Rows8):
+        raise ValueError("w: a Rows8")
+    dt, device, width = _dtype(out), out.device, w.width
+    t, n_out = out.shape
+    rx, rw = _rows8(x, "x", device, t, width), _rows8(w, "w", device, n_out, width)
     ro = _matrix(out, "out", out)
-    b = _vector(bias, "bias", out, w.rows)
-    p, n = _workspace(ws, out)
-    _call(lib().mopar_linear8, out.device, stream, dt, x.rows, w.rows, _size(w.width, "width"), rx, rw, b, ro, p, n)
+    b = None if bias is None else _vector(bias, "bias", out, n_out)
+    p, n = _workspace(ws, device)
+    _call(lib().mopar_linear8, device, stream, dt, t, n_out, _size(width, "width"), rx, rw, b, ro, p, n)
     return out
 
 
@@ -166,6 +173,6 @@ def mopar_token_logprobs(logits, tokens, logprob, entropy=None, rank=None, top_l
         _need(top_id.dim() == 2 and top_id.shape[0] == t, "top_id: [rows, top]")
         top = top_id.shape[1]
     tl, ti = _vector(top_logprob, "top_logprob", logits, t * top, f32), _vector(top_id, "top_id", logits, t * top, i32)
-    p, n = _workspace(ws, logits)
+    p, n = _workspace(ws, logits.device)
     _call(lib().mopar_token_logprobs, logits.device, stream, dt, t, _size(v, "vocab"), rl, scale, tok, _size(top, "top"), lp, en, rk, tl, ti, p, n)
     return logprob
