@@ -11,9 +11,9 @@
 // error of the largest are worked out in float64 first; bf16 norms and plain rows need not, their p is exact in float32.
 //
 // Bound by memory from some hundred rows on: bf16 norms with a residual, to 8 bits, of 16384 x 4096 take 89 us (5.3 TB/s, a large copy
-// 5.2), 65536 x 256 25 us, float32 4096 x 4096 53; rows of 4096 x 14336 39 us plain, 69 by SiLU (4.3 TB/s), 76 by GELU, which
-// its 23 instructions a value bound.  Few rows wait for their loads and one reduction: 8 x 8192 4.0 us, 64 x 14336 by SiLU 7.1.  Rows that
-// start between 16-byte places cost nothing (4001 x 11007 by GELU 60 us, 11008 on such places 59).
+// 5.2), 65536 x 256 25 us, float32 4096 x 4096 53; rows of 4096 x 14336 39 us plain, 70 by SiLU (4.2 TB/s), 76 by GELU, whose
+// vector instructions (some 50 a value in all) are active 80 % of the time.  Few rows wait for their loads and one reduction: 8 x 8192 4.0 us, 64 x 14336 by SiLU 7.1.  Rows that
+// start between 16-byte places cost nothing (4001 x 11007 by GELU 59 us, 11008 on such places 58).
 #include <algorithm>
 #include <type_traits>
 
@@ -87,12 +87,14 @@ __device__ __forceinline__ float exp_(float v) {
     const float e = __builtin_amdgcn_exp2f(hi);
     return __builtin_fmaf(e, lo * 0.693147181f, e);
 }
-// erf by formula 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical Functions, off by at most 1.5e-7, and by float32's roundings:
-// of t (2 half steps, where the polynomial in t changes by at most 1.1 of itself), its five steps, e^(-x^2) and their product, of at most 1
-__device__ __forceinline__ float erf_(float x) {
-    const float ax = __builtin_fabsf(x), t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * ax);
-    const float poly = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
-    return __builtin_copysignf(1.0f - poly * __builtin_amdgcn_exp2f(ax * ax * -1.44269504f), x);
+// (1 + erf(g / sqrt 2)) / 2, erf by formula 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical Functions, off by at most
+// 1.5e-7 / 2, and by float32's roundings: of t (3 half steps, where the polynomial in t changes by at most 1.1 of itself), its five
+// steps, e^(-g^2 / 2) and their product, of at most 1/2.  The factors 1 / sqrt 2 and 1 / 2 are in the constants.
+__device__ __forceinline__ float phi_(float g) {
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(fabsf(g), 0.231641889f, 1.0f));
+    const float poly = t * (0.127414796f + t * (-0.142248368f + t * (0.7107068705f + t * (-0.7265760135f + t * 0.5307027145f))));
+    const float tail = poly * __builtin_amdgcn_exp2f(g * g * -0.72134752f);
+    return g < 0.0f ? tail : 1.0f - tail;
 }
 
 constexpr float kHalfStep = 6.0e-8f;                 // 2^-24, and the roundings of the bounds
@@ -107,13 +109,13 @@ template <int KIND> __device__ __forceinline__ float value(float v, float w, flo
     } else if constexpr (KIND == MOPAR_GATE_GELU) {
         const float g = __builtin_fmaf(w, 0.0f, fmaxf(w, -15.0f));
         reach = fabsf(g * v);
-        return 0.5f * g * (1.0f + erf_(g * 0.707106781f)) * v;
+        return g * phi_(g) * v;
     } else {
         return v;
     }
 }
 // A product of two elements: half a step.  SiLU: exponential 4 half steps, sum 1, reciprocal 2, products 3, and 88 e^-88 |x| where g
-// is below -88 or the reciprocal underflows.  GELU: erf 1.5e-7 + 20 half steps (1.35e-6 in all) and 12 more of its argument, the sum
+// is below -88 or the reciprocal underflows.  GELU: erf 1.5e-7 + 20 half steps (1.35e-6 in all) and 12 more of the sum
 // and the products, all times |g x| / 2; g below -15 leaves less than that.
 template <int KIND> __device__ __forceinline__ float far_of(float top, float reach) {
     if constexpr (KIND == NORM) return top * kHalfStep;
