@@ -278,7 +278,7 @@ __global__ __launch_bounds__(TPR ? 256 : 1024) void rows8_kernel(const RowsParam
             }
             top64 = over_row<TPR>(best, [](double a, double b) { return fmax(a, b); }, lds64);
         }
-        if (me == 0) p.scale[row] = finite ? static_cast<float>(top64 * static_cast<double>(r) / 127.0) : __builtin_nanf("");
+        if (me == 0) p.scale[row] = !finite ? __builtin_nanf("") : top64 > 0.0 ? static_cast<float>(top64 * static_cast<double>(r) / 127.0) : 0.0f;   // (r may be infinite)
     }
     // (a row whose 127 / a is past float32, or that float32 knows too little of, has all of its steps worked out in float64)
     const bool some = finite && top64 > 0.0, tiny = top64 < 1e-30;

@@ -121,6 +121,20 @@ def test_norm_rows_that_are_odd(dt):
     assert float(out8.scales[0]) == 0 and bool(out8.scales[1:4].isnan().all()) and not bool(out[2].isfinite().any())
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_norm_of_zeros_without_eps(dt):
+    """A row of zeros has scale 0 where its factor is infinite, too; others do without eps."""
+    g = gen(16)
+    x, w = randn(g, 3, 300, dt=dt), randn(g, 300, dt=dt)
+    x[1] = 0
+    out8 = P.alloc_rows8(3, 300, "cuda")
+    P.mopar_rms_norm(x, w, 0.0, out8=out8)
+    steps = R.steps(x.cpu().double() * w.cpu().double())[0]
+    scales = R.norm(x[::2], w, 0.0)[4]
+    assert torch.equal(out8.values.cpu(), steps) and float(out8.scales[1]) == 0
+    check_scales(out8.scales[::2], scales, R.sum_bound(300) + 8 * U)
+
+
 def test_norm_steps_at_their_borders():
     """Values in the middle between two steps, and next to it: halves to even, as 64-bit arithmetic rounds them."""
     k = torch.arange(-127, 127, dtype=torch.float64)
