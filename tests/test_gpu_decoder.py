@@ -472,7 +472,7 @@ class Layer:
         b["ws2"] = P.alloc_token_logprobs_workspace(b["logits"], 4)
         return b
 
-    def step(self, b, x, attend, pos, tokens):
+    def step(self, b, x, attend, tokens):
         """One layer and the head; attend(qkv rows) fills b["att"]."""
         W = self.w
         P.mopar_rms_norm(x, self.n1, out8=b["a8"])
@@ -488,7 +488,7 @@ class Layer:
         P.mopar_linear8(b["a8"], W["head"], b["logits"], ws=b["ws"])
         P.mopar_token_logprobs(b["logits"], tokens, b["lp"], entropy=b["en"], top_logprob=b["tl"], top_id=b["ti"], ws=b["ws2"])
 
-    def plain(self, x, mask_from):
+    def plain(self, x):
         """The same in float64 with the weights' values: logits of every row (causal)."""
         deq = {k: v.dequantized().cpu().double() for k, v in self.w.items()}
         t = x.shape[0]
@@ -536,8 +536,8 @@ def test_a_prompt_and_steps_over_its_cache():
         P.mopar_attention_prompt(q, turned, v, b["att"].view(t, H, 64), ints(off), max(lens))
 
     b = layer.buffers(t)
-    layer.step(b, torch.cat([s[:-1] for s in seqs]), prompt, None, ints([5] * t))
-    want = [layer.plain(s, 0) for s in seqs]
+    layer.step(b, torch.cat([s[:-1] for s in seqs]), prompt, ints([5] * t))
+    want = [layer.plain(s) for s in seqs]
     err = (b["logits"].cpu().double() - torch.cat([w[:-1] for w in want])).norm() / torch.cat([w[:-1] for w in want]).norm()
     # Activations in 8 bits with a largest of about 4 to 5 standard deviations: a step is 1/29 of one, its rounding 1/100 (uniform: 29
     # sqrt 12); six such roundings and the bf16 ones meet in the logits, each of its own sign: sqrt 8 of a 1/100, and half as much again.
@@ -555,7 +555,7 @@ def test_a_prompt_and_steps_over_its_cache():
         ws = P.alloc_attention_workspace(q, cache, 1, 64)
         P.mopar_attention_cache(q, b1["att"].view(3, H, 64), cache, ints([0, 1, 2, 3]), 1, ints(lens), 64, ws=ws)
 
-    layer.step(b1, torch.stack([s[-1] for s in seqs]), token, None, ints([5] * 3))
+    layer.step(b1, torch.stack([s[-1] for s in seqs]), token, ints([5] * 3))
     last = torch.stack([w[-1] for w in want])
     err = (b1["logits"].cpu().double() - last).norm() / last.norm()
     assert err < 0.045, float(err)
@@ -575,15 +575,15 @@ def test_captured_and_replayed():
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
-        layer.step(b, x, attend, None, tokens)
+        layer.step(b, x, attend, tokens)
     torch.cuda.current_stream().wait_stream(side)
     graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
     for gr in graphs:
         with torch.cuda.graph(gr):
-            layer.step(b, x, attend, None, tokens)
+            layer.step(b, x, attend, tokens)
     for i in range(4):
         x.copy_(randn(gen(100 + i), t, layer.width))
-        layer.step(b, x, attend, None, tokens)
+        layer.step(b, x, attend, tokens)
         torch.cuda.synchronize()
         want = {k: b[k].clone() for k in names}
         for gr in graphs:
