@@ -377,12 +377,16 @@ template <typename T, int KIND> hipError_t launch(const RowsParams& p, hipStream
     integral_constant<int, 64> t64;
     // Threads by the row's length, so that each has 1 to 4 chunks, kept in registers: 32 threads for 256 columns 24 us at 65536 rows, 64
     // (half of them idle) 39.  Where the rows leave most of the card idle, a row's loads go out at once from as many threads as
-    // it has chunks: 8 x 8192 4.0 us, 256 threads 6.5; 64 x 14336 by SiLU 7.1 with two a thread, 7.8 with four.
-    if (p.chunks > 256 && p.chunks <= 2048 && p.tokens <= 512) return p.chunks <= 1024 ? row(one) : row(two);
+    // it has chunks: 8 x 8192 4.0 us, 256 threads 6.5; norms of 64 x 2048 3.6, a wave a row 6.3; 64 x 14336 by SiLU 7.1 with two a thread, 7.8 with four.
+    if (p.chunks > 64 && p.chunks <= 2048 && p.tokens <= 512) return p.chunks <= 1024 ? row(one) : row(two);
     if (p.chunks <= 32) return rows(t32, one);
     if (p.chunks <= 64) return rows(t64, one);
     if (p.chunks <= 128) return rows(t64, two);
-    if (p.chunks <= 256) return rows(t64, four);
+    // (past 1024 columns a wave a row holds its loads for long: 16384 x 2048 norms 49.5 us, 43.3 in blocks of two a thread, 8192 x 2048 in
+    // float32 by SiLU 35.8 and 31.6; bf16 rows to 8 bits, which have two loads a value at most, 41.9 and 48.1 by SiLU)
+    if constexpr (KIND != NORM && sizeof(T) == 2) {
+        if (p.chunks <= 256) return rows(t64, four);
+    }
     if constexpr (KIND == NORM) {
         // two a thread hide the loads of the others best: 4096 x 14336 80 us, four 86
         if (p.chunks <= 2048) return row(two);
