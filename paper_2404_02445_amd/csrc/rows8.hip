@@ -254,36 +254,39 @@ __global__ __launch_bounds__(TPR ? 256 : 1024) void rows8_kernel(const RowsParam
         if constexpr (!EXACT) {
             if constexpr (KIND != NORM) reach = over_row<TPR>(reach, most, lds[2]);
             far = far_of<KIND>(top, reach);
-            // the row's largest in float64 is among those that float32 has within twice that of its largest
+            // the row's largest in float64 is among those that float32 has within twice that of its largest; among all where float32 has
+            // none (a product past its range, or an infinity or NaN of the row)
             double best = 0.0;
-            if (finite && top + far > 0.0f && mine >= top - 2.0f * far) {
+            auto with = [&](double v) __attribute__((always_inline)) { best = fabs(v) < __builtin_inf() ? fmax(best, fabs(v)) : __builtin_inf(); };
+            if (!finite || (top + far > 0.0f && mine >= top - 2.0f * far)) {
                 if constexpr (CH > 0) {
                     uint64_t near = 0;
 #pragma unroll
                     for (int k = 0; k < CH; ++k)
                         if (me + k * many < p.chunks)
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) near |= fabsf(f[k][i]) >= top - 2.0f * far ? uint64_t(1) << (8 * k + i) : 0u;
-                    for (; near; near &= near - 1) {
+                            for (int i = 0; i < 8; ++i) near |= !finite || fabsf(f[k][i]) >= top - 2.0f * far ? uint64_t(1) << (8 * k + i) : 0u;
+                    for (; near && best < __builtin_inf(); near &= near - 1) {
                         const int at = place(__builtin_ctzll(near));
-                        if (at < p.width) best = fmax(best, fabs(exact(at)));
+                        if (at < p.width) with(exact(at));
                     }
                 } else {
-                    for (int c = me; c < p.chunks; c += many) {
+                    for (int c = me; c < p.chunks && best < __builtin_inf(); c += many) {
                         read(c, f[0], false);
                         for (int i = 0; i < min(8, p.width - c * 8); ++i)
-                            if (fabsf(f[0][i]) >= top - 2.0f * far) best = fmax(best, fabs(exact(c * 8 + i)));
+                            if (!finite || fabsf(f[0][i]) >= top - 2.0f * far) with(exact(c * 8 + i));
                     }
                 }
             }
             top64 = over_row<TPR>(best, [](double a, double b) { return fmax(a, b); }, lds64);
+            finite = top64 < __builtin_inf();
         }
         if (me == 0) p.scale[row] = !finite ? __builtin_nanf("") : top64 > 0.0 ? static_cast<float>(top64 * static_cast<double>(r) / 127.0) : 0.0f;   // (r may be infinite)
     }
-    // (a row whose 127 / a is past float32, or that float32 knows too little of, has all of its steps worked out in float64)
-    const bool some = finite && top64 > 0.0, tiny = top64 < 1e-30;
-    const float inv = some && !tiny ? static_cast<float>(127.0 / top64) : 0.0f;
-    const float middle = tiny ? -1.0f : 0.5f - (far * inv * 1.01f + 127.0f * 3.0f * kHalfStep);   // how far a sure step may be from its value
+    // (a row whose a or 127 / a is past float32, or that float32 knows too little of, has all of its steps worked out in float64)
+    const bool some = finite && top64 > 0.0, rough = top64 < 1e-30 || !(top < __builtin_inff());
+    const float inv = some && !rough ? static_cast<float>(127.0 / top64) : 0.0f;
+    const float middle = rough ? -1.0f : 0.5f - (far * inv * 1.01f + 127.0f * 3.0f * kHalfStep);   // how far a sure step may be from its value
     int8_t* const q = p.q ? p.q + row * p.qs : nullptr;
     auto right = [&](int at) __attribute__((always_inline)) { return static_cast<int8_t>(rint(exact(at) * 127.0 / top64)); };
     // the steps of chunk c to its place; those that are not sure are marked

@@ -1,0 +1,43 @@
+"""Norms, gated rows and log probabilities whose factors float32 holds and whose products it does not: past its largest
+value, below its smallest, or rounded on the way where it holds few bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2404_02445_amd as P
+from tests import decoder_ref as R
+from tests.decoder_ref import U, check
+from tests.test_gpu_decoder import DT, check_marks, gen, ints, marked, randn
+
+pytestmark = pytest.mark.gpu
+
+# one width for each way that a row is held: half a wave, a wave, a block, and read twice
+WIDTHS = [200, 600, 2056, 33000]
+
+
+def check_gated(x, gate, act):
+    q, out8 = marked(*x.shape)
+    P.mopar_quantize_rows(x, out8, gate=gate, act=act)
+    steps, top = R.steps(R.gated(x, gate, act))
+    assert torch.equal(out8.values.cpu(), steps)
+    want = (top / 127).float().double()              # (infinite past float32's range)
+    check(out8.scales, want, want.abs().nan_to_num(0.0, 0.0) * 2.02 * U + 1e-45)
+    check_marks(q, x.shape[1])
+    return out8
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("width", WIDTHS)
+def test_gated_rows_past_float32(dt, act, width):
+    """Finite gates and values whose products are not finite in float32: steps of the products, their scales where float32 holds them."""
+    g = gen(width)
+    x, gate = randn(g, 6, width, dt=dt).clamp(-3, 3), randn(g, 6, width, dt=dt).clamp(-4, 4)
+    gate[0, 3], x[0, 3] = 3e38, 2.0                   # one such product
+    gate[1] *= 8e37                                   # most of a row
+    x[2], gate[2] = x[2] * 1e38, gate[2] * 9.0
+    x[3], gate[3] = x[3] * 1e38, gate[3] * 8e37       # a scale that float32 does not hold
+    gate[4], x[4], x[4, 0] = gate[4] * 8e37, x[4] * 9.0, math.inf
+    out8 = check_gated(x, gate, act)
+    assert bool(out8.scales[:3].isfinite().all()) and bool(out8.scales[3].isinf()) and bool(out8.scales[4].isnan())
