@@ -254,31 +254,51 @@ __global__ __launch_bounds__(TPR ? 256 : 1024) void rows8_kernel(const RowsParam
         if constexpr (!EXACT) {
             if constexpr (KIND != NORM) reach = over_row<TPR>(reach, most, lds[2]);
             far = far_of<KIND>(top, reach);
-            // the row's largest in float64 is among those that float32 has within twice that of its largest; among all where float32 has
-            // none (a product past its range, or an infinity or NaN of the row)
-            double best = 0.0;
-            auto with = [&](double v) __attribute__((always_inline)) { best = fabs(v) < __builtin_inf() ? fmax(best, fabs(v)) : __builtin_inf(); };
-            if (!finite || (top + far > 0.0f && mine >= top - 2.0f * far)) {
+            // the row's largest in float64 is among those that float32 has within twice that of its largest, `bar` and more; among all where
+            // float32 has none (a product past its range, or an infinity or NaN of the row), or few bits of it, or lost them all
+            float bar = top + far > 0.0f ? top - 2.0f * far : __builtin_inff();
+            if (__builtin_expect(!finite, false)) bar = -1.0f;
+            if constexpr (KIND != NORM) {
+                if (__builtin_expect(top < 1e-30f, false)) {
+                    bar = reach > 0.0f ? -1.0f : __builtin_inff();
+                    // (GELU's reach is a product, too: its rows of zeros are read again, 4096 x 14336 of them 72 us for 61)
+                    if (KIND == MOPAR_GATE_GELU && reach == 0.0f)
+                        for (int c = me; c < p.chunks; c += many) {
+                            auto largest = [&](const T* factor) __attribute__((always_inline)) {
+                                float a[8], m = 0.0f;
+                                load8(factor + c * 8, p.width - c * 8, wide, a);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(a[i]));
+                                return m;
+                            };
+                            if (largest(x) > 0.0f && largest(other) > 0.0f) bar = -1.0f;
+                        }
+                }
+            }
+            uint64_t best = 0;                       // |p| as its bits: infinities and NaN are above all others
+            auto with = [&](double v) __attribute__((always_inline)) { best = max(best, __builtin_bit_cast(uint64_t, v) & ~(uint64_t(1) << 63)); };
+            if (!(mine < bar)) {
                 if constexpr (CH > 0) {
                     uint64_t near = 0;
 #pragma unroll
                     for (int k = 0; k < CH; ++k)
                         if (me + k * many < p.chunks)
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) near |= !finite || fabsf(f[k][i]) >= top - 2.0f * far ? uint64_t(1) << (8 * k + i) : 0u;
-                    for (; near && best < __builtin_inf(); near &= near - 1) {
+                            for (int i = 0; i < 8; ++i) near |= !(fabsf(f[k][i]) < bar) ? uint64_t(1) << (8 * k + i) : 0u;
+                    for (; near; near &= near - 1) {
                         const int at = place(__builtin_ctzll(near));
                         if (at < p.width) with(exact(at));
                     }
                 } else {
-                    for (int c = me; c < p.chunks && best < __builtin_inf(); c += many) {
+                    for (int c = me; c < p.chunks; c += many) {
                         read(c, f[0], false);
                         for (int i = 0; i < min(8, p.width - c * 8); ++i)
-                            if (!finite || fabsf(f[0][i]) >= top - 2.0f * far) with(exact(c * 8 + i));
+                            if (!(fabsf(f[0][i]) < bar)) with(exact(c * 8 + i));
                     }
                 }
             }
-            top64 = over_row<TPR>(best, [](double a, double b) { return fmax(a, b); }, lds64);
+            best = min(best, uint64_t(0x7ff) << 52);     // (NaN counts as infinity)
+            top64 = over_row<TPR>(__builtin_bit_cast(double, best), [](double a, double b) { return fmax(a, b); }, lds64);
             finite = top64 < __builtin_inf();
         }
         if (me == 0) p.scale[row] = !finite ? __builtin_nanf("") : top64 > 0.0 ? static_cast<float>(top64 * static_cast<double>(r) / 127.0) : 0.0f;   // (r may be infinite)
