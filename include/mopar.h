@@ -378,7 +378,8 @@ typedef struct {
  *          and a = max |p| of the row, q = 127 p / a rounded to the nearest integer, halves
  *          to even, as 64-bit arithmetic gives it, and scale = a r / 127 (infinite past float32's
  *          range).  A row of zeros has scale 0; one with an infinity or NaN has zeros and scale NaN.
- * The sum of squares is taken in float32, so rows whose squares pass its range are off.
+ * The sum of squares is taken in float32, so rows whose squares leave its range are off (one that has neither
+ * squares nor products there counts as one of zeros).
  * `width` 1 .. 2^24 elements a row, weight [width] in dtype.  total may be x or residual, out may be x
  * or residual when total is NULL or another (same data and stride); any other
  * overlap is undefined.  tokens 0: nothing to do.

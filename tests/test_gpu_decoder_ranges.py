@@ -62,3 +62,30 @@ def test_gated_rows_below_float32(dt, act, width):
     x[3] = 0
     gate[4] = 0
     check_gated(x, gate, act)
+
+
+# --- norms -------------------------------------------------------------------------------------------
+
+def far_norms(dt, width):
+    """Rows and weights whose products leave float32's range while squares, sums and results do not; eps of each set."""
+    g = gen(width + 1)
+    x, w = randn(g, 6, width, dt=dt), randn(g, width, dt=dt)
+    x[2], x[3, ::3], x[4, 1:] = 0, 0, 0
+    return [("past", x * 1e15, w * 1e30, 1e-5), ("below", x * 1e-18, w * 1e-22, 1e-5), ("far below", x * 1e-15, w * 1e-32, 0.0), ("some below", x, w * 1e-38, 1e-5),
+            ("some far below", x * 1e-10, torch.where(torch.arange(width, device="cuda") % 2 == 0, w * 1e-32, w), 0.0)]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("which", range(5))
+def test_norm_steps_outside_float32(dt, width, which):
+    name, x, w, eps = far_norms(dt, width)[which]
+    q, out8 = marked(*x.shape)
+    P.mopar_rms_norm(x, w, eps, out8=out8)
+    steps = R.steps(x.cpu().double() * w.cpu().double())[0]
+    assert torch.equal(out8.values.cpu(), steps), name
+    some = (x != 0).any(1).cpu()                      # (without eps the factor of a row of zeros is infinite)
+    want = R.norm(x[some.cuda()], w, eps)[4].float().double()
+    check(out8.scales[some.cuda()], want, want * (R.sum_bound(width) + 8 * U) + 1e-45)
+    assert not bool(out8.scales[~some.cuda()].any())
+    check_marks(q, width)
