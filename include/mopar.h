@@ -373,7 +373,8 @@ typedef struct {
 /* Root mean square norm of the residual stream.  h = x, or x + residual rounded to
  * dtype and stored in `total` (residual and total may be NULL, total only with
  * residual);  r = 1 / sqrt(mean(h^2) + eps);
- *   out  = h r weight, rounded once (NULL: not stored)
+ *   out  = h r weight, rounded once (NULL: not stored); what h weight has below 2^-149 is lost
+ *          where r is at most 2^24
  *   out8 = h r weight in 8 bits, not rounded before (NULL: not stored): with p = h weight
  *          and a = max |p| of the row, q = 127 p / a rounded to the nearest integer, halves
  *          to even, as 64-bit arithmetic gives it, and scale = a r / 127 (infinite past float32's

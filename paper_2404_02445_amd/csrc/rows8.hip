@@ -357,10 +357,23 @@ __global__ __launch_bounds__(TPR ? 256 : 1024) void rows8_kernel(const RowsParam
         }
         return near;
     };
+    // (h w may have passed float32's range where h r w does not; what it has lost below 2^-149 is counted where r makes it more than 2^-126)
+    const bool far_out = KIND == NORM && (top_bits >= 0x7f800000u || !(r <= 16777216.0f));
     auto store_out = [&](int c, const float (&a)[8]) __attribute__((always_inline)) {
         float o[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = a[i] * r;
+        if (__builtin_expect(far_out, false)) {
+            float h[8], w[8];
+            int again = c;
+            asm volatile("" : "+v"(again));          // (addresses worked out anew, not kept in registers since the first time)
+            load(again, h, false);
+            load8(other + again * 8, p.width - again * 8, wide, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)              // fractions times fractions, and the exponents at the end
+                o[i] = ldexpf(__builtin_amdgcn_frexp_mantf(h[i]) * __builtin_amdgcn_frexp_mantf(w[i]) * __builtin_amdgcn_frexp_mantf(r),
+                              __builtin_amdgcn_frexp_expf(h[i]) + __builtin_amdgcn_frexp_expf(w[i]) + __builtin_amdgcn_frexp_expf(r));
+        }
         store8(out + c * 8, p.width - c * 8, o);
     };
     // (out may be what the exact values are read from: it is stored after them)

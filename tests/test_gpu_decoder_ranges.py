@@ -89,3 +89,25 @@ def test_norm_steps_outside_float32(dt, width, which):
     check(out8.scales[some.cuda()], want, want * (R.sum_bound(width) + 8 * U) + 1e-45)
     assert not bool(out8.scales[~some.cuda()].any())
     check_marks(q, width)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("which", range(5))
+@pytest.mark.parametrize("form", ["out", "both", "in place", "residual", "total"])
+def test_norm_results_outside_float32(dt, width, which, form):
+    name, x, w, eps = far_norms(dt, width)[which]
+    some = (x != 0).any(1)
+    want, tol = (t[some.cpu()] for t in R.norm(x, w, eps)[1:3])
+    res = torch.zeros_like(x) if form in ("residual", "total") else None
+    out = x.clone() if form == "in place" else torch.full_like(x, 7.0)
+    total = torch.empty_like(x) if form == "total" else None
+    P.mopar_rms_norm(out if form == "in place" else x, w, eps, residual=res, total=total, out=out, out8=marked(*x.shape)[1] if form == "both" else None)
+    # (check() lets 1e-37 pass: results are taken to where that is nothing.  Results below 2^-126 have a rounding of half their type's smallest
+    # value; a product below it one of 2^-150, times r where r is at most 2^24.)
+    by = 2.0 ** 60 if "below" in name else 1.0
+    r = 1 / torch.sqrt(x[some].cpu().double().square().mean(1, keepdim=True) + eps)
+    tol = tol + 2.0 ** (-134 if dt == "bf16" else -150) * 1.01 + torch.where(r > 2.0 ** 24, 0.0, r * 2.0 ** -150 * 1.01)
+    check(out[some].double() * by, want * by, tol * by, name)
+    if eps:
+        assert not bool(out[~some].any())
