@@ -114,12 +114,12 @@ template <int KIND> __device__ __forceinline__ float value(float v, float w, flo
         return v;
     }
 }
-// A product of two elements: half a step.  SiLU: exponential 4 half steps, sum 1, reciprocal 2, products 3, and 88 e^-88 |x| where g
-// is below -88 or the reciprocal underflows.  GELU: erf 1.5e-7 + 20 half steps (1.35e-6 in all) and 12 more of the sum
+// A product of two elements: half a step.  SiLU: exponential 4 half steps, sum 1, reciprocal 2, products 3, and 1.1e-36 |x| where the
+// reciprocal underflows (from g = -126 ln 2 on, where g e^g is 1.03e-36), or g is below -88.  GELU: erf 1.5e-7 + 20 half steps (1.35e-6 in all) and 12 more of the sum
 // and the products, all times |g x| / 2; g below -15 leaves less than that.
 template <int KIND> __device__ __forceinline__ float far_of(float top, float reach) {
     if constexpr (KIND == NORM) return top * kHalfStep;
-    if constexpr (KIND == MOPAR_GATE_SILU) return top * (10.0f * kHalfStep) + reach * 1e-36f;
+    if constexpr (KIND == MOPAR_GATE_SILU) return top * (10.0f * kHalfStep) + reach * 1.1e-36f;
     return reach * (0.5f * (1.35e-6f + 12.0f * kHalfStep));
 }
 // (a call of its own: with its registers the kernels of 14336 columns gated by GELU took 127 us for 84)

@@ -111,3 +111,15 @@ def test_norm_results_outside_float32(dt, width, which, form):
     check(out[some].double() * by, want * by, tol * by, name)
     if eps:
         assert not bool(out[~some].any())
+
+
+# --- where float32 holds few bits ----------------------------------------------------------------------
+
+def test_silu_gates_where_its_reciprocal_ends():
+    """1 / (1 + e^-gate) at the end of float32's normal range: what it loses there is counted in what a step may be off."""
+    gates = torch.linspace(-87.5, -87.34, 60)
+    near = torch.linspace(0.49, 0.52, 40)             # steps that the far gates' products come to
+    x = torch.full((40, 61), 1e30)
+    x[:, 0] = 127 * 1.0268e-6 / near / 30
+    gate = torch.cat([torch.full((40, 1), 30.0), gates.expand(40, 60)], 1)
+    check_gated(x.cuda(), gate.cuda(), "silu")
