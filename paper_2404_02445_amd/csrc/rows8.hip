@@ -108,8 +108,9 @@ template <int KIND> __device__ __forceinline__ float value(float v, float w, flo
         return g * __builtin_amdgcn_rcpf(1.0f + exp_(-fminf(g, 104.0f))) * v;
     } else if constexpr (KIND == MOPAR_GATE_GELU) {
         const float g = __builtin_fmaf(w, 0.0f, fmaxf(w, -15.0f));
-        reach = fabsf(g * v);
-        return g * phi_(g) * v;
+        const float gv = g * v;                                         // (first: g phi(g) of a subnormal gate may be no float32)
+        reach = fabsf(gv);
+        return gv * phi_(g);
     } else {
         return v;
     }

@@ -123,3 +123,14 @@ def test_silu_gates_where_its_reciprocal_ends():
     x[:, 0] = 127 * 1.0268e-6 / near / 30
     gate = torch.cat([torch.full((40, 1), 30.0), gates.expand(40, 60)], 1)
     check_gated(x.cuda(), gate.cuda(), "silu")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gates_of_few_bits(dt, act):
+    """Subnormal gates beside values near float32's largest: half of such a gate may be no float32."""
+    tiny = 2.0 ** (-149 if dt == "f32" else -133)
+    gate = (torch.arange(1, 202, dtype=torch.float64) * tiny).to(DT[dt])[None].repeat(3, 1)
+    x = torch.full_like(gate, 1e38)
+    x[1], gate[2, ::2] = 3e30, -gate[2, ::2]      # (201: no step is a tie)
+    check_gated(x.cuda(), gate.cuda(), act)
