@@ -157,7 +157,8 @@ __device__ __forceinline__ void finish(const LogprobParams& p, int64_t row, floa
     const bool nothing = s == 0.0f;                  // every logit is -infinity
     auto logprob = [&](float x) {
         const float z = exponent(x, m, p.c);
-        return nothing ? -kInf : z == -kInf ? (x - m) * p.scale - log2s : (z - log2s) * 0.693147181f;      // (a type's lowest value: z is past float32)
+        // (z past float32, where the logarithm is nothing beside it: halves, whose difference is not)
+        return nothing ? -kInf : z == -kInf ? (0.5f * x - 0.5f * m) * p.scale * 2.0f - log2s : (z - log2s) * 0.693147181f;
     };
     if (lane == 0) {
         p.logprob[row] = known ? logprob(xt) : -kInf;

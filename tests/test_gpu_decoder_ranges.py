@@ -134,3 +134,17 @@ def test_gates_of_few_bits(dt, act):
     x = torch.full_like(gate, 1e38)
     x[1], gate[2, ::2] = 3e30, -gate[2, ::2]      # (201: no step is a tie)
     check_gated(x.cuda(), gate.cuda(), act)
+
+
+@pytest.mark.parametrize("scale", [0.25, 0.5, 1.0, 3e-5])
+def test_logprobs_of_logits_at_both_ends(scale):
+    """Logits whose difference passes float32 where its product with the scale does not."""
+    x = torch.tensor([[3e38, -3e38, 2.9e38, -2e38, 0.0], [3.4e38, -3.4e38, -math.inf, 3.4e38, 1.0], [1.7e38, -1.8e38, 1.0, 2.0, 3.0]], device="cuda")
+    ref = R.logprobs(x, ints([1, 1, 1]), scale, 5)
+    lp, en = torch.empty(3, device="cuda"), torch.empty(3, device="cuda")
+    tl, ti = torch.empty(3, 5, device="cuda"), ints([[0] * 5] * 3)
+    P.mopar_token_logprobs(x, ints([1, 1, 1]), lp, entropy=en, top_logprob=tl, top_id=ti, scale=scale)
+    assert torch.equal(ti.cpu().long(), ref["top_id"])
+    for got, name, tol in ((lp, "logprob", "logprob_tol"), (tl, "top_logprob", "top_tol")):
+        check(got, ref[name].float().double(), ref[tol])
+    check(en, ref["entropy"], torch.full_like(ref["entropy"], ref["entropy_tol"]))
