@@ -94,18 +94,20 @@ def mopar_rms_norm(x, weight, eps=1e-6, residual=None, total=None, out=None, out
     _call(lib().mopar_rms_norm, device, stream, dt, t, _size(w, "width"), rx, rr, rt, wt, eps, ro, r8)
 
 
-def mopar_quantize_rows(x, out8, gate=None, act="silu", stream=None):
-    """x, or act(gate) x ("silu" or "gelu"), as 8-bit rows out8."""
+def mopar_quantize_rows(x, out8, gate=None, act=None, stream=None):
+    """x, or with a gate act(gate) x ("silu", which is also without act, or "gelu"), as 8-bit rows out8."""
     if x.dim() != 2:
         raise ValueError("x: [tokens, width]")
-    if act not in L.GATE or (gate is not None and act == "none"):
-        raise ValueError("act: silu or gelu")
+    if act is None:
+        act = "none" if gate is None else "silu"
+    if act not in L.GATE or (gate is None) != (act == "none"):
+        raise ValueError("act: silu or gelu with a gate, none without")
     (t, w), device = x.shape, x.device
     dt = _dtype(x)
     rx = _matrix(x, "x", x)
     rg = None if gate is None else _matrix(gate, "gate", x, x.shape)
     r8 = _rows8(out8, "out8", device, t, w)
-    _call(lib().mopar_quantize_rows, device, stream, dt, t, _size(w, "width"), rx, rg, 0 if gate is None else L.GATE[act], r8)
+    _call(lib().mopar_quantize_rows, device, stream, dt, t, _size(w, "width"), rx, rg, L.GATE[act], r8)
     return out8
 
 

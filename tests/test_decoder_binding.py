@@ -1,0 +1,18 @@
+"""What the torch binding of a decoder's steps in 8 bits refuses beyond what the entry points do (CPU only)."""
+import pytest
+import torch
+
+import paper_2404_02445_amd as P
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_an_activation_without_a_gate_is_refused(act):
+    x, q = torch.zeros(3, 40), P.alloc_rows8(3, 40, "cpu")
+    with pytest.raises(ValueError, match="gate"):
+        P.mopar_quantize_rows(x, q, act=act)
+    for kw in (dict(), dict(act=None), dict(act="none")):                    # plain rows: as far as the CPU lets them
+        with pytest.raises(ValueError, match="GPU"):
+            P.mopar_quantize_rows(x, q, **kw)
+    for kw in (dict(gate=x), dict(gate=x, act=act)):
+        with pytest.raises(ValueError, match="GPU"):
+            P.mopar_quantize_rows(x, q, **kw)
