@@ -173,6 +173,7 @@ def mopar_token_logprobs(logits, tokens, logprob, entropy=None, rank=None, top_l
     top = 0
     if top_id is not None:
         _need(top_id.dim() == 2 and top_id.shape[0] == t, "top_id: [rows, top]")
+        _need(top_logprob.shape == top_id.shape, "top_logprob: [rows, top], as top_id")
         top = top_id.shape[1]
     tl, ti = _vector(top_logprob, "top_logprob", logits, t * top, f32), _vector(top_id, "top_id", logits, t * top, i32)
     p, n = _workspace(ws, logits.device)
