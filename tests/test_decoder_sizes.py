@@ -1,5 +1,5 @@
-"""Sizes of a decoder's steps in 8 bits (CPU only, tests/asan/decoder_sizes_driver.cpp): the
-products that the GPU tests run reach every form that any size chooses."""
+"""Sizes of a decoder's steps in 8 bits (CPU only, tests/asan/decoder_sizes_driver.cpp): workspaces hold what their launches write, and
+the products that the GPU tests run reach every form that any size chooses."""
 import os
 import subprocess
 
@@ -21,6 +21,11 @@ def lines(driver, *args, text=None):
     r = subprocess.run([driver, *args], input=text, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, (r.stdout + r.stderr)[-4000:]
     return [tuple(map(int, line.split())) for line in r.stdout.splitlines()]
+
+
+def test_logprobs_workspaces_hold_their_parts(driver):
+    r = subprocess.run([driver], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "0 failed checks" in r.stdout, (r.stdout + r.stderr)[-4000:]
 
 
 def test_the_products_that_are_tested_reach_every_form(driver):
