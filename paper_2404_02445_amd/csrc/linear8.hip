@@ -6,7 +6,7 @@
 // Operands come straight to LDS, 128 bytes of k a row and stage, eight rows (1 KB) a load instruction, whole lines where rows
 // start at multiples of 128 bytes.  The weight fragment is the MFMA's first operand: a lane ends up with four neighbouring columns of
 // one row.  Chunks past the sum read zeros; a chunk that the sum ends in is cut in the fragments of x.  Rows that start off 128-byte
-// lines: 8192 x 4096 by 14336 columns 404 -> 458 us, 64 x 14336 by 4096 23 -> 34.
+// lines (by 16): 8192 x 4096 by 14336 columns 395 -> 410 us, 64 x 14336 by 4096 15.4 -> 21.1, 128 x 14336 by 4096 20.2 -> 29.4.
 #pragma clang diagnostic ignored "-Winline-asm"      // (m0, which the loads into LDS take, is in no other use)
 #include <algorithm>
 #include <type_traits>
@@ -134,8 +134,8 @@ __device__ __forceinline__ bool place_of(const Linear8Params& p, int bm, int bn,
 // barrier behind each, and the second group runs one step behind the first: while one wave of a SIMD multiplies, the other
 // reads and loads.  256: two stages of 64 KB in LDS; A0 and the columns' halves (B) are read in the first phase and loaded again,
 // for the step after next, in the second; A1 the other way round.  128: one phase, four stages of 32 KB, loads three steps
-// ahead.  At the end of a memory step eight later loads stay in flight.  Bound by the matrix units: 8192 x 4096 by 14336 columns take
-// 400 us, 2.40 POP/s.
+// ahead.  At the end of a memory step eight later loads stay in flight.  8192 x 4096 by 14336 columns take 395 to 410 us, 2.4 POP/s of
+// the card's 5 (a library product 2.3); the matrix units are busy 68 % of the cycles, the rest is the steps' barriers and the tiles' ends.
 //
 // A block runs up to kPairTiles tiles, and the loads go on into the next one during the last steps of a tile.  The scales of a
 // tile come to LDS with its first step, into the wave's own space, where its results turn at the end so that a store covers
@@ -495,9 +495,10 @@ __global__ __launch_bounds__(512, 2) void linear8_pair_kernel(const Linear8Param
 // own, 128 bytes of k of all the tile's rows and columns; the waves' sums meet in LDS at the end.  XL: 8-row loads of x a
 // stage (rows past them are never stored).
 //
-// Up to 16 rows the weight's bytes bound it (1 x 4096 by 4096 columns 5.2 us, by 28672 23.2: 5.1 TB/s), past them what a CU
-// takes in by direct loads, some 45 to 50 GB/s for all that its tiles read (64 x 4096 by 4096 7.3 us, 64 x 14336 by 4096 15).  Operands
-// straight into registers took 38 us for 23 there, and 64 x 64 tiles of waves in step with each other 13.3 us for 8.5 at 128 x 4096.
+// Up to 16 rows the weight's bytes bound it (1 x 4096 by 4096 columns 4.3 us, 5.8 with other weights in every call, by 28672 23.2: 5.1
+// TB/s).  Past them about 3 us (launch, first loads, the waves' sums) and what a CU takes in by direct loads, 70 to 90 GB/s for all that its
+// tiles read: by 4096 columns, sums of 4096 and 14336, 32 rows 5.3 and 12.5 us, 64 rows 6.7 and 15.4, 128 rows 7.9 and 20.2, 192 rows 9.5 and 24.4.
+// Operands straight into registers took 38 us for 23 there, and 64 x 64 tiles of waves in step with each other 13.3 us for 8.5 at 128 x 4096.
 // ---------------------------------------------------------------------------
 template <typename T, int FM, int XL, int FN, int W, int NS>
 __global__ __launch_bounds__(W * 64) void linear8_wave_kernel(const Linear8Params p) {
@@ -627,6 +628,9 @@ __global__ __launch_bounds__(256) void linear8_join_kernel(const Linear8Params p
 // Tile edge of linear8_pair_kernel for a product, 0 where linear8_wave_kernel runs it: its tiles have to fill the CUs.  Sums of
 // 4096 in us: 128 tiles take 31.2 for 96 rows by 28672 columns (224 tiles), the others 41.7, 22.0 and 28.1 for 512 by 6144 (192 tiles), 20.8 and
 // 16.4 for 192 by 6144 (96); 256 tiles 60.5 for 512 by 28672 (224 tiles), 128 tiles 87.8.  64 rows by 28672: 30.6 and 30.9.
+// Sums up to 256, of fewer steps than the 128 tiles load ahead, go to the other form whatever their tiles: it shares out a sum among waves of which most
+// then have none, and stores 8 bytes a lane.  8192 by 4096 in bf16, sums of 16 to 256 75 to 79 us (13 to 14 for the results' bytes),
+// sums of 272 24 in 256 tiles and 82 in the others; 1024 by 4096, 256 and 272, 12.0 and 7.5.
 static int pair_tile(int64_t m, int64_t n, int k) {
     if (k <= 256 || m <= 64) return 0;
     const int64_t tiles = (m + 255) / 256 * ((n + 255) / 256), rounds = (tiles + kCUs - 1) / kCUs;

@@ -13,7 +13,8 @@
 // What bounds it, measured (a copy reaches 5.16 TB/s): 2048 x 128000 in bf16, 524 MB, 98 us without alternatives (memory; some ten
 // vector instructions a logit, of which the exponential counts four, keep the ALUs at two thirds), 119 with five (124 between other
 // calls), 129 with 20: the pieces that are looked at again, when nothing is left to be streamed.  64 registers, for eight waves a
-// SIMD: with 72 the 2048 blocks took two rounds of the card and 147 us.  257 x 32003 in float32 10.6 us: one row more than CUs (256
+// SIMD: with 72 the 2048 blocks took two rounds of the card and 147 us.  (That bound holds in every form; those with alternatives keep three vector
+// registers in scratch memory and 28 scalar ones in lanes for it, though few rows never have eight waves on a SIMD.)  257 x 32003 in float32 10.6 us: one row more than CUs (256
 // rows 9.3).  4 x 128000 with 20 alternatives 14.4 us: two launches, two loads in a row, and six barriers.
 // Tried without gain: keeping the list up to date along the row by bitonic sorts across lanes (4 x 128000 16.7, 2048 x 128000 138 us
 // with five), by insertions one at a time (17.4, 145), loads a step ahead (168).
@@ -471,9 +472,14 @@ int logprob_splits(int64_t rows, int vocab) {
 
 // The waves of a block.  One share of a row: four (4 x 128000 14.4 us, by eight 14.8), of long rows, of which each CU has one share, eight up to 8192
 // elements and 16 past them (16 x 128000 17.1 by four, 15.0 by eight, 16.5 by 16, 32 rows 21.6, 17.9, 17.6).  Whole rows: four
-// where they fill the card many times; 16 hold two rows a CU, so past 512 rows eight (600 x 32000 29.1 us by 16, 22.8 by eight, 24.0 by
-// four), and past 256, or up to 8192 elements, where a wave of 16 has two steps and less (257 x 32003 in float32 12.5 and 10.6, 300 x
-// 128000 36.7 and 43.2, 64 x 8000 10.1 and 8.6, 200 x 32000 14.5 and 16.2).
+// where they fill the card many times; 16 hold two rows a CU, so past 512 rows eight; and eight past 256 rows of up to 32768 elements, or up to 8192,
+// where a wave of 16 has two steps and less.  Both sides of each border, bf16 without alternatives, us:
+//   four and eight   1000 x 32000 20.6 and 19.4, 1024 20.7 and 19.7, 1200 22.9 and 24.9, 1500 25.6 and 28.1;
+//                    1000 x 128000 51.8 and 45.4, 1024 52.4 and 45.7, 1200 67.7 and 65.9, 1500 77.1 and 79.9
+//   eight and 16     512 x 128000 35.9 and 30.2, 513 38.2 and 39.9; 512 x 32003 11.9 and 13.3, 513 x 32000 13.2 and 15.4
+//                    300 x 32003 11.3 and 12.8, 33000 11.3 and 12.4, 40000 12.5 and 12.7, 64000 17.0 and 16.8, 128000 34.1 and 27.7
+//                    100 x 8000 4.8 and 5.1, 8200 5.3 and 5.4, 32000 8.9 and 7.7; 200 x 8000 5.3 and 5.3, 32000 9.2 and 8.1
+// (so the borders at 1024 rows and 32768 elements lie somewhat low: up to 14 and 10 % for what is just past them).
 static int logprob_waves(int64_t rows, int vocab, int splits, int share) {
     if (splits > 1) return rows <= 8 || vocab < 65536 ? 4 : share <= 8192 ? 8 : 16;
     if (rows >= 1024) return 4;

@@ -2,13 +2,14 @@
 //
 // A row's 8-bit steps are 127 p / a, a = max |p|, rounded to the nearest integer: p = h weight for the norm (its
 // factor r is the same for the whole row and goes into the scale alone), x, or activation(gate) x.  So the sum of squares and the
-// maximum come from one pass, and a row is read once, kept in registers and written once; rows past 32768 elements are read
-// again for the second pass.
+// maximum come from one pass, and a row is read once, kept in registers and written once; rows past 32768 elements, four chunks of eight for each
+// of 1024 threads, are read (and gated) again for the second pass: 300 x 40000 by SiLU 42 us, of a floor of 12.
 //
 // The steps are those of 64-bit arithmetic.  In float32 127 p / a is off by a part that is known (value()), which decides nothing
 // unless the value lies within it of the middle between two steps: those, one in some thousands, are worked out again in float64 (a row
 // that float32 knows too little of, as one of gates all far below zero, altogether).  So that a is exact too, the values within float32's
-// error of the largest are worked out in float64 first; bf16 norms and plain rows need not, their p is exact in float32.
+// error of the largest are worked out in float64 first; bf16 norms and plain rows need not, their p is exact in float32.  Rows whose largest
+// p float32 does not hold, or holds with few bits (below 1e-30), are worked out in float64 altogether, from what is read again.
 //
 // Bound by memory from some hundred rows on: bf16 norms with a residual, to 8 bits, of 16384 x 4096 take 89 us (5.3 TB/s, a large copy
 // 5.2), 65536 x 256 25 us, float32 4096 x 4096 53; rows of 4096 x 14336 39 us plain, 70 by SiLU (4.2 TB/s), 76 by GELU, whose
@@ -436,7 +437,7 @@ template <typename T, int KIND> hipError_t launch(const RowsParams& p, hipStream
     if (p.chunks <= 32) return rows(t32, one);
     if (p.chunks <= 64) return rows(t64, one);
     if (p.chunks <= 128) return rows(t64, two);
-    // (past 1024 columns a wave a row holds its loads for long: 16384 x 2048 norms 49.5 us, 43.3 in blocks of two a thread, 8192 x 2048 in
+    // (past 1024 columns a wave a row holds its loads for long: 16384 x 2048 norms 49.5 us, 43.3 in blocks of 256 threads, a chunk each, 8192 x 2048 in
     // float32 by SiLU 35.8 and 31.6; bf16 rows to 8 bits, which have two loads a value at most, 41.9 and 48.1 by SiLU)
     if constexpr (KIND != NORM && sizeof(T) == 2) {
         if (p.chunks <= 256) return rows(t64, four);
