@@ -401,9 +401,9 @@ int mopar_quantize_rows(int32_t dtype, int64_t tokens, int32_t width, const mopa
 
 /* out[t][n] = (sum_i x.q[t][i] w.q[n][i]) x.scale[t] w.scale[n] + bias[n], for x of `tokens` and w of n_out
  * rows of `width` (1 .. 131071: the sum is exact in 32 bits) values of 8 bits, -128 .. 127; out and bias
- * (NULL: none) in dtype.  The sum and its products are float32, from left to right (sum times x.scale may not leave its range), and the
- * result is rounded to dtype.  Sums are exact in any order, so how a product is cut never shows
- * in its bits.  `ws` holds mopar_linear8_workspace_bytes, which does not fall as tokens, n_out or width grow;
+ * (NULL: none) in dtype.  The sum goes to float32, is multiplied there from left to right (its product with x.scale
+ * must not leave float32's range) and the result rounded to dtype.  Sums are exact in any order, so how a product is
+ * cut never shows in its bits.  `ws` holds mopar_linear8_workspace_bytes, which does not fall as tokens, n_out or width grow;
  * NULL: long sums with few results are not shared out, which is right and slower.  Its contents need not
  * survive between calls, and calls that overlap need one each.  out must overlap nothing
  * that is read.  tokens or n_out 0: nothing to do.
